@@ -318,6 +318,118 @@ int microadam_step_noalloc(const microadam_config* cfg, const int64_t* numels, i
                            int64_t t, void* const* params, const void* const* grads, double lr,
                            void* stream);
 
+/*
+ * ------------------------------------------------- matrix updates
+ *
+ * Orthogonalisation of an update by Newton-Schulz products, and the Muon
+ * step built on it: the rule for weight matrices that is used beside an
+ * Adam-type rule for a model's other parameters.
+ *
+ * For a rows x cols matrix G, with X0 = G / (||G||_F + eps), transposed when
+ * rows > cols, each of `steps` steps takes
+ *     A = X X^T,   B = a I + b A + c A A,   X <- B X,
+ * which applies the odd polynomial a s + b s^3 + c s^5 to the singular values
+ * of X and keeps its singular vectors.  The default coefficients (3.4445,
+ * -4.7750, 2.0315) bring singular values above about 1e-2 of ||G||_F to
+ * between 0.7 and 1.2 in 5 steps.
+ *
+ *   coefficients  host array of 3 * steps values, (a, b, c) step by step, or
+ *                 NULL for the default.  Coefficients that let a singular
+ *                 value grow beyond 7 overflow the intermediates.
+ *   eps           added to the norm; > 0 (a zero matrix gives zeros).
+ *   steps         1..16.
+ *   precision     what the products' operands are held in, with binary32
+ *                 accumulation in any case:
+ *                 MICROADAM_PRECISION_F16    binary16, scaled by powers of two
+ *                   (each rounding 2^-11, an eighth of bfloat16's at the same
+ *                   rate of the matrix cores); results are good to 1e-3 to
+ *                   3e-3 in the Frobenius norm.
+ *                 MICROADAM_PRECISION_SPLIT  a sum of two binary16 numbers
+ *                   (22 bits); three products for one; results are good to
+ *                   1e-6.
+ *                 MICROADAM_PRECISION_AUTO   SPLIT for binary32 results or
+ *                   parameters, else F16.
+ */
+enum { MICROADAM_PRECISION_AUTO = 0, MICROADAM_PRECISION_F16 = 1, MICROADAM_PRECISION_SPLIT = 2 };
+
+typedef struct microadam_schulz_config {
+  const double* coefficients;
+  double eps;
+  int32_t steps;
+  int32_t precision;
+} microadam_schulz_config;
+
+/*
+ * One matrix: rows of `cols` contiguous elements, *_ld elements apart (at
+ * least cols, below 2^31).  Addresses are aligned to the element type; rows
+ * that start at multiples of 16 bytes are read and written in vectors.
+ *   grad      read only.
+ *   momentum  updated in place (microadam_muon_step; else NULL).
+ *   out       microadam_orthogonalize: the result, which may be grad itself
+ *             when dtypes and strides agree; microadam_muon_step: the
+ *             parameter, updated in place.
+ * At most 2^20 rows and columns and 2^33 elements.
+ */
+typedef struct microadam_matrix {
+  const void* grad;
+  void* momentum;
+  void* out;
+  int64_t rows, cols;
+  int64_t grad_ld, momentum_ld, out_ld;
+} microadam_matrix;
+
+/*
+ * Workspace for a list of matrices (only rows and cols are read): *min_bytes
+ * is what the calls below accept, *useful_bytes what lets them take matrices
+ * of the list together, at most 2 GiB or one matrix if that is larger.  The
+ * list is worked off in batches of as many matrices as the workspace holds
+ * (at most 64, of at most 8 shapes); a batch takes 2 + 3 * steps launches.
+ * Either output may be NULL.  out_dtype as for the call it is meant for (the
+ * parameters' dtype for microadam_muon_step).
+ */
+int microadam_matrix_workspace(const microadam_schulz_config* cfg, const microadam_matrix* matrices,
+                               int32_t n_matrices, int32_t out_dtype, uint64_t* min_bytes,
+                               uint64_t* useful_bytes);
+
+/*
+ * out = the orthogonalised grad, matrix by matrix, queued on `stream`.
+ * Nothing is allocated on the device and no handle is kept: the workspace
+ * (256-byte aligned, of any content) belongs to the caller and is in use
+ * until the queued work is done.  The same inputs give the same bits.
+ * A matrix that holds NaN or an infinity gives NaN throughout; the others of
+ * the list are not touched by it.
+ */
+int microadam_orthogonalize(const microadam_schulz_config* cfg, const microadam_matrix* matrices,
+                            int32_t n_matrices, int32_t grad_dtype, int32_t out_dtype, void* workspace,
+                            uint64_t workspace_bytes, void* stream);
+
+/*
+ * One Muon step over a list of matrices:
+ *     V <- mu V + (1 - mu) G                       (momentum, in place)
+ *     U  = mu V + (1 - mu) G with nesterov, else V (V before its rounding)
+ *     W <- (1 - lr * weight_decay) W - lr * s * orthogonalised U
+ * with s = 0.2 sqrt(max(rows, cols)) for MICROADAM_SCALE_MATCH_RMS (the root
+ * mean square of an Adam update, so that Adam's learning rates carry over),
+ * sqrt(max(1, rows / cols)) for MICROADAM_SCALE_SPECTRAL and 1 for
+ * MICROADAM_SCALE_NONE.  V starts as zeros, which the caller provides.
+ * Workspace, order and non-finite values as for microadam_orthogonalize.  The
+ * matrices of one list must not overlap.
+ */
+enum { MICROADAM_SCALE_MATCH_RMS = 0, MICROADAM_SCALE_SPECTRAL = 1, MICROADAM_SCALE_NONE = 2 };
+
+typedef struct microadam_muon_config {
+  microadam_schulz_config schulz;
+  double momentum;     /* mu in [0, 1) */
+  double weight_decay; /* >= 0 */
+  int32_t nesterov;    /* 0 or 1 */
+  int32_t scale;
+} microadam_muon_config;
+
+int microadam_muon_step(const microadam_muon_config* cfg, const microadam_matrix* matrices,
+                        int32_t n_matrices, int32_t grad_dtype, int32_t momentum_dtype,
+                        int32_t param_dtype, double lr, void* workspace, uint64_t workspace_bytes,
+                        void* stream);
+
 const char* microadam_error_string(int code);
 
 /* The calling thread's most recent error message ("" if none). */

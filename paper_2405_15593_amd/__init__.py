@@ -30,6 +30,12 @@ MICROADAM_F32 = 0
 MICROADAM_BF16 = 1
 MICROADAM_ROUND_NEAREST = 0
 MICROADAM_ROUND_RANDOMIZED = 1
+MICROADAM_PRECISION_AUTO = 0
+MICROADAM_PRECISION_F16 = 1
+MICROADAM_PRECISION_SPLIT = 2
+MICROADAM_SCALE_MATCH_RMS = 0
+MICROADAM_SCALE_SPECTRAL = 1
+MICROADAM_SCALE_NONE = 2
 
 
 class microadam_config(ctypes.Structure):
@@ -77,13 +83,45 @@ class microadam_layout(ctypes.Structure):
         return self.last_block if q == self.num_blocks - 1 else self.first_block + q
 
 
+class microadam_schulz_config(ctypes.Structure):
+    _fields_ = [
+        ("coefficients", ctypes.POINTER(ctypes.c_double)),
+        ("eps", ctypes.c_double),
+        ("steps", ctypes.c_int32),
+        ("precision", ctypes.c_int32),
+    ]
+
+
+class microadam_muon_config(ctypes.Structure):
+    _fields_ = [
+        ("schulz", microadam_schulz_config),
+        ("momentum", ctypes.c_double),
+        ("weight_decay", ctypes.c_double),
+        ("nesterov", ctypes.c_int32),
+        ("scale", ctypes.c_int32),
+    ]
+
+
+class microadam_matrix(ctypes.Structure):
+    _fields_ = [
+        ("grad", ctypes.c_void_p),
+        ("momentum", ctypes.c_void_p),
+        ("out", ctypes.c_void_p),
+        ("rows", ctypes.c_int64),
+        ("cols", ctypes.c_int64),
+        ("grad_ld", ctypes.c_int64),
+        ("momentum_ld", ctypes.c_int64),
+        ("out_ld", ctypes.c_int64),
+    ]
+
+
 # every symbol include/microadam.h declares
 EXPORTS = (
     "microadam_state_bytes", "microadam_init", "microadam_step", "microadam_destroy",
     "microadam_get_step", "microadam_set_step", "microadam_tensor_layout",
     "microadam_debug_moments", "microadam_step_kernels", "microadam_set_profiling", "microadam_kernel_times",
     "microadam_kernel_times_total", "microadam_step_noalloc", "microadam_error_string",
-    "microadam_last_error",
+    "microadam_last_error", "microadam_matrix_workspace", "microadam_orthogonalize", "microadam_muon_step",
 )
 
 
@@ -121,6 +159,12 @@ def load(path: str = LIBRARY):
     lib.microadam_set_profiling.argtypes = [vp, i32]
     lib.microadam_kernel_times.argtypes = [vp, P(ctypes.c_float)]
     lib.microadam_kernel_times_total.argtypes = [vp, P(ctypes.c_float), P(i64)]
+    lib.microadam_matrix_workspace.argtypes = [P(microadam_schulz_config), P(microadam_matrix), i32, i32, P(u64),
+                                               P(u64)]
+    lib.microadam_orthogonalize.argtypes = [P(microadam_schulz_config), P(microadam_matrix), i32, i32, i32, vp, u64,
+                                            vp]
+    lib.microadam_muon_step.argtypes = [P(microadam_muon_config), P(microadam_matrix), i32, i32, i32, i32,
+                                        ctypes.c_double, vp, u64, vp]
     lib.microadam_error_string.argtypes = [ctypes.c_int]
     lib.microadam_error_string.restype = ctypes.c_char_p
     lib.microadam_last_error.argtypes = []
@@ -128,7 +172,8 @@ def load(path: str = LIBRARY):
     for f in ("microadam_state_bytes", "microadam_init", "microadam_step", "microadam_destroy",
               "microadam_set_step", "microadam_tensor_layout", "microadam_debug_moments",
               "microadam_step_kernels", "microadam_set_profiling", "microadam_kernel_times",
-              "microadam_kernel_times_total", "microadam_step_noalloc"):
+              "microadam_kernel_times_total", "microadam_step_noalloc", "microadam_matrix_workspace",
+              "microadam_orthogonalize", "microadam_muon_step"):
         getattr(lib, f).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -247,6 +292,44 @@ def microadam_kernel_times_total(h: int) -> tuple:
     _check(load().microadam_kernel_times_total(ctypes.c_void_p(h), out, ctypes.byref(n)),
            "microadam_kernel_times_total")
     return float(out[0]), float(out[1]), int(n.value)
+
+
+def make_schulz_config(steps=5, coefficients=None, eps=1e-7,
+                       precision=MICROADAM_PRECISION_AUTO) -> microadam_schulz_config:
+    """`coefficients`: None (the default (a, b, c) at every step), one (a, b, c)
+    for every step, or one per step."""
+    cfg = microadam_schulz_config(None, float(eps), int(steps), int(precision))
+    if coefficients is not None:
+        flat = [float(x) for c in coefficients for x in (c if isinstance(c, (tuple, list)) else (c,))]
+        if len(flat) == 3:
+            flat = flat * int(steps)
+        if len(flat) != 3 * int(steps):
+            raise ValueError(f"coefficients: (a, b, c), or one for each of the {steps} steps")
+        cfg.coefficients = (ctypes.c_double * len(flat))(*flat)   # the structure keeps the array alive
+    return cfg
+
+
+def microadam_matrix_workspace(cfg: microadam_schulz_config, matrices, n: int, out_dtype: int) -> tuple:
+    """(min bytes, useful bytes) for an array of microadam_matrix."""
+    lo, hi = ctypes.c_uint64(0), ctypes.c_uint64(0)
+    _check(load().microadam_matrix_workspace(ctypes.byref(cfg), matrices, n, out_dtype, ctypes.byref(lo),
+                                             ctypes.byref(hi)), "microadam_matrix_workspace")
+    return lo.value, hi.value
+
+
+def microadam_orthogonalize(cfg: microadam_schulz_config, matrices, n: int, grad_dtype: int, out_dtype: int,
+                            workspace_ptr: int, workspace_bytes: int, stream: int = 0) -> None:
+    _check(load().microadam_orthogonalize(ctypes.byref(cfg), matrices, n, grad_dtype, out_dtype,
+                                          ctypes.c_void_p(workspace_ptr), workspace_bytes, ctypes.c_void_p(stream)),
+           "microadam_orthogonalize")
+
+
+def microadam_muon_step(cfg: microadam_muon_config, matrices, n: int, grad_dtype: int, momentum_dtype: int,
+                        param_dtype: int, lr: float, workspace_ptr: int, workspace_bytes: int,
+                        stream: int = 0) -> None:
+    _check(load().microadam_muon_step(ctypes.byref(cfg), matrices, n, grad_dtype, momentum_dtype, param_dtype,
+                                      float(lr), ctypes.c_void_p(workspace_ptr), workspace_bytes,
+                                      ctypes.c_void_p(stream)), "microadam_muon_step")
 
 
 def microadam_error_string(code: int) -> str:

@@ -1,5 +1,5 @@
 """Builds libmicroadam.so (HIP for gfx950) in-tree with hipcc: every source
-of csrc/ is compiled to an object file in parallel, then linked."""
+of csrc/ and csrc/ops/ is compiled to an object file in parallel, then linked."""
 from __future__ import annotations
 
 import concurrent.futures as cf
@@ -10,6 +10,7 @@ import subprocess
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
+OPS = os.path.join(CSRC, "ops")   # the loss and matrix-update operators
 INCLUDE = os.path.join(ROOT, "include")
 LIBRARY = os.path.join(PKG, "libmicroadam.so")
 OBJDIR = os.path.join(PKG, "_build")
@@ -22,22 +23,23 @@ COMPILE_FLAGS = [
     "-ffp-contract=off",
     # no packed FP32 instructions in generated code
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-    # device code: min/max without IEEE NaN quieting, so that they fuse with
-    # lane permutes (gradients are taken to be finite)
-    "-Xarch_device", "-fno-honor-nans", "-Xarch_device", "-mno-amdgpu-ieee",
     "-Wall", "-Wno-unused-function",
     "-I", INCLUDE, "-I", CSRC,
 ]
+# the optimizer step's device code: min/max without IEEE NaN quieting, so that
+# they fuse with lane permutes (gradients are taken to be finite)
+FINITE_FLAGS = ["-Xarch_device", "-fno-honor-nans", "-Xarch_device", "-mno-amdgpu-ieee"]
 LINK_FLAGS = ["--offload-arch=gfx950", "-shared", "-fPIC", "-Wl,-rpath,/opt/rocm/lib"]
 
 
 def sources() -> list[str]:
-    return sorted(glob.glob(os.path.join(CSRC, "*.hip")) + glob.glob(os.path.join(CSRC, "*.cpp")))
+    return sorted(f for d in (CSRC, OPS) for kind in ("*.hip", "*.cpp") for f in glob.glob(os.path.join(d, kind)))
 
 
 def _compile(src: str) -> str:
     obj = os.path.join(OBJDIR, os.path.basename(src) + ".o")
-    cmd = [HIPCC, *COMPILE_FLAGS, "-x", "hip", "-c", src, "-o", obj + ".tmp"]
+    flags = COMPILE_FLAGS if os.path.dirname(src) == OPS else COMPILE_FLAGS + FINITE_FLAGS
+    cmd = [HIPCC, *flags, "-x", "hip", "-c", src, "-o", obj + ".tmp"]
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
         raise RuntimeError(f"hipcc failed on {os.path.basename(src)} ({res.returncode}):\n{res.stderr[-6000:]}")

@@ -15,6 +15,7 @@
 
 #include "microadam.h"
 #include "microadam_device.h"
+#include "ops/ops_host.h"
 
 using microadam::StepParams;
 using microadam::TensorDesc;
@@ -871,3 +872,10 @@ const char* microadam_error_string(int code) {
 const char* microadam_last_error(void) { return g_last_error; }
 
 }  // extern "C"
+
+// The same reporting for the entry points of other files.
+namespace microadam {
+int report(int code, const char* msg) { return fail(code, msg); }
+int report_hip(hipError_t e, const char* what) { return hip_fail(e, what); }
+void clear_report() { clear_error(); }
+}  // namespace microadam

@@ -1,0 +1,226 @@
+// The two passes before the Newton-Schulz products: the Frobenius norm of
+// each matrix's update, then the update itself, normalised, as the binary16
+// iterate X and its transpose.
+//
+//   V' = mu V + (1 - mu) G;  U = mu V' + (1 - mu) G (Nesterov) or V';
+//   without momentum U = G.      X = S_X U / (||U||_F + eps)
+//
+// Both passes are bound by memory: they read G and V twice and write V', X
+// and X^T once.  U is not kept between them (it would have to be written and
+// read again), and the squares are summed in binary64, so neither tiny nor
+// huge gradients leave the range.  Every sum has a fixed order.
+#include "schulz_device.h"
+
+namespace microadam {
+namespace {
+
+typedef _Float16 half_t;
+typedef half_t half8 __attribute__((ext_vector_type(8)));
+typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
+typedef float float4v __attribute__((ext_vector_type(4)));
+
+__device__ inline float bf16_to_f32(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
+
+__device__ inline uint16_t f32_to_bf16(float x) {
+  const uint32_t u = __float_as_uint(x);
+  if ((u & 0x7fffffffu) > 0x7f800000u) return (uint16_t)((u >> 16) | 0x40);
+  return (uint16_t)((u + 0x7fffu + ((u >> 16) & 1)) >> 16);
+}
+
+// Up to eight elements of a row at element offset `at`, zeros past `count`.
+// A 16-byte aligned address is read in vectors where all eight exist.
+__device__ inline void load8(const void* base, int64_t at, int count, bool bf16, float* v) {
+  if (bf16) {
+    const uint16_t* p = (const uint16_t*)base + at;
+    if (count >= 8 && ((uintptr_t)p & 15) == 0) {
+      const uint4v q = *(const uint4v*)p;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __uint_as_float(q[i] << 16);
+        v[2 * i + 1] = __uint_as_float(q[i] & 0xffff0000u);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = i < count ? bf16_to_f32(p[i]) : 0.0f;
+    }
+  } else {
+    const float* p = (const float*)base + at;
+    if (count >= 8 && ((uintptr_t)p & 15) == 0) {
+      const float4v q0 = *(const float4v*)p, q1 = *(const float4v*)(p + 4);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        v[i] = q0[i];
+        v[4 + i] = q1[i];
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = i < count ? p[i] : 0.0f;
+    }
+  }
+}
+
+__device__ inline void store8(void* base, int64_t at, int count, bool bf16, const float* v) {
+  if (bf16) {
+    uint16_t* p = (uint16_t*)base + at;
+    if (count >= 8 && ((uintptr_t)p & 15) == 0) {
+      uint4v q;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        q[i] = (uint32_t)f32_to_bf16(v[2 * i]) | ((uint32_t)f32_to_bf16(v[2 * i + 1]) << 16);
+      *(uint4v*)p = q;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i < count) p[i] = f32_to_bf16(v[i]);
+    }
+  } else {
+    float* p = (float*)base + at;
+    if (count >= 8 && ((uintptr_t)p & 15) == 0) {
+      *(float4v*)p = float4v{v[0], v[1], v[2], v[3]};
+      *(float4v*)(p + 4) = float4v{v[4], v[5], v[6], v[7]};
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i < count) p[i] = v[i];
+    }
+  }
+}
+
+// The update of eight elements; v8 becomes the new momentum.
+__device__ inline void update8(const PackArgs& a, const float* g8, float* v8, bool momentum, float* u8) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    if (!momentum) {
+      u8[i] = g8[i];
+      continue;
+    }
+    v8[i] = a.mu * v8[i] + a.one_minus_mu * g8[i];
+    u8[i] = a.nesterov ? a.mu * v8[i] + a.one_minus_mu * g8[i] : v8[i];
+  }
+}
+
+__device__ inline double wave_sum(double x) {
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d);
+  return x;
+}
+
+// grid: (n_parts, matrices); part b takes every n_parts-th run of eight.
+__global__ __launch_bounds__(256) void norm_kernel(const PackArgs a) {
+  const int mat = blockIdx.y;
+  const SchulzGroup& g = a.group[a.of[mat]];
+  const bool tall = a.tall[mat];
+  const int rows = tall ? g.n : g.m, cols = tall ? g.m : g.n;
+  const PackMatrix& pm = a.mat[mat];
+  const bool momentum = pm.momentum != nullptr;
+  const uint32_t runs = (uint32_t)(cols + 7) / 8;
+  const int64_t total = (int64_t)runs * rows;
+  double sum = 0.0;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)a.n_parts * 256) {
+    const int64_t row = total < ((int64_t)1 << 32) ? (int64_t)((uint32_t)i / runs) : i / runs;
+    const int col = (int)(i - row * runs) * 8;
+    const int count = cols - col;
+    float g8[8], v8[8], u8[8];
+    load8(pm.grad, row * pm.grad_ld + col, count, a.grad_bf16, g8);
+    if (momentum) load8(pm.momentum, row * pm.momentum_ld + col, count, a.momentum_bf16, v8);
+    update8(a, g8, v8, momentum, u8);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum += (double)u8[k] * (double)u8[k];
+  }
+  __shared__ double part[4];
+  sum = wave_sum(sum);
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) a.partials[mat * kNormParts + blockIdx.x] = (part[0] + part[1]) + (part[2] + part[3]);
+}
+
+constexpr int kLdsRow = 64 + 8;  // halves per staged row: 16-byte aligned, off by 16 bytes per row
+
+// grid: (64 x 64 tiles of the largest padded matrix, matrices).
+__global__ __launch_bounds__(256) void pack_kernel(const PackArgs a) {
+  const int mat = blockIdx.y;
+  const SchulzGroup& g = a.group[a.of[mat]];
+  const bool tall = a.tall[mat];
+  const int rows = tall ? g.n : g.m, cols = tall ? g.m : g.n;
+  const int rows_p = tall ? g.np : g.mp, cols_p = tall ? g.mp : g.np;
+  const int tiles_c = cols_p / 64;
+  if ((int64_t)blockIdx.x >= (int64_t)tiles_c * (rows_p / 64)) return;  // the whole workgroup
+  const int r0 = (int)(blockIdx.x / tiles_c) * 64, c0 = (int)(blockIdx.x % tiles_c) * 64;
+
+  __shared__ double part[4];
+  __shared__ __align__(16) half_t stage[2][64 * kLdsRow];
+  double sum = (int)threadIdx.x < a.n_parts ? a.partials[mat * kNormParts + threadIdx.x] : 0.0;
+  sum = wave_sum(sum);
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
+  __syncthreads();
+  const double scale = (double)kScaleX / (sqrt((part[0] + part[1]) + (part[2] + part[3])) + a.eps);
+
+  const PackMatrix& pm = a.mat[mat];
+  const bool momentum = pm.momentum != nullptr;
+  uint8_t* rec = a.ws + g.base + (uint64_t)(mat - g.first) * g.record;
+  // the copy in the caller's orientation, and the transposed one
+  half_t* same = (half_t*)(rec + (tall ? g.xt : g.x));
+  half_t* flip = (half_t*)(rec + (tall ? g.x : g.xt));
+  const int64_t plane = (int64_t)g.mp * g.np;
+
+#pragma unroll
+  for (int it = 0; it < 2; ++it) {
+    const int r = (int)(threadIdx.x >> 3) + it * 32, c = (int)(threadIdx.x & 7) * 8;
+    const int row = r0 + r, col = c0 + c;
+    half8 hi, lo;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) hi[i] = lo[i] = (half_t)0.0f;
+    const int count = row < rows ? cols - col : 0;
+    if (count > 0) {
+      float g8[8], v8[8], u8[8];
+      load8(pm.grad, (int64_t)row * pm.grad_ld + col, count, a.grad_bf16, g8);
+      if (momentum) load8(pm.momentum, (int64_t)row * pm.momentum_ld + col, count, a.momentum_bf16, v8);
+      update8(a, g8, v8, momentum, u8);
+      if (momentum) store8(pm.momentum, (int64_t)row * pm.momentum_ld + col, count, a.momentum_bf16, v8);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float x = (float)((double)u8[i] * scale);
+        hi[i] = (half_t)x;
+        lo[i] = (half_t)((x - (float)hi[i]) * kSplitScale);
+      }
+    }
+    *(half8*)(same + (int64_t)row * cols_p + col) = hi;
+    if (a.split) *(half8*)(same + plane + (int64_t)row * cols_p + col) = lo;
+    *(half8*)&stage[0][r * kLdsRow + c] = hi;
+    if (a.split) *(half8*)&stage[1][r * kLdsRow + c] = lo;
+  }
+  __syncthreads();
+  for (int p = 0; p <= (a.split ? 1 : 0); ++p) {
+#pragma unroll
+    for (int it = 0; it < 2; ++it) {
+      const int c = (int)(threadIdx.x >> 3) + it * 32, r = (int)(threadIdx.x & 7) * 8;
+      half8 v;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = stage[p][(r + i) * kLdsRow + c];
+      *(half8*)(flip + p * plane + (int64_t)(c0 + c) * rows_p + r0 + r) = v;
+    }
+  }
+}
+
+}  // namespace
+
+hipError_t launch_schulz_norm(const PackArgs& a, int n_matrices, hipStream_t s) {
+  if (n_matrices < 1 || n_matrices > kMaxMatrices || a.n_parts < 1 || a.n_parts > kNormParts)
+    return hipErrorInvalidValue;
+  norm_kernel<<<dim3((unsigned)a.n_parts, (unsigned)n_matrices), 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_schulz_pack(const PackArgs& a, int n_matrices, hipStream_t s) {
+  if (n_matrices < 1 || n_matrices > kMaxMatrices) return hipErrorInvalidValue;
+  int64_t tiles = 0;
+  for (int i = 0; i < a.n_groups; ++i) {
+    const int64_t t = (int64_t)(a.group[i].mp / 64) * (a.group[i].np / 64);
+    if (t > tiles) tiles = t;
+  }
+  if (tiles >= ((int64_t)1 << 24)) return hipErrorInvalidValue;
+  pack_kernel<<<dim3((unsigned)tiles, (unsigned)n_matrices), 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace microadam
