@@ -430,6 +430,57 @@ int microadam_muon_step(const microadam_muon_config* cfg, const microadam_matrix
                         int32_t param_dtype, double lr, void* workspace, uint64_t workspace_bytes,
                         void* stream);
 
+/*
+ * ------------------------------------------------- token log probabilities
+ *
+ * `rows` rows of `vocab` logits x, ld elements apart (at least vocab), and one
+ * token per row.  With z = x / temperature, lp_v = z_v - log sum exp z and
+ * p = exp lp:
+ *     logp = lp at the row's token,   entropy = -sum p lp  (0 where p = 0),
+ * all sums in binary32, each exponent taken from the row's maximum.  vocab is
+ * at most 2^24, rows at most 2^20; addresses are aligned to their element
+ * type (rows may start anywhere; 16 bytes at a time are read either way).
+ *   - A row whose token is ignore_index is not read: logp and entropy 0,
+ *     alternatives 0 and -1, gradient 0.
+ *   - Logits of -inf (or so low that their p is 0) are tokens that cannot
+ *     occur.  A row with no other: logp -inf, entropy 0, alternatives -inf at
+ *     0, 1, .., gradient 0.
+ *   - A row with NaN or +inf: logp, entropy and gradient NaN, alternatives NaN
+ *     and -1.
+ *   - A token outside [0, vocab) that is not ignore_index: logp NaN, gradient
+ *     NaN (nothing outside the row is read).
+ * The same inputs give the same bits (rows that start elsewhere within 16
+ * bytes are summed in another order).
+ */
+typedef struct microadam_logits {
+  const void* data;
+  const int64_t* targets; /* rows tokens */
+  int64_t rows, vocab, ld;
+  int64_t ignore_index;
+  double temperature; /* finite, > 0 */
+  int32_t dtype;      /* MICROADAM_F32 or MICROADAM_BF16 */
+  int32_t reserved;   /* 0 */
+} microadam_logits;
+
+/*
+ * logp[rows], entropy[rows] (either may be NULL) and, with top_k > 0 (at most
+ * 64 and vocab), the top_k most probable tokens of each row in order, ties to
+ * the lowest index: top_logprobs and top_indices [rows][top_k].
+ */
+int microadam_token_logprobs(const microadam_logits* logits, int32_t top_k, float* logp,
+                             float* entropy, float* top_logprobs, int64_t* top_indices, void* stream);
+
+/*
+ * logp and entropy (either may be NULL) and, in the same pass, the gradient of
+ *     L = sum over rows of grad_logp * logp + grad_entropy * entropy
+ * with respect to the logits: grad[rows][vocab] of the logits' dtype, grad_ld
+ * elements from row to row.  grad_entropy may be NULL (zeros).  grad may be
+ * the logits themselves when the row strides agree.
+ */
+int microadam_token_logprobs_grad(const microadam_logits* logits, const float* grad_logp,
+                                  const float* grad_entropy, float* logp, float* entropy, void* grad,
+                                  int64_t grad_ld, void* stream);
+
 const char* microadam_error_string(int code);
 
 /* The calling thread's most recent error message ("" if none). */

@@ -115,6 +115,20 @@ class microadam_matrix(ctypes.Structure):
     ]
 
 
+class microadam_logits(ctypes.Structure):
+    _fields_ = [
+        ("data", ctypes.c_void_p),
+        ("targets", ctypes.c_void_p),
+        ("rows", ctypes.c_int64),
+        ("vocab", ctypes.c_int64),
+        ("ld", ctypes.c_int64),
+        ("ignore_index", ctypes.c_int64),
+        ("temperature", ctypes.c_double),
+        ("dtype", ctypes.c_int32),
+        ("reserved", ctypes.c_int32),
+    ]
+
+
 # every symbol include/microadam.h declares
 EXPORTS = (
     "microadam_state_bytes", "microadam_init", "microadam_step", "microadam_destroy",
@@ -122,6 +136,7 @@ EXPORTS = (
     "microadam_debug_moments", "microadam_step_kernels", "microadam_set_profiling", "microadam_kernel_times",
     "microadam_kernel_times_total", "microadam_step_noalloc", "microadam_error_string",
     "microadam_last_error", "microadam_matrix_workspace", "microadam_orthogonalize", "microadam_muon_step",
+    "microadam_token_logprobs", "microadam_token_logprobs_grad",
 )
 
 
@@ -165,6 +180,8 @@ def load(path: str = LIBRARY):
                                             vp]
     lib.microadam_muon_step.argtypes = [P(microadam_muon_config), P(microadam_matrix), i32, i32, i32, i32,
                                         ctypes.c_double, vp, u64, vp]
+    lib.microadam_token_logprobs.argtypes = [P(microadam_logits), i32, vp, vp, vp, vp, vp]
+    lib.microadam_token_logprobs_grad.argtypes = [P(microadam_logits), vp, vp, vp, vp, vp, i64, vp]
     lib.microadam_error_string.argtypes = [ctypes.c_int]
     lib.microadam_error_string.restype = ctypes.c_char_p
     lib.microadam_last_error.argtypes = []
@@ -173,7 +190,8 @@ def load(path: str = LIBRARY):
               "microadam_set_step", "microadam_tensor_layout", "microadam_debug_moments",
               "microadam_step_kernels", "microadam_set_profiling", "microadam_kernel_times",
               "microadam_kernel_times_total", "microadam_step_noalloc", "microadam_matrix_workspace",
-              "microadam_orthogonalize", "microadam_muon_step"):
+              "microadam_orthogonalize", "microadam_muon_step", "microadam_token_logprobs",
+              "microadam_token_logprobs_grad"):
         getattr(lib, f).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -330,6 +348,20 @@ def microadam_muon_step(cfg: microadam_muon_config, matrices, n: int, grad_dtype
     _check(load().microadam_muon_step(ctypes.byref(cfg), matrices, n, grad_dtype, momentum_dtype, param_dtype,
                                       float(lr), ctypes.c_void_p(workspace_ptr), workspace_bytes,
                                       ctypes.c_void_p(stream)), "microadam_muon_step")
+
+
+def microadam_token_logprobs(logits: microadam_logits, top_k: int, logp_ptr: int, entropy_ptr: int,
+                             top_logprobs_ptr: int, top_indices_ptr: int, stream: int = 0) -> None:
+    _check(load().microadam_token_logprobs(ctypes.byref(logits), top_k, logp_ptr, entropy_ptr, top_logprobs_ptr,
+                                           top_indices_ptr, stream), "microadam_token_logprobs")
+
+
+def microadam_token_logprobs_grad(logits: microadam_logits, grad_logp_ptr: int, grad_entropy_ptr: int,
+                                  logp_ptr: int, entropy_ptr: int, grad_ptr: int, grad_ld: int,
+                                  stream: int = 0) -> None:
+    _check(load().microadam_token_logprobs_grad(ctypes.byref(logits), grad_logp_ptr, grad_entropy_ptr, logp_ptr,
+                                                entropy_ptr, grad_ptr, grad_ld, stream),
+           "microadam_token_logprobs_grad")
 
 
 def microadam_error_string(code: int) -> str:

@@ -1,0 +1,164 @@
+"""Log probabilities of given tokens from logits, with the distribution's
+entropy, the most probable alternatives and the gradient, over the C ABI
+(``microadam_token_logprobs``, ``microadam_token_logprobs_grad``).
+
+``token_logprobs`` is differentiable in the logits through ``logp`` and
+``entropy``; a loss made of them (``-logp.mean()``, a policy gradient, an
+entropy bonus) trains as usual.  Where the loss's weight of every token is
+known before the call, ``token_logprobs_and_grad`` gives the values and the
+gradient in one pass over the logits.
+
+Logits are float32 or bfloat16 on a ROCm device, (..., vocab) with contiguous
+rows at one stride; targets are int64 of the leading shape, with
+``ignore_index`` for rows to leave out.  Work is queued on torch's current
+stream.
+"""
+from __future__ import annotations
+
+from typing import NamedTuple, Optional
+
+import torch
+
+from . import (MICROADAM_BF16, MICROADAM_F32, microadam_logits, microadam_token_logprobs,
+               microadam_token_logprobs_grad)
+
+_DTYPES = {torch.float32: MICROADAM_F32, torch.bfloat16: MICROADAM_BF16}
+
+
+class TokenLogprobs(NamedTuple):
+    logp: torch.Tensor                        # (...) float32
+    entropy: torch.Tensor                     # (...) float32
+    top_logprobs: Optional[torch.Tensor]      # (..., top_k) float32, or None
+    top_indices: Optional[torch.Tensor]       # (..., top_k) int64, or None
+
+
+class TokenLogprobsGrad(NamedTuple):
+    logp: torch.Tensor
+    entropy: torch.Tensor
+    grad: torch.Tensor                        # of the logits' shape and dtype
+
+
+def _rows(logits: torch.Tensor, targets: torch.Tensor):
+    """(logits as [rows, vocab], their row stride, targets as [rows])."""
+    code = _DTYPES.get(logits.dtype)
+    if code is None:
+        raise TypeError(f"logits: float32 or bfloat16, not {logits.dtype}")
+    if targets.dtype != torch.int64:
+        raise TypeError(f"targets: int64, not {targets.dtype}")
+    if not logits.is_cuda or targets.device != logits.device:
+        raise ValueError("logits and targets: tensors on one ROCm device")
+    if logits.dim() < 1 or targets.shape != logits.shape[:-1]:
+        raise ValueError("targets: the shape of logits without its last dimension")
+    vocab = logits.shape[-1]
+    if vocab > 1 and logits.stride(-1) != 1:
+        raise ValueError("logits: contiguous rows")
+    flat = logits if logits.dim() == 2 else logits.flatten(0, -2) if logits.dim() > 2 else logits[None]
+    rows = flat.shape[0]
+    ld = flat.stride(0) if rows > 1 else max(1, vocab)
+    if flat.data_ptr() != logits.data_ptr() or (rows > 1 and ld < vocab):
+        raise ValueError("logits: rows at one stride, not overlapping")
+    return code, flat, ld, targets.reshape(-1).contiguous()
+
+
+def _struct(code, flat, ld, targets, ignore_index, temperature):
+    rows, vocab = flat.shape
+    return microadam_logits(flat.data_ptr(), targets.data_ptr(), rows, vocab, ld, int(ignore_index),
+                            float(temperature), code, 0)
+
+
+def _values(logits, targets, top_k, temperature, ignore_index):
+    code, flat, ld, t = _rows(logits, targets)
+    lead, rows, dev = targets.shape, flat.shape[0], logits.device
+    logp, entropy = torch.empty((2, rows), dtype=torch.float32, device=dev).unbind(0)
+    top_v = top_i = None
+    if top_k:
+        top_v = torch.empty((rows, top_k), dtype=torch.float32, device=dev)
+        top_i = torch.empty((rows, top_k), dtype=torch.int64, device=dev)
+    with torch.cuda.device(dev):
+        microadam_token_logprobs(_struct(code, flat, ld, t, ignore_index, temperature), int(top_k), logp.data_ptr(),
+                                 entropy.data_ptr(), top_v.data_ptr() if top_k else None,
+                                 top_i.data_ptr() if top_k else None, torch.cuda.current_stream().cuda_stream)
+    if top_k:
+        top_v, top_i = top_v.view(*lead, top_k), top_i.view(*lead, top_k)
+    return TokenLogprobs(logp.view(lead), entropy.view(lead), top_v, top_i)
+
+
+def _grad_rows(flat: torch.Tensor, ld: int) -> torch.Tensor:
+    """[rows, vocab] for the gradient, whose rows start at the same place in 16
+    bytes as the logits' rows: at most 15 bytes of a row and of the start are
+    left unused, none where the logits are dense and start aligned."""
+    rows, vocab = flat.shape
+    size = flat.element_size()
+    per = 16 // size
+    start = flat.data_ptr() % 16 // size
+    gld = vocab + (ld - vocab) % per
+    store = torch.empty(start + rows * gld, dtype=flat.dtype, device=flat.device)
+    return store[start:].as_strided((rows, vocab), (gld, 1))
+
+
+def _upstream(g, lead, what):
+    if g.shape != lead:
+        raise ValueError(f"{what}: the targets' shape")
+    return g.reshape(-1).to(torch.float32).contiguous()
+
+
+def token_logprobs_and_grad(logits: torch.Tensor, targets: torch.Tensor, grad_logp: torch.Tensor,
+                            grad_entropy: Optional[torch.Tensor] = None, *, temperature: float = 1.0,
+                            ignore_index: int = -100, out: Optional[torch.Tensor] = None) -> TokenLogprobsGrad:
+    """Log probabilities, entropies and, in the same pass, the gradient with
+    respect to the logits of sum(grad_logp * logp + grad_entropy * entropy).
+    For the mean negative log likelihood of n tokens, grad_logp is -1/n.
+    ``out``: where the gradient goes (``logits`` itself is allowed)."""
+    logits = logits.detach()
+    code, flat, ld, t = _rows(logits, targets)
+    lead, dev = targets.shape, logits.device
+    gp = _upstream(grad_logp, lead, "grad_logp")
+    ge = None if grad_entropy is None else _upstream(grad_entropy, lead, "grad_entropy")
+    for g in (gp, ge):
+        if g is not None and g.device != dev:
+            raise ValueError("grad_logp and grad_entropy: the logits' device")
+    if out is None:
+        grad = _grad_rows(flat, ld)
+        gld, shaped = grad.stride(0), grad if logits.dim() == 2 else grad.view(logits.shape)
+    else:
+        if out.shape != logits.shape or out.dtype != logits.dtype:
+            raise ValueError("out: the logits' shape and dtype")
+        _, grad, gld, _ = _rows(out, targets)
+        shaped = out
+    logp, entropy = torch.empty((2, flat.shape[0]), dtype=torch.float32, device=dev).unbind(0)
+    with torch.cuda.device(dev):
+        microadam_token_logprobs_grad(_struct(code, flat, ld, t, ignore_index, temperature), gp.data_ptr(),
+                                      None if ge is None else ge.data_ptr(), logp.data_ptr(), entropy.data_ptr(),
+                                      grad.data_ptr(), gld, torch.cuda.current_stream().cuda_stream)
+    return TokenLogprobsGrad(logp.view(lead), entropy.view(lead), shaped)
+
+
+class _TokenLogprobs(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, targets, top_k, temperature, ignore_index):
+        r = _values(logits, targets, top_k, temperature, ignore_index)
+        ctx.save_for_backward(logits, targets)
+        ctx.settings = (temperature, ignore_index)
+        if top_k:
+            ctx.mark_non_differentiable(r.top_logprobs, r.top_indices)
+        return tuple(r)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, g_logp, g_entropy, *_):
+        logits, targets = ctx.saved_tensors
+        temperature, ignore_index = ctx.settings
+        return token_logprobs_and_grad(logits, targets, g_logp, g_entropy, temperature=temperature,
+                                       ignore_index=ignore_index).grad, None, None, None, None
+
+
+def token_logprobs(logits: torch.Tensor, targets: torch.Tensor, *, top_k: int = 0, temperature: float = 1.0,
+                   ignore_index: int = -100) -> TokenLogprobs:
+    """Per row of logits: the log probability of its target token, the entropy
+    of the distribution and, with ``top_k`` > 0 (at most 64), the ``top_k`` most
+    probable tokens with their log probabilities, ties to the lowest index.
+    Ignored rows give zeros (alternatives 0 and -1) and no gradient.  The
+    alternatives carry no gradient."""
+    if torch.is_grad_enabled() and logits.requires_grad:
+        return TokenLogprobs(*_TokenLogprobs.apply(logits, targets, top_k, temperature, ignore_index))
+    return _values(logits, targets, top_k, temperature, ignore_index)
