@@ -112,31 +112,6 @@ double update_scale(const Call& c, const microadam_matrix& a) {
   }
 }
 
-// Tile of a launch: the one whose rounds over the 256 CUs take the least
-// time, from the rate a CU reaches with each.
-int choose_tile(const GemmArgs& ga, SchulzPhase phase) {
-  static const struct {
-    int tile, per_cu;
-    double rate;
-  } kForms[3] = {{256, 1, 1.0}, {128, 2, 0.75}, {64, 4, 0.4}};
-  int best = 256;
-  double least = 0.0;
-  for (const auto& f : kForms) {
-    int64_t tiles = 0;
-    for (int i = 0; i < ga.n_groups; ++i) tiles += schulz_tiles(ga.group[i], phase, f.tile);
-    if (tiles >= ((int64_t)1 << 24)) continue;
-    const int64_t slots = 256 * f.per_cu;
-    const int64_t full = tiles / slots, rest = tiles % slots;
-    const double rounds = (double)full * f.per_cu + (double)((rest + 255) / 256);
-    const double time = rounds * f.tile * f.tile / f.rate;
-    if (least == 0.0 || time < least) {
-      least = time;
-      best = f.tile;
-    }
-  }
-  return best;
-}
-
 // Queues the matrices items[0..count) (equal working shapes adjacent).
 int queue_chunk(const Call& c, const Item* items, int32_t count, uint8_t* ws, hipStream_t s) {
   const bool split = use_split(c.cfg, c.out_dtype);
@@ -189,15 +164,16 @@ int queue_chunk(const Call& c, const Item* items, int32_t count, uint8_t* ws, hi
   ga.decay = (float)c.decay;
   ga.out_bf16 = c.out_dtype == MICROADAM_BF16;
   ga.update = c.update ? 1 : 0;
-  const int sym = choose_tile(ga, kGram), full = choose_tile(ga, kApply);
+  const int gram = choose_schulz_tile(ga, kGram), poly = choose_schulz_tile(ga, kPoly),
+            full = choose_schulz_tile(ga, kApply);
   for (int32_t k = 0; k < c.cfg->steps; ++k) {
     const double* co = c.cfg->coefficients ? c.cfg->coefficients + 3 * k : kDefaultCoefficients;
     ga.ca = (float)(co[0] * kScaleA);
     ga.cb = (float)co[1];
     ga.cc = (float)(co[2] / kScaleA);
     ga.buffer = k & 1;
-    if ((e = launch_schulz_gemm(ga, kGram, sym, s)) != hipSuccess ||
-        (e = launch_schulz_gemm(ga, kPoly, sym, s)) != hipSuccess ||
+    if ((e = launch_schulz_gemm(ga, kGram, gram, s)) != hipSuccess ||
+        (e = launch_schulz_gemm(ga, kPoly, poly, s)) != hipSuccess ||
         (e = launch_schulz_gemm(ga, k + 1 < c.cfg->steps ? kApply : kFinal, full, s)) != hipSuccess)
       return report_hip(e, "launching a product");
   }

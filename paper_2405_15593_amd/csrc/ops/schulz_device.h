@@ -18,8 +18,9 @@
 namespace microadam {
 
 constexpr int kMaxGroups = 8;     // working shapes per launch
-constexpr int kMaxMatrices = 64;  // matrices per launch (their addresses are kernel arguments)
+constexpr int kMaxMatrices = 96;  // matrices per launch (their addresses are kernel arguments)
 constexpr int kPad = 64;          // working dimensions are padded to this
+constexpr int64_t kMaxTiles = (int64_t)1 << 24;  // of a product's launch
 constexpr int kNormParts = 256;   // partial sums of a matrix's norm
 
 // Powers of two, so that scaling rounds nothing.  Elements of X are at most
@@ -81,7 +82,8 @@ struct GemmArgs {
   float ca, cb, cc;          // kPoly: factors of I, the stored A and the product
   float decay;               // kFinal: 1 - lr * weight_decay
   int32_t out_bf16, update;  // kFinal: update out in place (out = decay * out - scale * D) or store scale * D
-  int32_t tile_begin[kMaxGroups + 1];  // tiles before each group
+  int32_t tiles[kMaxGroups];           // of each group, and an eighth of them, rounded up
+  int32_t turns[kMaxGroups];
   SchulzGroup group[kMaxGroups];
   OutMatrix mat[kMaxMatrices];         // kFinal
   uint8_t tall[kMaxMatrices];
@@ -89,8 +91,14 @@ struct GemmArgs {
 
 hipError_t launch_schulz_norm(const PackArgs& a, int n_matrices, hipStream_t s);
 hipError_t launch_schulz_pack(const PackArgs& a, int n_matrices, hipStream_t s);
-// tile: 64, 128 or 256
-hipError_t launch_schulz_gemm(GemmArgs& a, SchulzPhase phase, int tile, hipStream_t s);
+
 int64_t schulz_tiles(const SchulzGroup& g, SchulzPhase phase, int tile);
+// The tile (64, 128, 192 or 256) that takes a launch's products least time.
+int choose_schulz_tile(const GemmArgs& a, SchulzPhase phase);
+hipError_t launch_schulz_gemm(GemmArgs& a, SchulzPhase phase, int tile, hipStream_t s);
+hipError_t launch_schulz_gemm_64(const GemmArgs& a, SchulzPhase phase, hipStream_t s);
+hipError_t launch_schulz_gemm_128(const GemmArgs& a, SchulzPhase phase, hipStream_t s);
+hipError_t launch_schulz_gemm_192(const GemmArgs& a, SchulzPhase phase, hipStream_t s);
+hipError_t launch_schulz_gemm_256(const GemmArgs& a, SchulzPhase phase, hipStream_t s);  // not split
 
 }  // namespace microadam

@@ -82,8 +82,8 @@ def test_lists_types_and_workspace():
     least, useful = ma.microadam_matrix_workspace(cfg, good(), 1, F32)
     refused(SIZE, orth, cfg, good(), 1, F32, F32, 256, least - 1)
     # 8 x 16 works as 64 x 64: X, its transpose twice, A and B, two planes each
-    assert least == useful == 64 * 256 * 8 + 5 * 64 * 64 * 2 * 2
-    assert ma.microadam_matrix_workspace(cfg, good(), 1, BF16)[0] == 64 * 256 * 8 + 5 * 64 * 64 * 2
+    assert least == useful == 96 * 256 * 8 + 5 * 64 * 64 * 2 * 2
+    assert ma.microadam_matrix_workspace(cfg, good(), 1, BF16)[0] == 96 * 256 * 8 + 5 * 64 * 64 * 2
     # the second of two is the one that does not fit
     two = matrices((4096, None, 8192, 8, 16, 16, 0, 16), (4096, None, 8192, 600, 900, 900, 0, 900))
     refused(SIZE, orth, cfg, two, 2, F32, F32, 256, least)
