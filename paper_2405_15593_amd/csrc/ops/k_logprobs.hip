@@ -87,11 +87,13 @@ __device__ inline void rebase(Sums& a, float to, float c) {
   a.m = to;
 }
 
-__device__ inline Sums join_wave(Sums a, float c) {
+// The sums of a wave; `lane_s` becomes this lane's part of s.
+__device__ inline Sums join_wave(Sums a, float c, float& lane_s) {
   float m = a.m;
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
   rebase(a, m, c);
+  lane_s = a.s;
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) {
     a.s += __shfl_xor(a.s, d);
@@ -108,10 +110,10 @@ struct Shared {
   float best_v[kMaxWaves];
   int best_i[kMaxWaves];
   float thread_max[kMaxThreads];
+  uint4v own[8];  // a thread's chunks
   float cand_v[kCandidates];
   int cand_i[kCandidates];
   int count;
-  float threshold;
   float rest;
 };
 
@@ -122,21 +124,19 @@ __device__ inline uint32_t ordered(float x) {
 }
 __device__ inline float from_ordered(uint32_t u) { return __uint_as_float((u >> 31) ? u & 0x7fffffffu : ~u); }
 
-// A value that at least k of the n maxima reach and, up to the low 16 bits
-// of its order, the largest such; one wave.
-__device__ inline float kth_of_maxima(const float* maxima, int n, int k) {
+// A value that at least k (at most 64) elements reach: with the threads'
+// maxima taken together lane by lane over the waves, the k-th largest of the
+// 64, down to the low 16 bits of its order.  Every wave finds it for itself.
+__device__ inline float reached_by(const float* maxima, int waves, int k) {
   const int lane = threadIdx.x & 63;
-  uint32_t key[kMaxWaves];
-#pragma unroll
-  for (int i = 0; i < kMaxWaves; ++i) key[i] = i * 64 + lane < n ? ordered(maxima[i * 64 + lane]) : 0u;
+  float m = maxima[lane];
+  for (int w = 1; w < waves; ++w) m = fmaxf(m, maxima[w * 64 + lane]);
+  const uint32_t key = ordered(m);
   uint32_t t = 0;
+#pragma unroll
   for (int bit = 31; bit >= 16; --bit) {
     const uint32_t probe = t | (1u << bit);
-    int reach = 0;
-#pragma unroll
-    for (int i = 0; i < kMaxWaves; ++i)
-      if (i * 64 < n) reach += __popcll(__ballot(key[i] >= probe));
-    if (reach >= k) t = probe;
+    if (__popcll(__ballot(key >= probe)) >= k) t = probe;
   }
   return t <= ordered(minus_inf()) ? minus_inf() : from_ordered(t);
 }
@@ -226,7 +226,8 @@ __global__ __launch_bounds__(kMaxThreads) void row_kernel(const LogprobArgs a) {
   // before the barrier: in place, the gradient's stores come after it
   const float x_target = tid == 0 && known ? C::load1(x, target) : 0.0f;
 
-  t = join_wave(t, a.c);
+  float lane_s, unused;
+  t = join_wave(t, a.c, lane_s);
   if (lane == 0) sh.sums[wave] = t;
   if (k) {
     sh.thread_max[tid] = thread_max;
@@ -235,25 +236,40 @@ __global__ __launch_bounds__(kMaxThreads) void row_kernel(const LogprobArgs a) {
   __syncthreads();
   t = sh.sums[lane < waves ? lane : 0];
   if (lane >= waves) t.s = t.w = 0.0f;
-  t = join_wave(t, a.c);
+  t = join_wave(t, a.c, unused);
 
   // t.s = 0: every logit is -inf (otherwise the largest adds 1); NaN: a NaN
   // or +inf logit.  Where one token has more than half the probability, s - 1
   // is summed apart from it, so that 1 - p and log s of that token are no
-  // differences of rounded numbers: its wave sums its elements again.
+  // differences of rounded numbers.  Only the thread that holds it had it in
+  // its sum: its wave takes that thread's elements again, one a lane.
   const bool empty = t.s == 0.0f;
   float rest = t.s - 1.0f;
   float log_s;
   if (!empty && t.s < 2.0f) {
-    if (sh.sums[wave].m == t.m) {
+    const uint64_t holds = __ballot(thread_max == t.m && lane_s >= 1.0f);  // its 2^0
+    if (holds) {
+      const int owner = __ffsll((unsigned long long)holds) - 1;
       auto other = [&](float v) { return v < t.m ? exp2_fast((v - t.m) * a.c) : 0.0f; };
-      float sum = other(xe);
+      float sum = lane == owner ? other(xe) : lane_s;
       for (int seg = 0; seg < segments; ++seg) {
         if (MULTI) load(seg);
+        if (lane == owner) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
+          for (int i = 0; i < NV; ++i) sh.own[i] = r[i].q;
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        for (int i = lane; i < NV * E; i += 64) {
+          C one;
+          one.q = sh.own[i / E];
+          float v = one.get(0);
 #pragma unroll
-          for (int e = 0; e < E; ++e) sum += other(r[i].get(e));
+          for (int e = 1; e < E; ++e) v = i % E == e ? one.get(e) : v;
+          sum += other(v);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
       }
 #pragma unroll
       for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
@@ -340,14 +356,9 @@ __global__ __launch_bounds__(kMaxThreads) void row_kernel(const LogprobArgs a) {
     }
     return;
   }
-  // At least k elements reach the k-th largest of the threads' maxima, and
-  // the first k are among those that do: few, unless many are equal.
-  if (wave == 0) {
-    const float v = kth_of_maxima(sh.thread_max, nt, k);
-    if (lane == 0) sh.threshold = v;
-  }
-  __syncthreads();
-  const float threshold = sh.threshold;
+  // The first k are among the elements that reach the threshold: few more
+  // than k, unless many are equal.
+  const float threshold = reached_by(sh.thread_max, waves, k);
   auto collect = [&](float v, int i) {
     if (v >= threshold) {
       const int n = atomicAdd(&sh.count, 1);
@@ -364,7 +375,10 @@ __global__ __launch_bounds__(kMaxThreads) void row_kernel(const LogprobArgs a) {
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         const int j = seg * per_segment + i * nt + tid;
-        if (j >= chunks) continue;
+        float m = r[i].get(0);
+#pragma unroll
+        for (int e = 1; e < E; ++e) m = fmaxf(m, r[i].get(e));
+        if (m < threshold) continue;  // also past the last chunk
 #pragma unroll
         for (int e = 0; e < E; ++e) collect(r[i].get(e), head + j * E + e);
       }

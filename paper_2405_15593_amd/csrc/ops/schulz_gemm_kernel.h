@@ -122,10 +122,17 @@ __global__ __launch_bounds__(128 * Form<T>::wq, 2) void gemm_kernel(const GemmAr
   // Workgroups go to the eight XCDs in turn: give each XCD one run of every
   // group's tiles, which share operand rows in its L2.
   const int xcd = (int)blockIdx.x & 7;
-  int turn = (int)blockIdx.x >> 3, gi = 0;
-  while (gi + 1 < a.n_groups && turn >= a.turns[gi]) turn -= a.turns[gi++];
-  const SchulzGroup& g = a.group[gi];
-  const int each = a.tiles[gi] >> 3, more = a.tiles[gi] & 7;
+  // (the first group's fields are fetched along with the number of groups)
+  int turn = (int)blockIdx.x >> 3;
+  SchulzGroup g = a.group[0];
+  int tiles = a.tiles[0];
+  if (a.n_groups > 1 && turn >= a.turns[0]) {
+    int gi = 0;
+    while (gi + 1 < a.n_groups && turn >= a.turns[gi]) turn -= a.turns[gi++];
+    g = a.group[gi];
+    tiles = a.tiles[gi];
+  }
+  const int each = tiles >> 3, more = tiles & 7;
   if (turn >= each + (xcd < more ? 1 : 0)) return;
   int tile = xcd * each + (xcd < more ? xcd : more) + turn;
 
@@ -232,6 +239,31 @@ __global__ __launch_bounds__(128 * Form<T>::wq, 2) void gemm_kernel(const GemmAr
     }
   };
 
+  // Element r of acc[i][j] is D at row (of the wave's tile) i * 16 + lane % 16
+  // and column j * 16 + 4 (lane / 16) + r.
+  const int lrow = lane & 15, lcol = (lane >> 4) * 4;
+
+  // kPoly adds A, which the smaller tiles have registers to fetch before the
+  // product (a memory round trip less at the end)
+  auto load_a = [&](int i, int j, int plane) {
+    const int row = p0 + wp0 + i * 16 + lrow, col = q0 + wq0 + j * 16 + lcol;
+    half4 h = {};
+    if (row < g.mp && col < g.mp)
+      h = *(const half4*)((const half_t*)(rec + g.a) + (plane ? (int64_t)g.mp * g.mp : 0) + (int64_t)row * g.mp + col);
+    return h;
+  };
+  constexpr bool kEarly = PHASE == kPoly && T <= 128;
+  constexpr int kEarlyPlanes = SPLIT ? 2 : 1;
+  half4 early[kEarly ? kEarlyPlanes : 1][kEarly ? kI : 1][kEarly ? kJ : 1];
+  if constexpr (kEarly) {
+#pragma unroll
+    for (int pl = 0; pl < kEarlyPlanes; ++pl)
+#pragma unroll
+      for (int i = 0; i < kI; ++i)
+#pragma unroll
+        for (int j = 0; j < kJ; ++j) early[pl][i][j] = load_a(i, j, pl);
+  }
+
   float4v acc[kI][kJ];
 #pragma unroll
   for (int i = 0; i < kI; ++i)
@@ -317,10 +349,6 @@ __global__ __launch_bounds__(128 * Form<T>::wq, 2) void gemm_kernel(const GemmAr
   for (; s < steps - 1; ++s) stage(s, false, true);
   stage(s, false, false);
 
-  // Element r of acc[i][j] is D at row (of the wave's tile) i * 16 + lane % 16
-  // and column j * 16 + 4 (lane / 16) + r.
-  const int lrow = lane & 15, lcol = (lane >> 4) * 4;
-
   if constexpr (PHASE == kFinal) {
     const OutMatrix& om = a.mat[mat];
     const int out_rows = swap ? g.n : g.m, out_cols = swap ? g.m : g.n;
@@ -377,7 +405,6 @@ __global__ __launch_bounds__(128 * Form<T>::wq, 2) void gemm_kernel(const GemmAr
     // the result at its stored scale, rounded once (and what that left)
     constexpr int kPlanes = SPLIT ? 2 : 1;
     half4 out[kPlanes][kI][kJ];
-    const half_t* am = (const half_t*)(rec + g.a);
 #pragma unroll
     for (int i = 0; i < kI; ++i) {
       const int row = p0 + wp0 + i * 16 + lrow;
@@ -387,10 +414,13 @@ __global__ __launch_bounds__(128 * Form<T>::wq, 2) void gemm_kernel(const GemmAr
           const int col = q0 + wq0 + j * 16 + lcol;
           float v[4];
           if constexpr (PHASE == kPoly) {  // b A + c D + a I
-            half4 h = {}, l = {};
-            if (row < g.mp && col < g.mp) {
-              h = *(const half4*)(am + (int64_t)row * g.mp + col);
-              if (SPLIT) l = *(const half4*)(am + (int64_t)g.mp * g.mp + (int64_t)row * g.mp + col);
+            half4 h, l;
+            if constexpr (kEarly) {
+              h = early[0][i][j];
+              l = early[kEarlyPlanes - 1][i][j];
+            } else {
+              h = load_a(i, j, 0);
+              if (SPLIT) l = load_a(i, j, 1);
             }
 #pragma unroll
             for (int r = 0; r < 4; ++r) {

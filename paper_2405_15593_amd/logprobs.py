@@ -15,6 +15,7 @@ stream.
 """
 from __future__ import annotations
 
+import contextlib
 from typing import NamedTuple, Optional
 
 import torch
@@ -22,6 +23,7 @@ import torch
 from . import (MICROADAM_BF16, MICROADAM_F32, microadam_logits, microadam_token_logprobs,
                microadam_token_logprobs_grad)
 
+_HERE = contextlib.nullcontext()
 _DTYPES = {torch.float32: MICROADAM_F32, torch.bfloat16: MICROADAM_BF16}
 
 
@@ -57,7 +59,14 @@ def _rows(logits: torch.Tensor, targets: torch.Tensor):
     ld = flat.stride(0) if rows > 1 else max(1, vocab)
     if flat.data_ptr() != logits.data_ptr() or (rows > 1 and ld < vocab):
         raise ValueError("logits: rows at one stride, not overlapping")
-    return code, flat, ld, targets.reshape(-1).contiguous()
+    if targets.dim() != 1 or not targets.is_contiguous():
+        targets = targets.reshape(-1).contiguous()
+    return code, flat, ld, targets
+
+
+def _on(device):
+    """The device as the current one; nothing to do where it is."""
+    return _HERE if device.index == torch.cuda.current_device() else torch.cuda.device(device)
 
 
 def _struct(code, flat, ld, targets, ignore_index, temperature):
@@ -69,18 +78,22 @@ def _struct(code, flat, ld, targets, ignore_index, temperature):
 def _values(logits, targets, top_k, temperature, ignore_index):
     code, flat, ld, t = _rows(logits, targets)
     lead, rows, dev = targets.shape, flat.shape[0], logits.device
-    logp, entropy = torch.empty((2, rows), dtype=torch.float32, device=dev).unbind(0)
+    values = torch.empty((2, rows), dtype=torch.float32, device=dev)
+    logp, entropy = values[0], values[1]
     top_v = top_i = None
     if top_k:
         top_v = torch.empty((rows, top_k), dtype=torch.float32, device=dev)
         top_i = torch.empty((rows, top_k), dtype=torch.int64, device=dev)
-    with torch.cuda.device(dev):
+    with _on(dev):
         microadam_token_logprobs(_struct(code, flat, ld, t, ignore_index, temperature), int(top_k), logp.data_ptr(),
                                  entropy.data_ptr(), top_v.data_ptr() if top_k else None,
                                  top_i.data_ptr() if top_k else None, torch.cuda.current_stream().cuda_stream)
     if top_k:
-        top_v, top_i = top_v.view(*lead, top_k), top_i.view(*lead, top_k)
-    return TokenLogprobs(logp.view(lead), entropy.view(lead), top_v, top_i)
+        if len(lead) != 1:
+            top_v, top_i = top_v.view(*lead, top_k), top_i.view(*lead, top_k)
+    if len(lead) != 1:
+        logp, entropy = logp.view(lead), entropy.view(lead)
+    return TokenLogprobs(logp, entropy, top_v, top_i)
 
 
 def _grad_rows(flat: torch.Tensor, ld: int) -> torch.Tensor:
@@ -92,14 +105,18 @@ def _grad_rows(flat: torch.Tensor, ld: int) -> torch.Tensor:
     per = 16 // size
     start = flat.data_ptr() % 16 // size
     gld = vocab + (ld - vocab) % per
+    if not start and gld == vocab:
+        return torch.empty((rows, vocab), dtype=flat.dtype, device=flat.device)
     store = torch.empty(start + rows * gld, dtype=flat.dtype, device=flat.device)
-    return store[start:].as_strided((rows, vocab), (gld, 1))
+    return store.as_strided((rows, vocab), (gld, 1), start)
 
 
 def _upstream(g, lead, what):
     if g.shape != lead:
         raise ValueError(f"{what}: the targets' shape")
-    return g.reshape(-1).to(torch.float32).contiguous()
+    if g.dtype is not torch.float32 or g.dim() != 1 or not g.is_contiguous():
+        g = g.reshape(-1).to(torch.float32).contiguous()
+    return g
 
 
 def token_logprobs_and_grad(logits: torch.Tensor, targets: torch.Tensor, grad_logp: torch.Tensor,
@@ -109,7 +126,8 @@ def token_logprobs_and_grad(logits: torch.Tensor, targets: torch.Tensor, grad_lo
     respect to the logits of sum(grad_logp * logp + grad_entropy * entropy).
     For the mean negative log likelihood of n tokens, grad_logp is -1/n.
     ``out``: where the gradient goes (``logits`` itself is allowed)."""
-    logits = logits.detach()
+    if logits.requires_grad:
+        logits = logits.detach()
     code, flat, ld, t = _rows(logits, targets)
     lead, dev = targets.shape, logits.device
     gp = _upstream(grad_logp, lead, "grad_logp")
@@ -125,12 +143,15 @@ def token_logprobs_and_grad(logits: torch.Tensor, targets: torch.Tensor, grad_lo
             raise ValueError("out: the logits' shape and dtype")
         _, grad, gld, _ = _rows(out, targets)
         shaped = out
-    logp, entropy = torch.empty((2, flat.shape[0]), dtype=torch.float32, device=dev).unbind(0)
-    with torch.cuda.device(dev):
+    values = torch.empty((2, flat.shape[0]), dtype=torch.float32, device=dev)
+    logp, entropy = values[0], values[1]
+    with _on(dev):
         microadam_token_logprobs_grad(_struct(code, flat, ld, t, ignore_index, temperature), gp.data_ptr(),
                                       None if ge is None else ge.data_ptr(), logp.data_ptr(), entropy.data_ptr(),
                                       grad.data_ptr(), gld, torch.cuda.current_stream().cuda_stream)
-    return TokenLogprobsGrad(logp.view(lead), entropy.view(lead), shaped)
+    if len(lead) != 1:
+        logp, entropy = logp.view(lead), entropy.view(lead)
+    return TokenLogprobsGrad(logp, entropy, shaped)
 
 
 class _TokenLogprobs(torch.autograd.Function):
