@@ -10,7 +10,7 @@
 //
 // In split precision an operand is hi + lo / 2048.  The product is taken as
 // three runs over K into the same accumulators: lo hi, hi lo, then, after a
-// factor 1/2048, hi hi.
+// factor 1/2048, hi hi; tiles of 64 take all three at once.
 //
 // The symmetric products compute the tiles on and below the diagonal and
 // store each twice.
@@ -109,7 +109,13 @@ __device__ inline void interleave() {
 template <int T, int PHASE, bool SPLIT>
 __global__ __launch_bounds__(128 * Form<T>::wq, 2) void gemm_kernel(const GemmArgs a) {
   constexpr int kWQ = Form<T>::wq, kWaves = 2 * kWQ;
-  constexpr int kPlaces = Form<T>::places, kAhead = (kPlaces + 1) / 2;
+  // A split stage of the small tile holds both planes of both operands and is
+  // multiplied at once, the cross terms into accumulators of their own: a
+  // third of the stages and two thirds of the loads, which such a tile's time
+  // goes by.  Larger tiles have no registers for that.
+  constexpr bool kFused = SPLIT && T == 64;
+  constexpr int kOps = kFused ? 4 : 2;             // loads per stage: P, Q (, what was left of P, of Q)
+  constexpr int kPlaces = kFused ? 10 : Form<T>::places, kAhead = (kPlaces + kOps - 1) / kOps;
   constexpr int kRowBytes = kStep * 2;             // of an operand's row in a stage
   constexpr int kLoads = T / 8 / kWaves;           // of an operand's stage, eight rows each, per wave
   constexpr int kI = T / 32, kJ = T / (16 * kWQ);  // a wave's 16 x 16 results
@@ -218,12 +224,15 @@ __global__ __launch_bounds__(128 * Form<T>::wq, 2) void gemm_kernel(const GemmAr
   const int load_row = lane >> 3;
   const int voff = load_row * (int)row_bytes + ((lane & 7) ^ spread(load_row)) * 16;
   const int ksteps = ld / kStep;
-  const int steps = SPLIT ? 3 * ksteps : ksteps;
+  const int steps = SPLIT && !kFused ? 3 * ksteps : ksteps;
 
-  // load u of an operand of stage t
-  auto load = [&](bool is_q, int t, int place) {
+  // load op of stage t
+  auto load = [&](int op, int t, int place) {
+    const bool is_q = op & 1;
     const uint8_t* base = is_q ? tq : tp;
-    if (SPLIT) {
+    if (kFused) {
+      if (op >= 2) base += is_q ? plane_q : plane_p;
+    } else if (SPLIT) {
       const int part = t >= 2 * ksteps ? 2 : t >= ksteps ? 1 : 0;
       t -= part * ksteps;
       if (part == (is_q ? 1 : 0)) base += is_q ? plane_q : plane_p;
@@ -272,39 +281,59 @@ __global__ __launch_bounds__(128 * Form<T>::wq, 2) void gemm_kernel(const GemmAr
 #pragma unroll
       for (int r = 0; r < 4; ++r) acc[i][j][r] = 0.0f;
 
-  half8 fp[2][kI], fq[2][kJ];
-  // place: of the stage's P; its Q follows
+  constexpr int kParts = kFused ? 2 : 1;
+  float4v cross[kFused ? kI : 1][kFused ? kJ : 1] = {};
+  half8 fp[2][kParts][kI], fq[2][kParts][kJ];
+  // place: of the stage's P; its other loads follow
+  auto at = [&](int place, int op) { return place + op >= kPlaces ? place + op - kPlaces : place + op; };
   auto read = [&](int place, int kk, int set) {
-    const int place_q = place + 1 == kPlaces ? 0 : place + 1;
     const uint8_t* b = lds + (lane & 15) * kRowBytes + (((kk * 4 + (lane >> 4)) ^ spread(lane & 15)) * 16);
 #pragma unroll
-    for (int j = 0; j < kJ; ++j) fq[set][j] = *(const half8*)(b + place_q * kOperand + (wq0 + j * 16) * kRowBytes);
+    for (int part = 0; part < kParts; ++part) {
 #pragma unroll
-    for (int i = 0; i < kI; ++i) fp[set][i] = *(const half8*)(b + place * kOperand + (wp0 + i * 16) * kRowBytes);
+      for (int j = 0; j < kJ; ++j)
+        fq[set][part][j] = *(const half8*)(b + at(place, 2 * part + 1) * kOperand + (wq0 + j * 16) * kRowBytes);
+#pragma unroll
+      for (int i = 0; i < kI; ++i)
+        fp[set][part][i] = *(const half8*)(b + at(place, 2 * part) * kOperand + (wp0 + i * 16) * kRowBytes);
+    }
   };
   auto multiply = [&](int set) {
 #pragma unroll
     for (int i = 0; i < kI; ++i)
 #pragma unroll
       for (int j = 0; j < kJ; ++j)
-        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fq[set][j], fp[set][i], acc[i][j], 0, 0, 0);
+        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fq[set][0][j], fp[set][0][i], acc[i][j], 0, 0, 0);
+    if constexpr (kFused) {
+#pragma unroll
+      for (int i = 0; i < kI; ++i)
+#pragma unroll
+        for (int j = 0; j < kJ; ++j)
+          cross[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fq[set][1][j], fp[set][0][i], cross[i][j], 0, 0, 0);
+#pragma unroll
+      for (int i = 0; i < kI; ++i)
+#pragma unroll
+        for (int j = 0; j < kJ; ++j)
+          cross[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fq[set][0][j], fp[set][1][i], cross[i][j], 0, 0, 0);
+    }
   };
+  constexpr int kReads = kParts * (kI + kJ), kMfmas = (kFused ? 3 : 1) * kI * kJ;
 
   // The places of stage s are loaded again as soon as every wave has read the
   // last of s into registers; the fragments of each half stage are read half a
   // stage ahead.
 #pragma unroll
   for (int u = 0; u < kPlaces; ++u)
-    if (u / 2 < steps) load(u & 1, u / 2, u);
+    if (u / kOps < steps) load(u % kOps, u / kOps, u);
   if (steps >= kAhead)
-    wait_vmcnt<(kPlaces - 2) * kLoads>();
+    wait_vmcnt<(kPlaces - kOps) * kLoads>();
   else
     wait_vmcnt<0>();
   __builtin_amdgcn_s_barrier();
   read(0, 0, 0);
   int place = 0;  // of stage s of P
   auto stage = [&](int s, bool more, bool next) {
-    if (SPLIT && s == 2 * ksteps) {
+    if (SPLIT && !kFused && s == 2 * ksteps) {
 #pragma unroll
       for (int i = 0; i < kI; ++i)
 #pragma unroll
@@ -314,33 +343,33 @@ __global__ __launch_bounds__(128 * Form<T>::wq, 2) void gemm_kernel(const GemmAr
     for (int kk = 0; kk < kK - 1; ++kk) {
       read(place, kk + 1, (kk + 1) & 1);
       multiply(kk & 1);
-      interleave<kI + kJ, 0, kI * kJ>();
+      interleave<kReads, 0, kMfmas>();
       __builtin_amdgcn_sched_barrier(0);
     }
     if (next) {
       __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): stage s is in registers
       if (more)
-        wait_vmcnt<(kPlaces - 4) * kLoads>();
+        wait_vmcnt<(kPlaces - 2 * kOps) * kLoads>();
       else
         wait_vmcnt<0>();
       __builtin_amdgcn_s_barrier();
       __builtin_amdgcn_sched_barrier(0);
-      const int place_q = place + 1 == kPlaces ? 0 : place + 1;
-      const int after = place + 2 >= kPlaces ? place + 2 - kPlaces : place + 2;
+      const int after = at(place, kOps);
       read(after, 0, 0);
-      // loads 2 s + places and 2 s + places + 1
-      constexpr bool first_q = kPlaces & 1;
-      constexpr int first = kPlaces / 2, second = (kPlaces + 1) / 2;  // stages after s
-      if (more || s + first < steps) load(first_q, s + first, place);
-      if (more) load(!first_q, s + second, place_q);
+      // loads kOps * s + kPlaces and on
+#pragma unroll
+      for (int i = 0; i < kOps; ++i) {
+        const int later = (kPlaces + i) / kOps;  // stages after s
+        if (more || s + later < steps) load((kPlaces + i) % kOps, s + later, at(place, i));
+      }
       place = after;
     }
     multiply((kK - 1) & 1);
     if (next) {
       if (more)
-        interleave<kI + kJ, 2 * kLoads, kI * kJ>();
+        interleave<kReads, kOps * kLoads, kMfmas>();
       else
-        interleave<kI + kJ, 0, kI * kJ>();
+        interleave<kReads, 0, kMfmas>();
     }
     __builtin_amdgcn_sched_barrier(0);
   };
@@ -348,6 +377,12 @@ __global__ __launch_bounds__(128 * Form<T>::wq, 2) void gemm_kernel(const GemmAr
   for (; s < steps - kAhead; ++s) stage(s, true, true);
   for (; s < steps - 1; ++s) stage(s, false, true);
   stage(s, false, false);
+  if constexpr (kFused) {
+#pragma unroll
+    for (int i = 0; i < kI; ++i)
+#pragma unroll
+      for (int j = 0; j < kJ; ++j) acc[i][j] += cross[i][j] * (1.0f / kSplitScale);
+  }
 
   if constexpr (PHASE == kFinal) {
     const OutMatrix& om = a.mat[mat];

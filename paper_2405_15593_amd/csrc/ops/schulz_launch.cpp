@@ -20,11 +20,14 @@ struct TileForm {
   float few_stage, few_rest, full_stage, full_rest;
 };
 constexpr TileForm kTileForms[] = {
-    {256, 1, 1.40f, 4.0f, 1.60f, 14.0f},
+    {256, 1, 1.40f, 4.0f, 1.60f, 13.0f},
     {192, 1, 0.95f, 3.0f, 1.08f, 13.0f},
-    {128, 2, 0.70f, 2.0f, 1.04f, 9.0f},
+    {128, 2, 0.70f, 2.0f, 1.04f, 9.5f},
     {64, 2, 0.38f, 1.5f, 0.45f, 2.3f},
 };
+// the 64-tile in split precision, whose stage holds all three products (the
+// others take three stages)
+constexpr TileForm kSplit64 = {64, 2, 0.62f, 2.0f, 0.90f, 3.0f};
 constexpr int kCus = 256;
 
 // Time until the last workgroup is done when the groups' tiles are handed out
@@ -46,7 +49,7 @@ float makespan(const GemmArgs& a, SchulzPhase phase, const TileForm& f) {
   for (int i = 0; i < a.n_groups; ++i) {
     const SchulzGroup& g = a.group[i];
     const int k = phase == kGram ? g.np : g.mp;
-    const float stages = (float)(k / 64 * (a.split ? 3 : 1));
+    const float stages = (float)(k / 64 * (a.split && f.tile != 64 ? 3 : 1));
     const float each = full ? stages * f.full_stage + f.full_rest : stages * f.few_stage + f.few_rest;
     int64_t left = schulz_tiles(g, phase, f.tile);
     // whole rounds leave the differences between the places as they are
@@ -88,7 +91,7 @@ int choose_schulz_tile(const GemmArgs& a, SchulzPhase phase) {
     int64_t tiles = 0;
     for (int i = 0; i < a.n_groups; ++i) tiles += schulz_tiles(a.group[i], phase, f.tile);
     if (tiles >= kMaxTiles) continue;
-    const float time = makespan(a, phase, f);
+    const float time = makespan(a, phase, a.split && f.tile == 64 ? kSplit64 : f);
     if (!best || time < least) {
       least = time;
       best = f.tile;
