@@ -461,13 +461,17 @@ hipError_t launch_rows(const LogprobArgs& a, hipStream_t s) {
     const int n = ((chunks + nv - 1) / nv + 63) / 64 * 64;
     return n < 64 ? 64 : n;
   };
-  // the fewest chunks per thread that 256 threads cover, then up to 8 in
-  // larger workgroups, then segments
-  if (threads(1) <= 256)
+  // Up to 8 chunks per thread in workgroups of up to 512, which leave a CU room
+  // for a second row (509 x 30522 bf16 with the gradient: 15 us, with 4 chunks
+  // in 1024 threads 18 us); with few rows a row's own time counts, and more
+  // threads shorten it (1 x 32000 bf16: 8.7 us, against 9.3).
+  const bool few = a.rows <= 128;
+  const int most = few ? kMaxThreads : 256;
+  if (threads(1) <= most)
     row_kernel<BF16, 1, GRAD, ENTGRAD, false><<<grid, threads(1), 0, s>>>(a);
-  else if (threads(2) <= 256)
+  else if (threads(2) <= most)
     row_kernel<BF16, 2, GRAD, ENTGRAD, false><<<grid, threads(2), 0, s>>>(a);
-  else if (threads(4) <= 512)
+  else if (threads(4) <= (few ? kMaxThreads : 512))
     row_kernel<BF16, 4, GRAD, ENTGRAD, false><<<grid, threads(4), 0, s>>>(a);
   else if (threads(8) <= kMaxThreads)
     row_kernel<BF16, 8, GRAD, ENTGRAD, false><<<grid, threads(8), 0, s>>>(a);

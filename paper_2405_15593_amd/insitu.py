@@ -1,6 +1,7 @@
 """MicroAdam inside a training loop: a small randomly initialised decoder-only
-transformer on synthetic tokens, trained with ``MicroAdamW`` and, for
-comparison, with torch's dense AdamW.
+transformer on synthetic tokens, trained with ``MicroAdamW``, with ``Muon`` for
+the blocks' matrices beside ``MicroAdamW`` for the other parameters (the loss
+from ``token_logprobs``), and, for comparison, with torch's dense AdamW.
 
 The tokens follow a fixed random first-order Markov chain (seeded), so the
 loss has a floor well below log(V) that a working optimizer approaches.  The
@@ -85,26 +86,37 @@ class MarkovTokens:
 
 def train(opt_name: str, steps: int, vocab=1024, dim=256, layers=4, heads=4, seq=128, batch=32,
           lr=1e-3, seed=0, device="cuda", log_every=10):
+    from .logprobs import token_logprobs
+    from .muon import Muon
     from .optim import MicroAdamW
     torch.manual_seed(seed)
     model = TinyLM(vocab, dim, layers, heads, seq).to(device)
     params = [p for p in model.parameters()]
     n_params = sum(p.numel() for p in params)
     if opt_name == "microadam":
-        opt = MicroAdamW(params, lr=lr)
+        opts = [MicroAdamW(params, lr=lr)]
+    elif opt_name == "muon":
+        matrices = [p for p in model.blocks.parameters() if p.dim() == 2]
+        taken = {id(p) for p in matrices}
+        opts = [Muon(matrices, lr=lr), MicroAdamW([p for p in params if id(p) not in taken], lr=lr)]
     else:
-        opt = torch.optim.AdamW(params, lr=lr, weight_decay=0.0)
+        opts = [torch.optim.AdamW(params, lr=lr, weight_decay=0.0)]
     data = MarkovTokens(vocab, seq, batch, device, seed=seed)
     losses, opt_ms = [], []
     ev = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
     t0 = time.perf_counter()
     for step in range(steps):
         x, y = data.next()
-        loss = F.cross_entropy(model(x).reshape(-1, vocab), y.reshape(-1))
-        opt.zero_grad(set_to_none=True)
+        if opt_name == "muon":
+            loss = -token_logprobs(model(x), y).logp.mean()
+        else:
+            loss = F.cross_entropy(model(x).reshape(-1, vocab), y.reshape(-1))
+        for opt in opts:
+            opt.zero_grad(set_to_none=True)
         loss.backward()
         ev[0].record()
-        opt.step()
+        for opt in opts:
+            opt.step()
         ev[1].record()
         if step % log_every == 0 or step == steps - 1:
             torch.cuda.synchronize()
@@ -112,10 +124,10 @@ def train(opt_name: str, steps: int, vocab=1024, dim=256, layers=4, heads=4, seq
             opt_ms.append(ev[0].elapsed_time(ev[1]))
     torch.cuda.synchronize()
     wall = time.perf_counter() - t0
-    if opt_name == "microadam":
-        state = opt.state_bytes()
+    if opt_name != "adamw":
+        state = sum(opt.state_bytes() for opt in opts)
     else:
-        state = sum(v.numel() * v.element_size() for st in opt.state.values()
+        state = sum(v.numel() * v.element_size() for st in opts[0].state.values()
                     for v in st.values() if torch.is_tensor(v))
     return {"optimizer": opt_name, "params": n_params, "steps": steps, "losses": losses,
             "final_loss": losses[-1][1], "opt_step_ms": sum(opt_ms[1:]) / max(1, len(opt_ms) - 1),
@@ -131,7 +143,7 @@ def main():
     ap.add_argument("--lr", type=float, default=1e-3)
     args = ap.parse_args()
     out = {name: train(name, args.steps, layers=args.layers, dim=args.dim, lr=args.lr)
-           for name in ("microadam", "adamw")}
+           for name in ("microadam", "muon", "adamw")}
     print(json.dumps(out))
 
 

@@ -87,7 +87,7 @@ def _values(logits, targets, top_k, temperature, ignore_index):
     with _on(dev):
         microadam_token_logprobs(_struct(code, flat, ld, t, ignore_index, temperature), int(top_k), logp.data_ptr(),
                                  entropy.data_ptr(), top_v.data_ptr() if top_k else None,
-                                 top_i.data_ptr() if top_k else None, torch.cuda.current_stream().cuda_stream)
+                                 top_i.data_ptr() if top_k else None, torch.cuda.current_stream(dev.index).cuda_stream)
     if top_k:
         if len(lead) != 1:
             top_v, top_i = top_v.view(*lead, top_k), top_i.view(*lead, top_k)
@@ -148,7 +148,7 @@ def token_logprobs_and_grad(logits: torch.Tensor, targets: torch.Tensor, grad_lo
     with _on(dev):
         microadam_token_logprobs_grad(_struct(code, flat, ld, t, ignore_index, temperature), gp.data_ptr(),
                                       None if ge is None else ge.data_ptr(), logp.data_ptr(), entropy.data_ptr(),
-                                      grad.data_ptr(), gld, torch.cuda.current_stream().cuda_stream)
+                                      grad.data_ptr(), gld, torch.cuda.current_stream(dev.index).cuda_stream)
     if len(lead) != 1:
         logp, entropy = logp.view(lead), entropy.view(lead)
     return TokenLogprobsGrad(logp, entropy, shaped)

@@ -14,7 +14,7 @@ unless it is given one.
 """
 from __future__ import annotations
 
-import ctypes
+import contextlib
 
 import torch
 
@@ -27,6 +27,14 @@ _DTYPES = {torch.float32: MICROADAM_F32, torch.bfloat16: MICROADAM_BF16}
 _PRECISIONS = {"auto": MICROADAM_PRECISION_AUTO, "f16": MICROADAM_PRECISION_F16, "split": MICROADAM_PRECISION_SPLIT}
 _SCALES = {"match_rms": MICROADAM_SCALE_MATCH_RMS, "spectral": MICROADAM_SCALE_SPECTRAL,
            "none": MICROADAM_SCALE_NONE}
+
+
+_HERE = contextlib.nullcontext()
+
+
+def _on(device):
+    """The device as the current one; nothing to do where it is."""
+    return _HERE if device.index == torch.cuda.current_device() else torch.cuda.device(device)
 
 
 def _code(t: torch.Tensor, what: str) -> int:
@@ -105,10 +113,10 @@ def orthogonalize(grad: torch.Tensor, *, steps: int = 5, coefficients=None, eps:
         return out
     r, c = grad.shape[-2:]
     array = (microadam_matrix * len(g))(*[(gp, None, op, r, c, gl, 0, ol) for (gp, gl), (op, ol) in zip(g, o)])
-    with torch.cuda.device(grad.device):
+    with _on(grad.device):
         ptr, size, keep = _workspace(cfg, array, len(g), ocode, grad.device, workspace)
         microadam_orthogonalize(cfg, array, len(g), gcode, ocode, ptr, size,
-                                torch.cuda.current_stream().cuda_stream)
+                                torch.cuda.current_stream(grad.device.index).cuda_stream)
     return out
 
 
@@ -145,9 +153,9 @@ def muon_step(params, grads, momenta, *, lr: float, momentum: float = 0.95, nest
                                                 _matrices(v, "momenta")):
             rows.append((gp, vp, pp, r, c, gl, vl, pl))
     array = (microadam_matrix * len(rows))(*rows)
-    with torch.cuda.device(device):
+    with _on(device):
         ptr, size, keep = _workspace(cfg.schulz, array, len(rows), codes[2], device, workspace)
-        microadam_muon_step(cfg, array, len(rows), *codes, lr, ptr, size, torch.cuda.current_stream().cuda_stream)
+        microadam_muon_step(cfg, array, len(rows), *codes, lr, ptr, size, torch.cuda.current_stream(device.index).cuda_stream)
 
 
 class Muon(torch.optim.Optimizer):
