@@ -1,11 +1,11 @@
 // The two passes before the Newton-Schulz products: the Frobenius norm of
 // each matrix's update, then the update itself, normalised, as the binary16
-// iterate X and its transpose.
+// iterate, transposed.
 //
 //   V' = mu V + (1 - mu) G;  U = mu V' + (1 - mu) G (Nesterov) or V';
 //   without momentum U = G.      X = S_X U / (||U||_F + eps)
 //
-// Both passes are bound by memory: they read G and V twice and write V', X
+// Both passes are bound by memory: they read G and V twice and write V'
 // and X^T once.  U is not kept between them (it would have to be written and
 // read again), and the squares are summed in binary64, so neither tiny nor
 // huge gradients leave the range.  Every sum has a fixed order.
@@ -158,9 +158,8 @@ __global__ __launch_bounds__(256) void pack_kernel(const PackArgs a) {
   const PackMatrix& pm = a.mat[mat];
   const bool momentum = pm.momentum != nullptr;
   uint8_t* rec = a.ws + g.base + (uint64_t)(mat - g.first) * g.record;
-  // the copy in the caller's orientation, and the transposed one
-  half_t* same = (half_t*)(rec + (tall ? g.xt : g.x));
-  half_t* flip = (half_t*)(rec + (tall ? g.x : g.xt));
+  // a tall matrix lies as X^T does; another is turned in LDS
+  half_t* xt = (half_t*)(rec + g.xt);
   const int64_t plane = (int64_t)g.mp * g.np;
 
 #pragma unroll
@@ -184,11 +183,15 @@ __global__ __launch_bounds__(256) void pack_kernel(const PackArgs a) {
         lo[i] = (half_t)((x - (float)hi[i]) * kSplitScale);
       }
     }
-    *(half8*)(same + (int64_t)row * cols_p + col) = hi;
-    if (a.split) *(half8*)(same + plane + (int64_t)row * cols_p + col) = lo;
-    *(half8*)&stage[0][r * kLdsRow + c] = hi;
-    if (a.split) *(half8*)&stage[1][r * kLdsRow + c] = lo;
+    if (tall) {
+      *(half8*)(xt + (int64_t)row * g.mp + col) = hi;
+      if (a.split) *(half8*)(xt + plane + (int64_t)row * g.mp + col) = lo;
+    } else {
+      *(half8*)&stage[0][r * kLdsRow + c] = hi;
+      if (a.split) *(half8*)&stage[1][r * kLdsRow + c] = lo;
+    }
   }
+  if (tall) return;
   __syncthreads();
   for (int p = 0; p <= (a.split ? 1 : 0); ++p) {
 #pragma unroll
@@ -197,7 +200,7 @@ __global__ __launch_bounds__(256) void pack_kernel(const PackArgs a) {
       half8 v;
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] = stage[p][(r + i) * kLdsRow + c];
-      *(half8*)(flip + p * plane + (int64_t)(c0 + c) * rows_p + r0 + r) = v;
+      *(half8*)(xt + p * plane + (int64_t)(c0 + c) * g.mp + r0 + r) = v;
     }
   }
 }

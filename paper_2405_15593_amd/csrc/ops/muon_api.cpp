@@ -81,11 +81,10 @@ SchulzGroup group_of(int32_t m, int32_t n, bool split) {
   g.np = (int32_t)up(n, kPad);
   const uint64_t xb = (uint64_t)g.mp * g.np * 2 * (split ? 2 : 1);
   const uint64_t ab = (uint64_t)g.mp * g.mp * 2 * (split ? 2 : 1);
-  g.x = 0;  // every size is a multiple of 8192 bytes
-  g.xt = xb;
-  g.a = 3 * xb;
-  g.b = 3 * xb + ab;
-  g.record = 3 * xb + 2 * ab;
+  g.xt = 0;  // every size is a multiple of 8192 bytes
+  g.a = 2 * xb;
+  g.b = 2 * xb + ab;
+  g.record = 2 * xb + 2 * ab;
   return g;
 }
 

@@ -4,8 +4,7 @@
 // group have one working shape m x n with m <= n (a matrix with more rows
 // than columns is worked on as its transpose), padded with zeros to multiples
 // of kPad, and one record each in the workspace:
-//   X   [mp][np]   the iterate
-//   XT  [np][mp]   its transpose, in two buffers that the steps alternate
+//   XT  [np][mp]   the iterate X transposed, in two buffers that the steps alternate
 //   A   [mp][mp]   S_A X X^T
 //   B   [mp][mp]   S_A (a I + b A + c A^2)
 // All are binary16, X scaled by S_X; in split precision each is followed by a
@@ -34,7 +33,7 @@ constexpr float kSplitScale = 2048.0f;
 struct SchulzGroup {
   uint64_t base;        // of the group's first record, bytes from the workspace
   uint64_t record;      // bytes of a record
-  uint64_t x, xt, a, b; // offsets in a record (xt: of the first of its two buffers)
+  uint64_t xt, a, b;    // offsets in a record (xt: of the first of its two buffers)
   int32_t m, n;         // working shape, m <= n
   int32_t mp, np;       // padded
   int32_t first, count; // matrices of the launch
@@ -66,12 +65,11 @@ struct PackArgs {
   uint8_t of[kMaxMatrices];  // matrix -> group
 };
 
-// Products of a step, all of the form D = P Q^T with the operands' rows
-// contiguous along the summed dimension.
+// Products of a step.
 enum SchulzPhase {
   kGram = 0,   // A = X X^T (symmetric)
   kPoly = 1,   // B = a I + b A + c A A^T (symmetric)
-  kApply = 2,  // X <- B X, and its transpose into the other buffer
+  kApply = 2,  // X^T <- X^T B, into the other buffer
   kFinal = 3   // the caller's matrix from B X
 };
 

@@ -1,12 +1,15 @@
-// The products of a Newton-Schulz step on the matrix cores: D = P Q^T with
-// binary16 operands whose rows are contiguous along the summed dimension, and
-// binary32 accumulators.
+// The products of a Newton-Schulz step on the matrix cores, with binary16
+// operands and binary32 accumulators: D = P Q^T with the operands' rows
+// contiguous along the summed dimension, and X X^T = P^T Q from X^T, whose rows
+// run along it.  So only X^T is kept, and one product writes it once.
 //
 // A workgroup computes a T x T tile of D.  K is taken in stages of 64 elements
 // that go straight from memory to LDS, one to three stages ahead of the matrix
-// instructions (16x16x32).  Rows are kept with their
-// 16-byte chunks permuted, so that sixteen rows' chunks, which a 16-byte read
-// takes in one cycle, lie on different banks (64 of 4 bytes).
+// instructions (16x16x32).  Rows are kept with their 16-byte chunks permuted, so
+// that sixteen rows' chunks, which a 16-byte read takes in one cycle, lie on
+// different banks (64 of 4 bytes).  Stages of X^T are kept as they lie, 64 rows
+// of T elements, with their 32-byte segments permuted likewise, and read with
+// the transposing LDS read (four rows of 16 elements to sixteen lanes of four).
 //
 // In split precision an operand is hi + lo / 2048.  The product is taken as
 // three runs over K into the same accumulators: lo hi, hi lo, then, after a
@@ -26,7 +29,9 @@ typedef half_t half8 __attribute__((ext_vector_type(8)));
 typedef float float4v __attribute__((ext_vector_type(4)));
 typedef float float16v __attribute__((ext_vector_type(16)));
 typedef uint32_t uint2v __attribute__((ext_vector_type(2)));
+typedef short short4v __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) void* lds_ptr;
+typedef __attribute__((address_space(3))) short4v* lds_short4;
 
 __device__ inline float bf16_to_f32(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
 
@@ -70,6 +75,14 @@ __device__ inline int triangle_row(int t) {
   while (r * (r + 1) / 2 > t) --r;
   while ((r + 1) * (r + 2) / 2 <= t) ++r;
   return r;
+}
+
+// The transposing LDS read: of sixteen lanes, lanes 4 r to 4 r + 3 address row
+// r's four times four elements, and lane i receives element i of four rows.
+// (`restrict`: without alias information the compiler waits for all loads to
+// LDS before it; the loop below waits for those of its stage.)
+__device__ inline short4v read_tr16(const uint8_t* __restrict__ p) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4)p);
 }
 
 template <int N>
@@ -148,7 +161,8 @@ __global__ __launch_bounds__(128 * Form<T>::wq, 2) void gemm_kernel(const GemmAr
   const int which = uniform(tile / per);
   tile -= which * per;
   const int mat = g.first + which;
-  const bool swap = PHASE == kFinal && uniform(a.tall[mat]);
+  // X^T's rows are D's rows: always to keep X^T, at the end for a tall matrix
+  const bool swap = PHASE == kApply || (PHASE == kFinal && uniform(a.tall[mat]));
 
   // Tile (ti, tj) of D: strips of kStrip tile rows, column by column, so that
   // the 32 tiles an XCD's CUs take at a time need about 8 + 4 operand tiles.
@@ -182,23 +196,20 @@ __global__ __launch_bounds__(128 * Form<T>::wq, 2) void gemm_kernel(const GemmAr
   const uint8_t* xt = rec + g.xt + (a.buffer ? xt_bytes : 0);
   const uint8_t *p, *q;
   uint64_t plane_p, plane_q;
-  int ld, rows_p, rows_q;  // ld: halves per row, also the summed length
+  int rows_p, rows_q;
   if (PHASE == kGram) {
-    p = q = rec + g.x;
+    p = q = xt;
     plane_p = plane_q = plane_x;
-    ld = g.np;
     rows_p = rows_q = g.mp;
   } else if (PHASE == kPoly) {
     p = q = rec + g.a;
     plane_p = plane_q = plane_a;
-    ld = g.mp;
     rows_p = rows_q = g.mp;
   } else {
     p = swap ? xt : rec + g.b;
     q = swap ? rec + g.b : xt;
     plane_p = swap ? plane_x : plane_a;
     plane_q = swap ? plane_a : plane_x;
-    ld = g.mp;
     rows_p = swap ? g.np : g.mp;
     rows_q = swap ? g.mp : g.np;
   }
@@ -214,16 +225,32 @@ __global__ __launch_bounds__(128 * Form<T>::wq, 2) void gemm_kernel(const GemmAr
   const int wave = uniform((int)threadIdx.x >> 6);
   const int wp0 = (wave & 1) * (T / 2), wq0 = (wave >> 1) * (T / kWQ);
 
-  // rows past the operand read as zeros (the resource's size)
-  const uint32_t row_bytes = (uint32_t)ld * 2;
-  const uint8_t* tp = p + (uint64_t)p0 * row_bytes;
-  const uint8_t* tq = q + (uint64_t)q0 * row_bytes;
-  const int size_p = (int)((uint32_t)left_p * row_bytes), size_q = (int)((uint32_t)left_q * row_bytes);
+  // What lies past the operand reads as zeros (the resource's size).  kGram: a
+  // stage's 64 rows of X^T from column p0 (q0) on; columns past the matrix read
+  // the next row's, whose results are not stored.
+  const uint32_t row_bytes = (uint32_t)g.mp * 2;
+  const uint8_t* tp = p + (PHASE == kGram ? (uint64_t)p0 * 2 : (uint64_t)p0 * row_bytes);
+  const uint8_t* tq = q + (PHASE == kGram ? (uint64_t)q0 * 2 : (uint64_t)q0 * row_bytes);
+  const int size_p = (int)(PHASE == kGram ? kStep * row_bytes - (uint32_t)p0 * 2 : (uint32_t)left_p * row_bytes);
+  const int size_q = (int)(PHASE == kGram ? kStep * row_bytes - (uint32_t)q0 * 2 : (uint32_t)left_q * row_bytes);
   // the 16-byte chunk c of row r is kept at position c ^ spread(r)
   auto spread = [](int r) { return (r >> 1) & 7; };
   const int load_row = lane >> 3;
   const int voff = load_row * (int)row_bytes + ((lane & 7) ^ spread(load_row)) * 16;
-  const int ksteps = ld / kStep;
+  const int ksteps = (PHASE == kGram ? g.np : g.mp) / kStep;
+  // kGram: the 32-byte segment s of row r is kept at position s ^ turn, by the
+  // bits of r that the rows of one read differ in
+  constexpr bool kWide = T % 128 == 0;  // whole 256-byte rows: all of a read's eight rows on the same banks
+  auto turn_of = [](int r) { return kWide ? (r & 3) | ((r >> 3 & 1) << 2) : (r >> 1 & 1) | ((r >> 3 & 1) << 1); };
+  int voff_gram[PHASE == kGram ? kLoads : 1];
+  if constexpr (PHASE == kGram) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int at = (wave * kLoads + i) * 1024 + lane * 16;
+      const int r = at / (2 * T), in = at % (2 * T);
+      voff_gram[i] = r * (int)row_bytes + (((in >> 5) ^ turn_of(r)) << 5) + (in & 31);
+    }
+  }
   const int steps = SPLIT && !kFused ? 3 * ksteps : ksteps;
 
   // load op of stage t
@@ -237,14 +264,16 @@ __global__ __launch_bounds__(128 * Form<T>::wq, 2) void gemm_kernel(const GemmAr
       t -= part * ksteps;
       if (part == (is_q ? 1 : 0)) base += is_q ? plane_q : plane_p;
     }
+    if (PHASE == kGram) base += (uint64_t)((uint32_t)t * kStep) * row_bytes;
     auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, is_q ? size_q : size_p, 0x00020000);
     uint8_t* dst = lds + place * kOperand;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const int c = wave * kLoads + i;
-      const int soff = c * 8 * (int)row_bytes + t * kRowBytes;
       // the second eight of sixteen rows have bit 2 of their chunks' places flipped
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_ptr)(dst + c * 1024), 16, c & 1 ? voff ^ 64 : voff, soff, 0, 0);
+      const int v = PHASE == kGram ? voff_gram[PHASE == kGram ? i : 0] : c & 1 ? voff ^ 64 : voff;
+      const int soff = PHASE == kGram ? 0 : c * 8 * (int)row_bytes + t * kRowBytes;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_ptr)(dst + c * 1024), 16, v, soff, 0, 0);
     }
   };
 
@@ -286,16 +315,27 @@ __global__ __launch_bounds__(128 * Form<T>::wq, 2) void gemm_kernel(const GemmAr
   half8 fp[2][kParts][kI], fq[2][kParts][kJ];
   // place: of the stage's P; its other loads follow
   auto at = [&](int place, int op) { return place + op >= kPlaces ? place + op - kPlaces : place + op; };
+  // kGram: fragment i of an operand is its segment i of 16 columns; lane l
+  // takes part in rows 8 (l / 16) + (l % 16) / 4 and four on
+  auto read_turned = [&](const uint8_t* operand, int segment, int kk) {
+    const int r = (lane >> 4) * 8 + ((lane & 15) >> 2);
+    const uint8_t* b = operand + r * (2 * T) + ((segment ^ turn_of(r)) << 5) + (lane & 3) * 8 + kk * 32 * (2 * T);
+    const short4v lo = read_tr16(b), hi = read_tr16(b + 4 * (2 * T));
+    return __builtin_bit_cast(half8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  };
   auto read = [&](int place, int kk, int set) {
     const uint8_t* b = lds + (lane & 15) * kRowBytes + (((kk * 4 + (lane >> 4)) ^ spread(lane & 15)) * 16);
 #pragma unroll
     for (int part = 0; part < kParts; ++part) {
+      const int op = at(place, 2 * part) * kOperand, oq = at(place, 2 * part + 1) * kOperand;
 #pragma unroll
       for (int j = 0; j < kJ; ++j)
-        fq[set][part][j] = *(const half8*)(b + at(place, 2 * part + 1) * kOperand + (wq0 + j * 16) * kRowBytes);
+        fq[set][part][j] = PHASE == kGram ? read_turned(lds + oq, wq0 / 16 + j, kk)
+                                          : *(const half8*)(b + oq + (wq0 + j * 16) * kRowBytes);
 #pragma unroll
       for (int i = 0; i < kI; ++i)
-        fp[set][part][i] = *(const half8*)(b + at(place, 2 * part) * kOperand + (wp0 + i * 16) * kRowBytes);
+        fp[set][part][i] = PHASE == kGram ? read_turned(lds + op, wp0 / 16 + i, kk)
+                                          : *(const half8*)(b + op + (wp0 + i * 16) * kRowBytes);
     }
   };
   auto multiply = [&](int set) {
@@ -317,7 +357,7 @@ __global__ __launch_bounds__(128 * Form<T>::wq, 2) void gemm_kernel(const GemmAr
           cross[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fq[set][0][j], fp[set][1][i], cross[i][j], 0, 0, 0);
     }
   };
-  constexpr int kReads = kParts * (kI + kJ), kMfmas = (kFused ? 3 : 1) * kI * kJ;
+  constexpr int kReads = kParts * (kI + kJ) * (PHASE == kGram ? 2 : 1), kMfmas = (kFused ? 3 : 1) * kI * kJ;
 
   // The places of stage s are loaded again as soon as every wave has read the
   // last of s into registers; the fragments of each half stage are read half a
@@ -475,10 +515,10 @@ __global__ __launch_bounds__(128 * Form<T>::wq, 2) void gemm_kernel(const GemmAr
           }
         }
     }
-    // D at (p0, q0) of an array with rows of `width`, or its transpose at
+    // D at (p0, q0) of an array of `height` rows, or its transpose at
     // (q0, p0), staged in LDS so that rows are stored whole
     half_t* const stage = (half_t*)lds;
-    auto store = [&](uint8_t* dst, int width, int height, bool flip, int plane) {
+    auto store = [&](uint8_t* dst, int height, bool flip, int plane) {
       __syncthreads();
 #pragma unroll
       for (int i = 0; i < kI; ++i)
@@ -496,22 +536,21 @@ __global__ __launch_bounds__(128 * Form<T>::wq, 2) void gemm_kernel(const GemmAr
           }
       __syncthreads();
       const int r0 = flip ? q0 : p0, c0 = flip ? p0 : q0;
-      half_t* d = (half_t*)dst + (int64_t)r0 * width + c0;
+      half_t* d = (half_t*)dst + (int64_t)r0 * g.mp + c0;
       for (int c = threadIdx.x; c < T * (T / 8); c += 64 * kWaves) {
         const int row = c / (T / 8), col = (c % (T / 8)) * 8;
-        if (r0 + row < height && c0 + col < width)
-          *(half8*)(d + (int64_t)row * width + col) = *(const half8*)(stage + row * kStageRow + col);
+        if (r0 + row < height && c0 + col < g.mp)
+          *(half8*)(d + (int64_t)row * g.mp + col) = *(const half8*)(stage + row * kStageRow + col);
       }
     };
 #pragma unroll
     for (int pl = 0; pl < kPlanes; ++pl) {
       if constexpr (kSym) {
         uint8_t* dst = rec + (PHASE == kGram ? g.a : g.b) + (pl ? plane_a : 0);
-        store(dst, g.mp, g.mp, false, pl);
-        if (ti != tj) store(dst, g.mp, g.mp, true, pl);
+        store(dst, g.mp, false, pl);
+        if (ti != tj) store(dst, g.mp, true, pl);
       } else {
-        store(rec + g.x + (pl ? plane_x : 0), g.np, g.mp, false, pl);
-        store(rec + g.xt + (a.buffer ? 0 : xt_bytes) + (pl ? plane_x : 0), g.mp, g.np, true, pl);
+        store(rec + g.xt + (a.buffer ? 0 : xt_bytes) + (pl ? plane_x : 0), g.np, false, pl);
       }
     }
   }

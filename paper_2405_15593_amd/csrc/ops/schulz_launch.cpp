@@ -12,22 +12,23 @@ namespace {
 
 // What a workgroup of each tile takes for a stage of 64 elements of K and for
 // the rest of its work (microseconds), with few others on the device and with
-// every CU holding per_cu of them.  Measured on products of 1024^2, 4096^2,
-// 4096 x 11008 and on 64 matrices of 768 x 768 and 768 x 3072, where the rest,
-// mostly the stores of all CUs at once, is half the time of a 256-tile.
+// every CU holding per_cu of them; the rest of a symmetric product, which
+// stores off-diagonal tiles twice, apart.  Measured on products of 1024^2,
+// 4096^2, 4096 x 11008 and on 72 matrices of 768 x 768 and 768 x 3072, where
+// the rest, mostly the stores of all CUs at once, is 40% of a 256-tile's time.
 struct TileForm {
   int tile, per_cu;
-  float few_stage, few_rest, full_stage, full_rest;
+  float few_stage, few_rest, full_stage, full_rest, full_rest_symmetric;
 };
 constexpr TileForm kTileForms[] = {
-    {256, 1, 1.40f, 4.0f, 1.60f, 13.0f},
-    {192, 1, 0.95f, 3.0f, 1.08f, 13.0f},
-    {128, 2, 0.70f, 2.0f, 1.04f, 9.5f},
-    {64, 2, 0.38f, 1.5f, 0.45f, 2.3f},
+    {256, 1, 1.40f, 4.0f, 1.60f, 10.0f, 15.0f},
+    {192, 1, 0.95f, 3.0f, 1.08f, 7.0f, 11.0f},
+    {128, 2, 0.70f, 2.0f, 1.04f, 4.0f, 8.0f},
+    {64, 2, 0.38f, 1.5f, 0.45f, 1.2f, 2.1f},
 };
 // the 64-tile in split precision, whose stage holds all three products (the
 // others take three stages)
-constexpr TileForm kSplit64 = {64, 2, 0.62f, 2.0f, 0.90f, 3.0f};
+constexpr TileForm kSplit64 = {64, 2, 0.62f, 2.0f, 0.90f, 2.0f, 3.0f};
 constexpr int kCus = 256;
 
 // Time until the last workgroup is done when the groups' tiles are handed out
@@ -38,6 +39,7 @@ float makespan(const GemmArgs& a, SchulzPhase phase, const TileForm& f) {
   // (up to one workgroup a CU, those of two a CU run alone)
   const bool full = all > (f.per_cu > 1 ? kCus : 3 * kCus / 4);
   const int64_t places = (int64_t)kCus * (full ? f.per_cu : 1);
+  const float rest = phase == kGram || phase == kPoly ? f.full_rest_symmetric : f.full_rest;
   // places that become free at the same time, earliest first
   struct Level {
     float at;
@@ -50,7 +52,7 @@ float makespan(const GemmArgs& a, SchulzPhase phase, const TileForm& f) {
     const SchulzGroup& g = a.group[i];
     const int k = phase == kGram ? g.np : g.mp;
     const float stages = (float)(k / 64 * (a.split && f.tile != 64 ? 3 : 1));
-    const float each = full ? stages * f.full_stage + f.full_rest : stages * f.few_stage + f.few_rest;
+    const float each = full ? stages * f.full_stage + rest : stages * f.few_stage + f.few_rest;
     int64_t left = schulz_tiles(g, phase, f.tile);
     // whole rounds leave the differences between the places as they are
     const int64_t rounds = left / places;
