@@ -158,6 +158,7 @@ class _TokenLogprobs(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, targets, top_k, temperature, ignore_index):
         r = _values(logits, targets, top_k, temperature, ignore_index)
+        ctx.set_materialize_grads(False)
         ctx.save_for_backward(logits, targets)
         ctx.settings = (temperature, ignore_index)
         if top_k:
@@ -169,6 +170,10 @@ class _TokenLogprobs(torch.autograd.Function):
     def backward(ctx, g_logp, g_entropy, *_):
         logits, targets = ctx.saved_tensors
         temperature, ignore_index = ctx.settings
+        if g_logp is None and g_entropy is None:
+            return None, None, None, None, None
+        if g_logp is None:
+            g_logp = torch.zeros_like(g_entropy)
         return token_logprobs_and_grad(logits, targets, g_logp, g_entropy, temperature=temperature,
                                        ignore_index=ignore_index).grad, None, None, None, None
 

@@ -50,14 +50,21 @@ def _schulz(steps, coefficients, eps, precision):
     return make_schulz_config(steps, coefficients, eps, _PRECISIONS[precision])
 
 
-def _matrices(t: torch.Tensor, what: str) -> list:
-    """(address, row stride) of each matrix of `t`."""
+def _matrices(t: torch.Tensor, what: str, written: bool = True) -> list:
+    """(address, row stride) of each matrix of `t`; what is written must not
+    overlap itself."""
     if t.dim() < 2:
         raise ValueError(f"{what}: a matrix or a stack of matrices, not {t.dim()} dimensions")
     r, c = t.shape[-2:]
     if (c > 1 and t.stride(-1) != 1) or (r > 1 and t.stride(-2) < c):
         raise ValueError(f"{what}: rows must be contiguous and not overlap")
     ld = t.stride(-2) if r > 1 else c
+    if written and t.dim() > 2:
+        reach = (r - 1) * ld + c
+        for stride, n in sorted((s, n) for s, n in zip(t.stride()[:-2], t.shape[:-2]) if n > 1):
+            if stride < reach:
+                raise ValueError(f"{what}: matrices of a stack must not overlap")
+            reach += (n - 1) * stride
     base, size = t.data_ptr(), t.element_size()
     if t.dim() == 2:
         return [(base, ld)]
@@ -108,7 +115,7 @@ def orthogonalize(grad: torch.Tensor, *, steps: int = 5, coefficients=None, eps:
     elif out.shape != grad.shape or out.device != grad.device:
         raise ValueError("out: grad's shape and device")
     ocode = _code(out, "out")
-    g, o = _matrices(grad, "grad"), _matrices(out, "out")
+    g, o = _matrices(grad, "grad", written=False), _matrices(out, "out")
     if grad.numel() == 0:
         return out
     r, c = grad.shape[-2:]
@@ -149,7 +156,7 @@ def muon_step(params, grads, momenta, *, lr: float, momentum: float = 0.95, nest
         if p.numel() == 0:
             raise ValueError("an empty matrix")
         r, c = p.shape[-2:]
-        for (pp, pl), (gp, gl), (vp, vl) in zip(_matrices(p, "params"), _matrices(g, "grads"),
+        for (pp, pl), (gp, gl), (vp, vl) in zip(_matrices(p, "params"), _matrices(g, "grads", written=False),
                                                 _matrices(v, "momenta")):
             rows.append((gp, vp, pp, r, c, gl, vl, pl))
     array = (microadam_matrix * len(rows))(*rows)

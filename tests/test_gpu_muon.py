@@ -105,6 +105,8 @@ def test_strides_and_in_place():
             orthogonalize(view, out=out)
             assert off(out, schulz64(view)) < tol
             assert bool((big[:, :2] == 7).all()) and bool((big[:, 2 + view.shape[1]:] == 7).all())
+        one = gradient(20, 30, dtype)
+        assert torch.equal(*orthogonalize(one.expand(2, 20, 30)))      # read twice: fine
         four = torch.stack([gradient(20, 30, dtype, i) for i in range(6)]).view(2, 3, 20, 30)
         want = schulz64(four[1, 2].clone())
         assert orthogonalize(four, out=four) is four
@@ -262,6 +264,8 @@ def test_refusals_with_tensors():
         orthogonalize(g, workspace=torch.empty(4096, dtype=torch.uint8, device="cuda"))
     assert e.value.code == ma.MICROADAM_ERR_STATE_SIZE
     v = torch.zeros_like(g)
+    with pytest.raises(ValueError):
+        orthogonalize(torch.stack([g, g]), out=g.clone().expand(2, 8, 8))
     with pytest.raises(ValueError):
         muon_step([g], [g], [v, v], lr=0.1)
     with pytest.raises(ValueError):
