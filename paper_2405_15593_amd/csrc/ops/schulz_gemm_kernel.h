@@ -17,6 +17,12 @@
 //
 // The symmetric products compute the tiles on and below the diagonal and
 // store each twice.
+//
+// Large products are bound by the power limit: X^T B of 4096 x 11008 takes 285
+// to 305 us in 256-tiles (1.2 to 1.3 PFLOP/s; the library's 8192^3 in binary16:
+// 1.33), the matrix cores busy for 65% of 1.6 to 1.8 GHz.  With K = 768 the
+// stores of all CUs at once are 40% of a 256-tile's time (0.85 PFLOP/s); a few
+// 64-tiles take 4 to 5 us however little they compute.
 #pragma once
 #include "schulz_device.h"
 
