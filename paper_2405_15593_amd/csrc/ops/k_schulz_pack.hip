@@ -153,14 +153,26 @@ __global__ __launch_bounds__(256) void pack_kernel(const PackArgs a) {
 
   __shared__ double part[4];
   __shared__ __align__(16) half_t stage[2][64 * kLdsRow];
+  const PackMatrix& pm = a.mat[mat];
+  const bool momentum = pm.momentum != nullptr;
+  // the elements are fetched before the norm is put together
+  float g8[2][8], v8[2][8];
+#pragma unroll
+  for (int it = 0; it < 2; ++it) {
+    const int row = r0 + (int)(threadIdx.x >> 3) + it * 32, col = c0 + (int)(threadIdx.x & 7) * 8;
+    const int count = row < rows ? cols - col : 0;
+    if (count > 0) {
+      load8(pm.grad, (int64_t)row * pm.grad_ld + col, count, a.grad_bf16, g8[it]);
+      if (momentum) load8(pm.momentum, (int64_t)row * pm.momentum_ld + col, count, a.momentum_bf16, v8[it]);
+    }
+  }
+
   double sum = (int)threadIdx.x < a.n_parts ? a.partials[mat * kNormParts + threadIdx.x] : 0.0;
   sum = wave_sum(sum);
   if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
   __syncthreads();
   const double scale = (double)kScaleX / (sqrt((part[0] + part[1]) + (part[2] + part[3])) + a.eps);
 
-  const PackMatrix& pm = a.mat[mat];
-  const bool momentum = pm.momentum != nullptr;
   uint8_t* rec = a.ws + g.base + (uint64_t)(mat - g.first) * g.record;
   // a tall matrix lies as X^T does; another is turned in LDS
   half_t* xt = (half_t*)(rec + g.xt);
@@ -175,11 +187,9 @@ __global__ __launch_bounds__(256) void pack_kernel(const PackArgs a) {
     for (int i = 0; i < 8; ++i) hi[i] = lo[i] = (half_t)0.0f;
     const int count = row < rows ? cols - col : 0;
     if (count > 0) {
-      float g8[8], v8[8], u8[8];
-      load8(pm.grad, (int64_t)row * pm.grad_ld + col, count, a.grad_bf16, g8);
-      if (momentum) load8(pm.momentum, (int64_t)row * pm.momentum_ld + col, count, a.momentum_bf16, v8);
-      update8(a, g8, v8, momentum, u8);
-      if (momentum) store8(pm.momentum, (int64_t)row * pm.momentum_ld + col, count, a.momentum_bf16, v8);
+      float u8[8];
+      update8(a, g8[it], v8[it], momentum, u8);
+      if (momentum) store8(pm.momentum, (int64_t)row * pm.momentum_ld + col, count, a.momentum_bf16, v8[it]);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const float x = (float)((double)u8[i] * scale);
@@ -188,8 +198,8 @@ __global__ __launch_bounds__(256) void pack_kernel(const PackArgs a) {
       }
     }
     if (tall) {
-      *(half8*)(xt + (int64_t)row * g.mp + col) = hi;
-      if (a.split) *(half8*)(xt + plane + (int64_t)row * g.mp + col) = lo;
+      *(half8*)(xt + (int64_t)row * cols_p + col) = hi;
+      if (a.split) *(half8*)(xt + plane + (int64_t)row * cols_p + col) = lo;
     } else {
       *(half8*)&stage[0][r * kLdsRow + c] = hi;
       if (a.split) *(half8*)&stage[1][r * kLdsRow + c] = lo;

@@ -152,8 +152,8 @@ int queue_chunk(const Call& c, const Item* items, int32_t count, uint8_t* ws, hi
   pa.nesterov = c.nesterov ? 1 : 0;
   pa.grad_bf16 = c.grad_dtype == MICROADAM_BF16;
   pa.momentum_bf16 = c.momentum_dtype == MICROADAM_BF16;
-  // parts of about 8192 elements
-  pa.n_parts = (int32_t)std::min<int64_t>(kNormParts, std::max<int64_t>(1, most / 8192));
+  // parts of about 2048 elements, one read of each thread
+  pa.n_parts = (int32_t)std::min<int64_t>(kNormParts, std::max<int64_t>(1, most / 2048));
   hipError_t e;
   if ((e = launch_schulz_norm(pa, count, s)) != hipSuccess) return report_hip(e, "launching the norm kernel");
   if ((e = launch_schulz_pack(pa, count, s)) != hipSuccess) return report_hip(e, "launching the pack kernel");

@@ -39,7 +39,9 @@ float makespan(const GemmArgs& a, SchulzPhase phase, const TileForm& f) {
   // (up to one workgroup a CU, those of two a CU run alone)
   const bool full = all > (f.per_cu > 1 ? kCus : 3 * kCus / 4);
   const int64_t places = (int64_t)kCus * (full ? f.per_cu : 1);
-  const float rest = phase == kGram || phase == kPoly ? f.full_rest_symmetric : f.full_rest;
+  // two planes to store in split precision (the 64-tile's figures have them)
+  const float planes = a.split && f.tile != 64 ? 3.0f : 0.0f;
+  const float rest = (phase == kGram || phase == kPoly ? f.full_rest_symmetric : f.full_rest) + planes;
   // places that become free at the same time, earliest first
   struct Level {
     float at;
@@ -52,7 +54,7 @@ float makespan(const GemmArgs& a, SchulzPhase phase, const TileForm& f) {
     const SchulzGroup& g = a.group[i];
     const int k = phase == kGram ? g.np : g.mp;
     const float stages = (float)(k / 64 * (a.split && f.tile != 64 ? 3 : 1));
-    const float each = full ? stages * f.full_stage + rest : stages * f.few_stage + f.few_rest;
+    const float each = full ? stages * f.full_stage + rest : stages * f.few_stage + f.few_rest + planes;
     int64_t left = schulz_tiles(g, phase, f.tile);
     // whole rounds leave the differences between the places as they are
     const int64_t rounds = left / places;

@@ -147,7 +147,8 @@ def muon_step(params, grads, momenta, *, lr: float, momentum: float = 0.95, nest
     dtypes = grads[0].dtype, momenta[0].dtype, params[0].dtype
     rows = []
     for p, g, v in zip(params, grads, momenta):
-        if p.shape != g.shape or p.shape != v.shape:
+        shape = p.shape
+        if shape != g.shape or shape != v.shape:
             raise ValueError("a gradient or momentum has another shape than its parameter")
         if (g.dtype, v.dtype, p.dtype) != dtypes:
             raise TypeError("params, grads and momenta: one dtype per list")
@@ -155,14 +156,19 @@ def muon_step(params, grads, momenta, *, lr: float, momentum: float = 0.95, nest
             raise ValueError("params, grads and momenta: one device")
         if p.numel() == 0:
             raise ValueError("an empty matrix")
-        r, c = p.shape[-2:]
+        if len(shape) == 2 and p.is_contiguous() and g.is_contiguous() and v.is_contiguous():
+            r, c = shape
+            rows.append((g.data_ptr(), v.data_ptr(), p.data_ptr(), r, c, c, c, c))
+            continue
+        r, c = shape[-2:] if len(shape) >= 2 else (0, 0)
         for (pp, pl), (gp, gl), (vp, vl) in zip(_matrices(p, "params"), _matrices(g, "grads", written=False),
                                                 _matrices(v, "momenta")):
             rows.append((gp, vp, pp, r, c, gl, vl, pl))
     array = (microadam_matrix * len(rows))(*rows)
     with _on(device):
         ptr, size, keep = _workspace(cfg.schulz, array, len(rows), codes[2], device, workspace)
-        microadam_muon_step(cfg, array, len(rows), *codes, lr, ptr, size, torch.cuda.current_stream(device.index).cuda_stream)
+        microadam_muon_step(cfg, array, len(rows), *codes, lr, ptr, size,
+                            torch.cuda.current_stream(device.index).cuda_stream)
 
 
 class Muon(torch.optim.Optimizer):

@@ -85,6 +85,23 @@ def test_large_tiles():
         assert off(o[i], schulz64(g[i])) < F16_TOL + BF16
 
 
+# between them, every tile of every product in both precisions, with sizes that
+# end inside a tile
+TILED = [("f16", (194, 209), 54), ("f16", (132, 167), 88), ("f16", (67, 332), 87), ("f16", (455, 461), 33),
+         ("f16", (133, 406), 78), ("split", (336, 365), 76), ("split", (321, 338), 50), ("split", (65, 584), 80),
+         ("split", (132, 1318), 25)]
+
+
+@pytest.mark.parametrize("precision,shape,count", TILED, ids=str)
+def test_many_matrices(precision, shape, count):
+    print(f"[muon] {count} of {shape} {precision}", flush=True)
+    for r, c in (shape, shape[::-1]):
+        g = torch.stack([gradient(r, c, torch.float32, i) for i in range(count)])
+        o = orthogonalize(g, precision=precision)
+        worst = max(off(o[i], schulz64(g[i])) for i in range(count))
+        assert worst < (F16_TOL if precision == "f16" else SPLIT_TOL)
+
+
 def test_own_coefficients_and_steps():
     print("[muon] coefficients", flush=True)
     g = gradient(130, 200, torch.float32)
