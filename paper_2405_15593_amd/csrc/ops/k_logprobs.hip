@@ -458,23 +458,31 @@ __global__ __launch_bounds__(kMaxThreads) void row_kernel(const LogprobArgs a) {
 
 template <bool BF16, bool GRAD, bool ENTGRAD>
 hipError_t launch_rows(const LogprobArgs& a, hipStream_t s) {
-  const int chunks = a.vocab / Chunk<BF16>::kElems + 1;  // at most
+  const int chunks = a.vocab / Chunk<BF16>::kElems;  // at most
   const dim3 grid((unsigned)a.rows);
   auto threads = [&](int nv) {
     const int n = ((chunks + nv - 1) / nv + 63) / 64 * 64;
     return n < 64 ? 64 : n;
   };
-  // Up to 8 chunks per thread in workgroups of up to 512, which leave a CU room
-  // for a second row (509 x 30522 bf16 with the gradient: 15 us, with 4 chunks
-  // in 1024 threads 18 us); with few rows a row's own time counts, and more
-  // threads shorten it (1 x 32000 bf16: 8.7 us, against 9.3).
+  // With few rows a row's own time counts: few chunks in up to 1024 threads
+  // (1 x 32000 bf16: 8.7 us, with 8 chunks in 512 threads 9.3).  With many, up
+  // to 8 chunks in small workgroups, of which a CU holds more (2048 x 16384
+  // bf16 with 8 alternatives: 18.9 us in 256 threads, 27.5 in 512 with 4).
+  //
+  // Values alone read a row once in segments too, in a third of the registers:
+  // long rows without alternatives take 256 threads (2048 x 50257 bf16: 42 us,
+  // held whole 61), and so do longer ones with them, which are then read twice
+  // (67 us, held whole 81; binary32, twice the bytes, gains only beyond its
+  // registers).
   const bool few = a.rows <= 128;
-  const int most = few ? kMaxThreads : 256;
-  if (threads(1) <= most)
+  const int most = few ? kMaxThreads : 64;
+  if (!GRAD && !few && threads(8) > (a.top_k == 0 ? 256 : BF16 ? 512 : 2 * kMaxThreads))
+    row_kernel<BF16, 8, GRAD, ENTGRAD, true><<<grid, 256, 0, s>>>(a);
+  else if (threads(1) <= most)
     row_kernel<BF16, 1, GRAD, ENTGRAD, false><<<grid, threads(1), 0, s>>>(a);
   else if (threads(2) <= most)
     row_kernel<BF16, 2, GRAD, ENTGRAD, false><<<grid, threads(2), 0, s>>>(a);
-  else if (threads(4) <= (few ? kMaxThreads : 512))
+  else if (threads(4) <= (few ? kMaxThreads : 256))
     row_kernel<BF16, 4, GRAD, ENTGRAD, false><<<grid, threads(4), 0, s>>>(a);
   else if (threads(8) <= kMaxThreads)
     row_kernel<BF16, 8, GRAD, ENTGRAD, false><<<grid, threads(8), 0, s>>>(a);

@@ -103,6 +103,23 @@ def test_sizes(vocab, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("vocab", [500, 1024, 2048, 4096, 9001, 16384, 24001, 32000, 50257, 70001])
+def test_many_rows(vocab, dtype):
+    """Enough rows that throughput decides the launch's form."""
+    print(f"[logprobs] 200 rows of {vocab} {dtype}", flush=True)
+    x, t = logits_of(200, vocab, dtype, vocab, 1)
+    t[::7] = -100
+    x[3, :] = NINF
+    x[4, : vocab // 2] = NINF
+    check_values(x, t, 0, 0.8)
+    check_values(x, t, 11)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    gp, gh = torch.randn(2, 200, generator=g, device="cuda")
+    check_grad(x, t, gp, None)
+    check_grad(x, t, gp, gh, 1.4)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("k", [1, 2, 20, 63, 64])
 def test_alternatives(k, dtype):
     """Ties, few allowed tokens, the best ones side by side or at the ends."""
