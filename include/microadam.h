@@ -396,6 +396,8 @@ int microadam_matrix_workspace(const microadam_schulz_config* cfg, const microad
  * Nothing is allocated on the device and no handle is kept: the workspace
  * (256-byte aligned, of any content) belongs to the caller and is in use
  * until the queued work is done.  The same inputs give the same bits.
+ * Outputs must not overlap each other, nor any grad but their own; one address
+ * twice is refused.
  * A matrix that holds NaN or an infinity gives NaN throughout; the others of
  * the list are not touched by it.
  */
@@ -413,7 +415,7 @@ int microadam_orthogonalize(const microadam_schulz_config* cfg, const microadam_
  * sqrt(max(1, rows / cols)) for MICROADAM_SCALE_SPECTRAL and 1 for
  * MICROADAM_SCALE_NONE.  V starts as zeros, which the caller provides.
  * Workspace, order and non-finite values as for microadam_orthogonalize.  The
- * matrices of one list must not overlap.
+ * matrices of one list must not overlap, and none is in it twice.
  */
 enum { MICROADAM_SCALE_MATCH_RMS = 0, MICROADAM_SCALE_SPECTRAL = 1, MICROADAM_SCALE_NONE = 2 };
 
@@ -475,7 +477,8 @@ int microadam_token_logprobs(const microadam_logits* logits, int32_t top_k, floa
  *     L = sum over rows of grad_logp * logp + grad_entropy * entropy
  * with respect to the logits: grad[rows][vocab] of the logits' dtype, grad_ld
  * elements from row to row.  grad_entropy may be NULL (zeros).  grad may be
- * the logits themselves when the row strides agree.
+ * the logits themselves when the row strides agree; any other overlap of its
+ * rows with theirs is refused.
  */
 int microadam_token_logprobs_grad(const microadam_logits* logits, const float* grad_logp,
                                   const float* grad_entropy, float* logp, float* entropy, void* grad,

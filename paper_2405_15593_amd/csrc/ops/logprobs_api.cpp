@@ -50,6 +50,17 @@ int check(const microadam_logits* l, LogprobArgs& a) {
   return MICROADAM_OK;
 }
 
+// Whether rows of `width` bytes, `stride` apart, starting at x and at g share
+// bytes: one stride, the places within it decide; two, the ranges do.
+bool share_bytes(const void* x, int64_t stride_x, const void* g, int64_t stride_g, int64_t rows, int64_t width) {
+  const uintptr_t a = (uintptr_t)x, b = (uintptr_t)g;
+  const uint64_t reach_x = (uint64_t)((rows - 1) * stride_x + width), reach_g = (uint64_t)((rows - 1) * stride_g + width);
+  if (a <= b ? b - a >= reach_x : a - b >= reach_g) return false;
+  if (rows == 1 || stride_x != stride_g) return true;
+  const int64_t place = (int64_t)((a <= b ? b - a : a - b) % (uint64_t)stride_x);
+  return place < width || place > stride_x - width;
+}
+
 bool aligned4(const void* p) { return (uintptr_t)p % 4 == 0; }
 
 int launch(const LogprobArgs& a, int32_t dtype, void* stream) {
@@ -96,6 +107,9 @@ int microadam_token_logprobs_grad(const microadam_logits* logits, const float* g
     if (grad_ld > ((int64_t)1 << 40)) return report(MICROADAM_ERR_UNSUPPORTED, "the gradient's row stride is above 2^40");
     if (grad == logits->data && grad_ld != logits->ld)
       return report(MICROADAM_ERR_INVALID_ARG, "in place, the row strides must agree");
+    const int64_t size = logits->dtype == MICROADAM_BF16 ? 2 : 4;
+    if (grad != logits->data && share_bytes(logits->data, logits->ld * size, grad, grad_ld * size, a.rows, a.vocab * size))
+      return report(MICROADAM_ERR_INVALID_ARG, "the gradient overlaps the logits without being in place");
     if (!aligned4(grad_logp) || !aligned4(grad_entropy) || !aligned4(logp) || !aligned4(entropy) ||
         (uintptr_t)grad % (logits->dtype == MICROADAM_BF16 ? 2 : 4))
       return report(MICROADAM_ERR_INVALID_ARG, "an argument is not aligned to its element type");

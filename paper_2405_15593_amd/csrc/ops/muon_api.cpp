@@ -71,6 +71,18 @@ int check_operand(const void* p, int64_t ld, int64_t cols, int32_t dtype, const 
   return MICROADAM_OK;
 }
 
+// What is written must not be in the list twice: its tiles would race.
+int check_once(const microadam_matrix* mats, int32_t n, bool momentum) {
+  std::vector<uintptr_t> at((size_t)n);
+  for (int pass = 0; pass < (momentum ? 2 : 1); ++pass) {
+    for (int32_t i = 0; i < n; ++i) at[i] = (uintptr_t)(pass ? mats[i].momentum : mats[i].out);
+    std::sort(at.begin(), at.end());
+    if (std::adjacent_find(at.begin(), at.end()) != at.end())
+      return report(MICROADAM_ERR_INVALID_ARG, pass ? "a momentum is in the list twice" : "an output is in the list twice");
+  }
+  return MICROADAM_OK;
+}
+
 // Padded sizes and the offsets of a record of a group of m x n.
 SchulzGroup group_of(int32_t m, int32_t n, bool split) {
   SchulzGroup g;
@@ -202,6 +214,8 @@ int run(const Call& c, int32_t n, void* workspace, uint64_t workspace_bytes, hip
   for (const Item& it : items)
     if (kPartialBytes + group_of(it.m, it.n, split).record > workspace_bytes)
       return report(MICROADAM_ERR_STATE_SIZE, "workspace smaller than microadam_matrix_workspace's minimum");
+  const int twice = check_once(c.mats, n, c.momentum);
+  if (twice) return twice;
   int32_t begin = 0;
   while (begin < n) {
     uint64_t bytes = kPartialBytes;

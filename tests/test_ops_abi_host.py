@@ -177,6 +177,42 @@ def test_logprob_arguments():
     f(logits(rows=0, data=0, targets=0), 3, None, None, None, None)   # nothing to do
 
 
+@pytest.mark.parametrize("dtype,size", [(F32, 4), (BF16, 2)])
+def test_gradient_that_overlaps_the_logits(dtype, size):
+    """Rows of 100 at a stride of 256: a gradient that starts in a row, or ends
+    in one, is refused; between the rows, behind them or in place is not (no
+    target address: those come to the next refusal, by its own message)."""
+    g = ma.microadam_token_logprobs_grad
+    at = 1 << 20
+    x = logits(data=at, ld=256, dtype=dtype)
+    ends = 3 * 256 + 100  # of the four rows
+    for off in (1, 99, 157, 255, 256, 355, 413, -1, -99, -157, -256, ends - 1, -(ends - 1)):
+        with pytest.raises(ma.MicroAdamError, match="overlaps"):
+            g(x, 256, None, 256, 256, at + off * size, 256)
+    for off in (1, 100, ends - 1, -1, -(3 * 300 + 99)):  # another stride, ranges that meet
+        with pytest.raises(ma.MicroAdamError, match="overlaps"):
+            g(x, 256, None, 256, 256, at + off * size, 300)
+    one = logits(data=at, rows=1, ld=100, dtype=dtype)
+    for off in (1, 99, -1, -99):
+        with pytest.raises(ma.MicroAdamError, match="overlaps"):
+            g(one, 256, None, 256, 256, at + off * size, 100)
+    # these pass the overlap check and are refused for logp's alignment
+    for off, ld in ((100, 256), (156, 256), (356, 256), (-100, 256), (-156, 256), (ends, 300), (0, 256),
+                    (-(3 * 300 + 100), 300)):
+        with pytest.raises(ma.MicroAdamError, match="an argument is not aligned"):
+            g(x, 256, None, 257, 256, at + off * size, ld)
+
+
+def test_a_matrix_twice():
+    a = dict(grad=4096, momentum=None, out=8192, rows=8, cols=16, grad_ld=16, momentum_ld=0, out_ld=16)
+    twice = matrices(tuple(a.values()), tuple(dict(a, grad=1 << 16).values()))
+    refused(INVALID, orth, ma.make_schulz_config(), twice, 2)
+    m = dict(a, momentum=1 << 17, momentum_ld=16)
+    for other in (dict(m, momentum=1 << 18), dict(m, out=1 << 18)):
+        refused(INVALID, ma.microadam_muon_step, muon_config(), matrices(tuple(m.values()), tuple(other.values())), 2,
+                F32, F32, F32, 0.1, 256, 1 << 30)
+
+
 def test_null_pointers():
     lib = ma.load()
     assert lib.microadam_orthogonalize(None, good(), 1, F32, F32, None, 0, None) == INVALID
