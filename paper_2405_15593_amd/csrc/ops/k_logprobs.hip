@@ -13,9 +13,9 @@
 // thread sums against its own maximum, and one reduction joins (max, s, w) of
 // the threads, so that no pass over the row waits for a maximum of all.  The
 // alternatives and the gradient come from the registers.  A row too long for
-// them is taken in segments, read twice.  The bound is memory, a row's bytes
-// once and once more for the gradient: 8192 x 32000 bf16 with the gradient takes
-// 157 us (6.0 TB/s).  4096 x 32000 with 8 alternatives and no gradient takes 69
+// them is taken in segments, and read again for the alternatives or the
+// gradient.  The bound is memory, a row's bytes once and once more for the
+// gradient: 8192 x 32000 bf16 with the gradient takes 158 us (6.6 TB/s).  4096 x 32000 with 8 alternatives and no gradient takes 69
 // us (3.8 TB/s): 13 vector operations and an exponential per element, and two
 // rows a CU to overlap them with the loads.
 #include "logprobs_device.h"
