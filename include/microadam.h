@@ -383,7 +383,9 @@ typedef struct microadam_matrix {
  * is what the calls below accept, *useful_bytes what lets them take matrices
  * of the list together, at most 2 GiB or one matrix if that is larger.  The
  * list is worked off in batches of as many matrices as the workspace holds
- * (at most 96, of at most 8 shapes); a batch takes 2 + 3 * steps launches.
+ * (at most 96, of at most 8 shapes); a batch takes 2 + 3 * steps launches, and
+ * one more per step where few rows against a long side have their products
+ * summed in parts.
  * Either output may be NULL.  out_dtype as for the call it is meant for (the
  * parameters' dtype for microadam_muon_step).
  */

@@ -17,6 +17,7 @@ namespace microadam {
 namespace {
 
 typedef _Float16 half_t;
+typedef half_t half4 __attribute__((ext_vector_type(4)));
 typedef half_t half8 __attribute__((ext_vector_type(8)));
 typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
 typedef float float4v __attribute__((ext_vector_type(4)));
@@ -219,6 +220,62 @@ __global__ __launch_bounds__(256) void pack_kernel(const PackArgs a) {
   }
 }
 
+// A 64 x 64 tile of A from the sums of its K's parts, in a fixed order; four
+// workgroups take 16 rows each, and each quarter of a workgroup every fourth
+// part.  grid: (4 x tiles of the group with most, matrices).
+__global__ __launch_bounds__(1024) void join_kernel(const GemmArgs a) {
+  int gi = 0;
+  while (gi + 1 < a.n_groups && (int)blockIdx.y >= a.group[gi + 1].first) ++gi;
+  const SchulzGroup& g = a.group[gi];
+  const int parts = a.parts[gi];
+  constexpr int T = 64;
+  const int tm = g.mp / T, per = tm * (tm + 1) / 2;
+  const int tile = (int)blockIdx.x >> 2, r0 = ((int)blockIdx.x & 3) * 16;
+  if (parts == 1 || tile >= per) return;
+  int ti, tj;
+  symmetric_tile(tile, tm, ti, tj);
+
+  uint8_t* rec = a.ws + g.base + (uint64_t)((int)blockIdx.y - g.first) * g.record;
+  const uint64_t xt_bytes = (uint64_t)g.mp * g.np * (a.split ? 4 : 2);
+  const int quarter = (int)threadIdx.x >> 8, t = (int)threadIdx.x & 255;
+  const int row = r0 + (t >> 4), col = (t & 15) * 4;
+  const int64_t plane = (int64_t)g.mp * g.mp, at = (int64_t)(ti * T + row) * g.mp + tj * T + col;
+  const float* sums = (const float*)(rec + g.xt + (a.buffer ? 0 : xt_bytes)) + at;
+  float4v sum = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 8
+  for (int p = quarter; p < parts; p += 4) sum += *(const float4v*)(sums + p * plane);
+  __shared__ float4v quarters[3][256];
+  __shared__ half_t stage[2][T][16 + 2];
+  if (quarter) quarters[quarter - 1][t] = sum;
+  __syncthreads();
+  half_t* out = (half_t*)(rec + g.a);
+  if (!quarter) {
+    sum = (sum + quarters[0][t]) + (quarters[1][t] + quarters[2][t]);
+    // rounded once (and what that left)
+    half4 hi, lo;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float v = sum[i] * (kScaleA / (kScaleX * kScaleX));
+      hi[i] = (half_t)v;
+      lo[i] = (half_t)((v - (float)hi[i]) * kSplitScale);
+      stage[0][col + i][row - r0] = hi[i];
+      stage[1][col + i][row - r0] = lo[i];
+    }
+    *(half4*)(out + at) = hi;
+    if (a.split) *(half4*)(out + plane + at) = lo;
+  }
+  if (ti == tj) return;  // the whole workgroup
+  __syncthreads();
+  if (quarter) return;
+  const int c = t >> 2, r = (t & 3) * 4;
+  for (int p = 0; p <= (a.split ? 1 : 0); ++p) {
+    half4 v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = stage[p][c][r + i];
+    *(half4*)(out + p * plane + (int64_t)(tj * T + c) * g.mp + ti * T + r0 + r) = v;
+  }
+}
+
 }  // namespace
 
 hipError_t launch_schulz_norm(const PackArgs& a, int n_matrices, hipStream_t s) {
@@ -237,6 +294,21 @@ hipError_t launch_schulz_pack(const PackArgs& a, int n_matrices, hipStream_t s) 
   }
   if (tiles >= ((int64_t)1 << 24)) return hipErrorInvalidValue;
   pack_kernel<<<dim3((unsigned)tiles, (unsigned)n_matrices), 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_schulz_join(const GemmArgs& a, hipStream_t s) {
+  if (a.n_groups < 1 || a.n_groups > kMaxGroups) return hipErrorInvalidValue;
+  int64_t tiles = 0;
+  int matrices = 0;
+  for (int i = 0; i < a.n_groups; ++i) {
+    const int64_t tm = a.group[i].mp / 64;
+    if (a.parts[i] > 1) tiles = tm * (tm + 1) / 2 > tiles ? tm * (tm + 1) / 2 : tiles;
+    matrices = a.group[i].first + a.group[i].count;
+  }
+  if (tiles == 0) return hipSuccess;
+  if (4 * tiles >= kMaxTiles || matrices > kMaxMatrices) return hipErrorInvalidValue;
+  join_kernel<<<dim3((unsigned)(4 * tiles), (unsigned)matrices), 1024, 0, s>>>(a);
   return hipGetLastError();
 }
 

@@ -21,6 +21,7 @@ constexpr int kMaxMatrices = 96;  // matrices per launch (their addresses are ke
 constexpr int kPad = 64;          // working dimensions are padded to this
 constexpr int64_t kMaxTiles = (int64_t)1 << 24;  // of a product's launch
 constexpr int kNormParts = 256;   // partial sums of a matrix's norm
+constexpr int kPartTile = 128;    // the largest tile whose products may be split over K
 
 // Powers of two, so that scaling rounds nothing.  Elements of X are at most
 // about 1 and around 1/sqrt(mn) at the start (1.5e-4 for 4096 x 11008), those
@@ -82,18 +83,58 @@ struct GemmArgs {
   int32_t out_bf16, update;  // kFinal: update out in place (out = decay * out - scale * D) or store scale * D
   int32_t tiles[kMaxGroups];           // of each group, and an eighth of them, rounded up
   int32_t turns[kMaxGroups];
+  // kGram in tiles of up to kPartTile: a tile's K is taken in `parts` runs of
+  // `part_stages` stages of 64 by as many workgroups.  Where they are more than
+  // one, their binary32 sums lie in the XT buffer that the step has yet to
+  // write, [part][mp][mp] with the tiles on and below the diagonal, until they
+  // are joined.
+  int32_t parts[kMaxGroups], part_stages[kMaxGroups];
   SchulzGroup group[kMaxGroups];
   OutMatrix mat[kMaxMatrices];         // kFinal
   uint8_t tall[kMaxMatrices];
 };
 
+constexpr int kStrip = 8;  // tile rows
+
+#ifdef __HIPCC__
+// The row r of a triangle of rows 0, 1, 2, .. of 1, 2, 3, .. that entry t
+// falls in.
+__device__ inline int triangle_row(int t) {
+  int r = (int)((__builtin_amdgcn_sqrtf(8.0f * (float)t + 1.0f) - 1.0f) * 0.5f);
+  while (r * (r + 1) / 2 > t) --r;
+  while ((r + 1) * (r + 2) / 2 <= t) ++r;
+  return r;
+}
+
+// Tile `tile` of the tiles on and below the diagonal of tm x tm, in strips of
+// kStrip tile rows, column by column.  The same in every lane.
+__device__ inline void symmetric_tile(int tile, int tm, int& ti, int& tj) {
+  auto uniform = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+  // rows before a strip of a triangle hold first * (first + 1) / 2 tiles
+  const int first = uniform(triangle_row(tile)) / kStrip * kStrip;
+  const int high = tm - first < kStrip ? tm - first : kStrip;
+  const int in = tile - first * (first + 1) / 2;
+  if (in < high * first) {
+    tj = uniform(in / high);
+    ti = first + in - tj * high;
+  } else {
+    const int corner = in - high * first;
+    const int r = uniform(triangle_row(corner));
+    ti = first + r;
+    tj = first + corner - r * (r + 1) / 2;
+  }
+}
+#endif
+
 hipError_t launch_schulz_norm(const PackArgs& a, int n_matrices, hipStream_t s);
 hipError_t launch_schulz_pack(const PackArgs& a, int n_matrices, hipStream_t s);
 
 int64_t schulz_tiles(const SchulzGroup& g, SchulzPhase phase, int tile);
-// The tile (64, 128, 192 or 256) that takes a launch's products least time.
-int choose_schulz_tile(const GemmArgs& a, SchulzPhase phase);
+// The tile (64, 128, 192 or 256) that takes a launch's products least time;
+// sets parts and part_stages for kGram.
+int choose_schulz_tile(GemmArgs& a, SchulzPhase phase);
 hipError_t launch_schulz_gemm(GemmArgs& a, SchulzPhase phase, int tile, hipStream_t s);
+hipError_t launch_schulz_join(const GemmArgs& a, hipStream_t s);
 hipError_t launch_schulz_gemm_64(const GemmArgs& a, SchulzPhase phase, hipStream_t s);
 hipError_t launch_schulz_gemm_128(const GemmArgs& a, SchulzPhase phase, hipStream_t s);
 hipError_t launch_schulz_gemm_192(const GemmArgs& a, SchulzPhase phase, hipStream_t s);

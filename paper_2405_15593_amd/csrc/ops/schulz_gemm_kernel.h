@@ -18,6 +18,10 @@
 // The symmetric products compute the tiles on and below the diagonal and
 // store each twice.
 //
+// X X^T of few rows is a few tiles with a long K: the K of tiles up to 128
+// can be split over workgroups, whose sums join_kernel (k_schulz_pack.hip)
+// adds up (what it gives stands in schulz_launch.cpp).
+//
 // Large products are bound by the power limit: X^T B of 4096 x 11008 takes 285
 // to 305 us in 256-tiles (1.2 to 1.3 PFLOP/s; the library's 8192^3 in binary16:
 // 1.33), the matrix cores busy for 65% of 1.6 to 1.8 GHz.  With K = 768 the
@@ -75,15 +79,6 @@ struct Form<64> {
 
 // A value that is the same in every lane, as a scalar.
 __device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-
-// The row r of a triangle of rows 0, 1, 2, .. of 1, 2, 3, .. that entry t
-// falls in.
-__device__ inline int triangle_row(int t) {
-  int r = (int)((__builtin_amdgcn_sqrtf(8.0f * (float)t + 1.0f) - 1.0f) * 0.5f);
-  while (r * (r + 1) / 2 > t) --r;
-  while ((r + 1) * (r + 2) / 2 <= t) ++r;
-  return r;
-}
 
 // The transposing LDS read: of sixteen lanes, lanes 4 r to 4 r + 3 address row
 // r's four times four elements, and lane i receives element i of four rows.
@@ -153,11 +148,17 @@ __global__ __launch_bounds__(128 * Form<T>::wq, 2) void gemm_kernel(const GemmAr
   int turn = (int)blockIdx.x >> 3;
   SchulzGroup g = a.group[0];
   int tiles = a.tiles[0];
+  constexpr bool kRuns = PHASE == kGram && T <= kPartTile;
+  int parts = kRuns ? a.parts[0] : 1, part_stages = kRuns ? a.part_stages[0] : 0;
   if (a.n_groups > 1 && turn >= a.turns[0]) {
     int gi = 0;
     while (gi + 1 < a.n_groups && turn >= a.turns[gi]) turn -= a.turns[gi++];
     g = a.group[gi];
     tiles = a.tiles[gi];
+    if (kRuns) {
+      parts = a.parts[gi];
+      part_stages = a.part_stages[gi];
+    }
   }
   const int each = tiles >> 3, more = tiles & 7;
   if (turn >= each + (xcd < more ? 1 : 0)) return;
@@ -166,30 +167,21 @@ __global__ __launch_bounds__(128 * Form<T>::wq, 2) void gemm_kernel(const GemmAr
   const int tm = (g.mp + T - 1) / T, tn = (g.np + T - 1) / T;
   constexpr bool kSym = PHASE == kGram || PHASE == kPoly;
   const int per = kSym ? tm * (tm + 1) / 2 : tm * tn;
-  const int which = uniform(tile / per);
+  int which = uniform(tile / per), part = 0;
   tile -= which * per;
+  if (kRuns && parts > 1) {
+    part = uniform(which % parts);
+    which = uniform(which / parts);
+  }
   const int mat = g.first + which;
   // X^T's rows are D's rows: always to keep X^T, at the end for a tall matrix
   const bool swap = PHASE == kApply || (PHASE == kFinal && uniform(a.tall[mat]));
 
   // Tile (ti, tj) of D: strips of kStrip tile rows, column by column, so that
   // the 32 tiles an XCD's CUs take at a time need about 8 + 4 operand tiles.
-  constexpr int kStrip = 8;
   int ti, tj;
   if (kSym) {
-    // rows before a strip of a triangle hold first * (first + 1) / 2 tiles
-    const int first = uniform(triangle_row(tile)) / kStrip * kStrip;
-    const int high = tm - first < kStrip ? tm - first : kStrip;
-    const int in = tile - first * (first + 1) / 2;
-    if (in < high * first) {
-      tj = uniform(in / high);
-      ti = first + in - tj * high;
-    } else {
-      const int corner = in - high * first;
-      const int r = uniform(triangle_row(corner));
-      ti = first + r;
-      tj = first + corner - r * (r + 1) / 2;
-    }
+    symmetric_tile(tile, tm, ti, tj);
   } else {
     const int strip = uniform(tile / (kStrip * tn)), first = strip * kStrip;
     const int high = tm - first < kStrip ? tm - first : kStrip;
@@ -237,15 +229,17 @@ __global__ __launch_bounds__(128 * Form<T>::wq, 2) void gemm_kernel(const GemmAr
   // stage's 64 rows of X^T from column p0 (q0) on; columns past the matrix read
   // the next row's, whose results are not stored.
   const uint32_t row_bytes = (uint32_t)g.mp * 2;
-  const uint8_t* tp = p + (PHASE == kGram ? (uint64_t)p0 * 2 : (uint64_t)p0 * row_bytes);
-  const uint8_t* tq = q + (PHASE == kGram ? (uint64_t)q0 * 2 : (uint64_t)q0 * row_bytes);
+  const int first_stage = kRuns ? part * part_stages : 0;
+  const uint8_t* tp = p + (PHASE == kGram ? (uint64_t)p0 * 2 + (uint64_t)((uint32_t)first_stage * kStep) * row_bytes : (uint64_t)p0 * row_bytes);
+  const uint8_t* tq = q + (PHASE == kGram ? (uint64_t)q0 * 2 + (uint64_t)((uint32_t)first_stage * kStep) * row_bytes : (uint64_t)q0 * row_bytes);
   const int size_p = (int)(PHASE == kGram ? kStep * row_bytes - (uint32_t)p0 * 2 : (uint32_t)left_p * row_bytes);
   const int size_q = (int)(PHASE == kGram ? kStep * row_bytes - (uint32_t)q0 * 2 : (uint32_t)left_q * row_bytes);
   // the 16-byte chunk c of row r is kept at position c ^ spread(r)
   auto spread = [](int r) { return (r >> 1) & 7; };
   const int load_row = lane >> 3;
   const int voff = load_row * (int)row_bytes + ((lane & 7) ^ spread(load_row)) * 16;
-  const int ksteps = (PHASE == kGram ? g.np : g.mp) / kStep;
+  int ksteps = (PHASE == kGram ? g.np : g.mp) / kStep;
+  if (kRuns && parts > 1) ksteps = ksteps - first_stage < part_stages ? ksteps - first_stage : part_stages;
   // kGram: the 32-byte segment s of row r is kept at position s ^ turn, by the
   // bits of r that the rows of one read differ in
   constexpr bool kWide = T % 128 == 0;  // whole 256-byte rows: all of a read's eight rows on the same banks
@@ -432,6 +426,19 @@ __global__ __launch_bounds__(128 * Form<T>::wq, 2) void gemm_kernel(const GemmAr
       for (int j = 0; j < kJ; ++j) acc[i][j] += cross[i][j] * (1.0f / kSplitScale);
   }
 
+  if constexpr (kRuns) {
+    if (parts > 1) {
+      float* sums = (float*)(rec + g.xt + (a.buffer ? 0 : xt_bytes)) + (int64_t)part * g.mp * g.mp;
+#pragma unroll
+      for (int i = 0; i < kI; ++i)
+#pragma unroll
+        for (int j = 0; j < kJ; ++j) {
+          const int row = p0 + wp0 + i * 16 + lrow, col = q0 + wq0 + j * 16 + lcol;
+          if (row < g.mp && col < g.mp) *(float4v*)(sums + (int64_t)row * g.mp + col) = acc[i][j];
+        }
+      return;
+    }
+  }
   if constexpr (PHASE == kFinal) {
     const OutMatrix& om = a.mat[mat];
     const int out_rows = swap ? g.n : g.m, out_cols = swap ? g.m : g.n;

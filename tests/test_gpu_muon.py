@@ -206,6 +206,44 @@ def test_muon_step(dtype, vdtype, nesterov, scale):
             assert float(err) < tol * float(move.norm()) + rounding * float(p.double().norm())
 
 
+# few rows against a long side: X X^T's sums are taken in runs (of at most
+# 1152 terms here, no more than SPLIT_TOL covers) and joined
+LONG = [(1, 20000), (2, 4097), (16, 11008), (64, 8192), (70, 9001), (200, 6100), (257, 2500), (520, 7777)]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("shape", LONG, ids=str)
+def test_long_sides(shape, dtype):
+    print(f"[muon] long {shape} {dtype}", flush=True)
+    for s in (shape, shape[::-1]):
+        g = gradient(*s, dtype)
+        a, b = orthogonalize(g), orthogonalize(g)
+        assert torch.equal(a, b)
+        assert off(a, schulz64(g)) < (SPLIT_TOL if dtype == torch.float32 else F16_TOL + BF16), s
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_long_sides_among_others(dtype):
+    """One list, whose shapes take different numbers of runs, in the useful
+    workspace and in the least; scratch of any content."""
+    print(f"[muon] long sides among others {dtype}", flush=True)
+    shapes = [(16, 9000), (40, 40), (9000, 16), (16, 9000), (130, 3000), (64, 4096), (1, 5000), (300, 300)]
+    lo, hi = workspace_bytes(shapes, dtype)
+    tol = SPLIT_TOL if dtype == torch.float32 else F16_TOL
+    rounding = 2.0 ** -23 if dtype == torch.float32 else BF16
+    for size in (hi, lo):
+        ws = torch.full((size,), 255, dtype=torch.uint8, device="cuda")
+        ps = [gradient(*s, dtype, 3 + i, 0.5) for i, s in enumerate(shapes)]
+        gs = [gradient(*s, dtype, 30 + i) for i, s in enumerate(shapes)]
+        vs = [torch.zeros(s, device="cuda") for s in shapes]
+        before = [p.double().clone() for p in ps]
+        muon_step(ps, gs, vs, lr=0.1, momentum=0.5, nesterov=False, scale="none", workspace=ws)
+        for p, p0, g in zip(ps, before, gs):
+            move = 0.1 * schulz64(g)
+            err = (p.double() - (p0 - move)).norm()
+            assert float(err) < tol * float(move.norm()) + rounding * float(p.double().norm()), tuple(p.shape)
+
+
 def test_graph_replays():
     """Captured, the call replays on what the buffers then hold."""
     print("[muon] graph", flush=True)
