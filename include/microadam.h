@@ -397,7 +397,9 @@ int microadam_matrix_workspace(const microadam_schulz_config* cfg, const microad
  * out = the orthogonalised grad, matrix by matrix, queued on `stream`.
  * Nothing is allocated on the device and no handle is kept: the workspace
  * (256-byte aligned, of any content) belongs to the caller and is in use
- * until the queued work is done.  The same inputs give the same bits.
+ * until the queued work is done.  The same list in a workspace of the same size
+ * gives the same bits (batches of other matrices may be summed in another
+ * order).
  * Outputs must not overlap each other, nor any grad but their own; one address
  * twice is refused.
  * A matrix that holds NaN or an infinity gives NaN throughout; the others of
