@@ -440,7 +440,9 @@ int microadam_muon_step(const microadam_muon_config* cfg, const microadam_matrix
  * ------------------------------------------------- token log probabilities
  *
  * `rows` rows of `vocab` logits x, ld elements apart (at least vocab), and one
- * token per row.  With z = x / temperature, lp_v = z_v - log sum exp z and
+ * token per row.  With group_rows > 0 (a divisor of rows) they come in groups
+ * of as many, which start group_stride elements apart: the rows [:, :-1] of
+ * sequences, say.  With z = x / temperature, lp_v = z_v - log sum exp z and
  * p = exp lp:
  *     logp = lp at the row's token,   entropy = -sum p lp  (0 where p = 0),
  * all sums in binary32, each exponent taken from the row's maximum.  vocab is
@@ -466,6 +468,8 @@ typedef struct microadam_logits {
   double temperature; /* finite, > 0 */
   int32_t dtype;      /* MICROADAM_F32 or MICROADAM_BF16 */
   int32_t reserved;   /* 0 */
+  int64_t group_rows;   /* 0: rows at one stride */
+  int64_t group_stride;
 } microadam_logits;
 
 /*
@@ -481,7 +485,7 @@ int microadam_token_logprobs(const microadam_logits* logits, int32_t top_k, floa
  *     L = sum over rows of grad_logp * logp + grad_entropy * entropy
  * with respect to the logits: grad[rows][vocab] of the logits' dtype, grad_ld
  * elements from row to row.  grad_entropy may be NULL (zeros).  grad may be
- * the logits themselves when the row strides agree; any other overlap of its
+ * the logits themselves when the row strides agree and group_rows is 0; any other overlap of its
  * rows with theirs is refused.
  */
 int microadam_token_logprobs_grad(const microadam_logits* logits, const float* grad_logp,

@@ -126,6 +126,8 @@ class microadam_logits(ctypes.Structure):
         ("temperature", ctypes.c_double),
         ("dtype", ctypes.c_int32),
         ("reserved", ctypes.c_int32),
+        ("group_rows", ctypes.c_int64),
+        ("group_stride", ctypes.c_int64),
     ]
 
 

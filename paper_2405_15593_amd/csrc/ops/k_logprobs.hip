@@ -155,7 +155,12 @@ __global__ __launch_bounds__(kMaxThreads) void row_kernel(const LogprobArgs a) {
   const int lane = tid & 63, wave = tid >> 6;
   const int64_t target = a.targets[row];
   const int k = GRAD ? 0 : a.top_k;
-  const uint8_t* const x = (const uint8_t*)a.logits + row * a.ld * C::kSize;
+  int64_t start = row * a.ld;
+  if (a.group_rows) {
+    const uint32_t group = (uint32_t)row / (uint32_t)a.group_rows;
+    start = group * a.group_stride + (int64_t)((uint32_t)row - group * (uint32_t)a.group_rows) * a.ld;
+  }
+  const uint8_t* const x = (const uint8_t*)a.logits + start * C::kSize;
   uint8_t* const dx = GRAD ? (uint8_t*)a.grad + row * a.grad_ld * C::kSize : nullptr;
   const int V = a.vocab;
 

@@ -27,6 +27,11 @@ int check(const microadam_logits* l, LogprobArgs& a) {
   if (l->rows > kMaxRows) return report(MICROADAM_ERR_UNSUPPORTED, "more than 2^20 rows");
   if (l->ld < l->vocab && l->rows > 1) return report(MICROADAM_ERR_INVALID_ARG, "the row stride is below vocab");
   if (l->ld > ((int64_t)1 << 40)) return report(MICROADAM_ERR_UNSUPPORTED, "the row stride is above 2^40");
+  if (l->group_rows < 0 || (l->group_rows > 0 && l->rows % l->group_rows) || l->group_stride < 0 ||
+      (l->group_rows == 0 && l->group_stride != 0))
+    return report(MICROADAM_ERR_INVALID_ARG, "group_rows must divide rows, and group_stride be 0 without it");
+  if (l->group_stride > ((int64_t)1 << 40))
+    return report(MICROADAM_ERR_UNSUPPORTED, "the stride of groups is above 2^40");
   if (!(l->temperature > 0.0) || !std::isfinite(l->temperature))
     return report(MICROADAM_ERR_INVALID_ARG, "temperature must be finite and > 0");
   const double c = 1.4426950408889634 / l->temperature;
@@ -45,18 +50,24 @@ int check(const microadam_logits* l, LogprobArgs& a) {
   a.ignore_index = l->ignore_index;
   a.rows = l->rows;
   a.vocab = (int32_t)l->vocab;
+  a.group_rows = l->rows > 0 ? (int32_t)l->group_rows : 0;
+  a.group_stride = l->group_stride;
   a.c = (float)c;
   a.inv_t = (float)(1.0 / l->temperature);
   return MICROADAM_OK;
 }
 
-// Whether rows of `width` bytes, `stride` apart, starting at x and at g share
-// bytes: one stride, the places within it decide; two, the ranges do.
-bool share_bytes(const void* x, int64_t stride_x, const void* g, int64_t stride_g, int64_t rows, int64_t width) {
-  const uintptr_t a = (uintptr_t)x, b = (uintptr_t)g;
-  const uint64_t reach_x = (uint64_t)((rows - 1) * stride_x + width), reach_g = (uint64_t)((rows - 1) * stride_g + width);
+// Whether the rows of logits and gradient share bytes: rows at the same
+// stride, the places within it decide; else the ranges do.
+bool share_bytes(const LogprobArgs& l, const void* g, int64_t grad_ld, int64_t size) {
+  const uintptr_t a = (uintptr_t)l.logits, b = (uintptr_t)g;
+  const int64_t width = l.vocab * size, stride_x = l.ld * size, stride_g = grad_ld * size;
+  const int64_t inner = l.group_rows ? l.group_rows : l.rows;
+  const uint64_t reach_x =
+      (uint64_t)((l.rows / inner - 1) * l.group_stride * size + (inner - 1) * stride_x + width);
+  const uint64_t reach_g = (uint64_t)((l.rows - 1) * stride_g + width);
   if (a <= b ? b - a >= reach_x : a - b >= reach_g) return false;
-  if (rows == 1 || stride_x != stride_g) return true;
+  if (l.rows == 1 || l.group_rows || stride_x != stride_g) return true;
   const int64_t place = (int64_t)((a <= b ? b - a : a - b) % (uint64_t)stride_x);
   return place < width || place > stride_x - width;
 }
@@ -105,10 +116,10 @@ int microadam_token_logprobs_grad(const microadam_logits* logits, const float* g
     if (grad_ld < logits->vocab && a.rows > 1)
       return report(MICROADAM_ERR_INVALID_ARG, "the gradient's row stride is below vocab");
     if (grad_ld > ((int64_t)1 << 40)) return report(MICROADAM_ERR_UNSUPPORTED, "the gradient's row stride is above 2^40");
-    if (grad == logits->data && grad_ld != logits->ld)
-      return report(MICROADAM_ERR_INVALID_ARG, "in place, the row strides must agree");
+    if (grad == logits->data && (grad_ld != logits->ld || a.group_rows))
+      return report(MICROADAM_ERR_INVALID_ARG, "in place, the rows must have one stride, the same one");
     const int64_t size = logits->dtype == MICROADAM_BF16 ? 2 : 4;
-    if (grad != logits->data && share_bytes(logits->data, logits->ld * size, grad, grad_ld * size, a.rows, a.vocab * size))
+    if (grad != logits->data && share_bytes(a, grad, grad_ld, size))
       return report(MICROADAM_ERR_INVALID_ARG, "the gradient overlaps the logits without being in place");
     if (!aligned4(grad_logp) || !aligned4(grad_entropy) || !aligned4(logp) || !aligned4(entropy) ||
         (uintptr_t)grad % (logits->dtype == MICROADAM_BF16 ? 2 : 4))

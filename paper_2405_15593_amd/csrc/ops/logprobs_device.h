@@ -12,10 +12,12 @@ struct LogprobArgs {
   const void* logits;
   const int64_t* targets;
   int64_t ld, grad_ld;  // elements
+  int64_t group_stride;        // of the logits; elements
   int64_t ignore_index;
   int64_t rows;
   int32_t vocab;
   int32_t top_k;
+  int32_t group_rows;          // 0: rows at one stride
   float c;              // log2(e) / temperature
   float inv_t;          // 1 / temperature
   float* logp;          // each of these may be NULL

@@ -9,7 +9,8 @@ known before the call, ``token_logprobs_and_grad`` gives the values and the
 gradient in one pass over the logits.
 
 Logits are float32 or bfloat16 on a ROCm device, (..., vocab) with contiguous
-rows at one stride; targets are int64 of the leading shape, with
+rows at one stride, or at two (``logits[:, :-1]`` of a batch of sequences);
+targets are int64 of the leading shape, with
 ``ignore_index`` for rows to leave out.  Work is queued on torch's current
 stream.
 """
@@ -40,8 +41,23 @@ class TokenLogprobsGrad(NamedTuple):
     grad: torch.Tensor                        # of the logits' shape and dtype
 
 
+def _joined(lead):
+    """Leading (size, stride) with neighbours joined where one stride serves
+    both; a single empty dimension if any is."""
+    if any(n == 0 for n, _ in lead):
+        return [(0, 0)]
+    out = [lead[0]]
+    for n, s in lead[1:]:
+        if out[-1][1] == n * s:
+            out[-1] = (out[-1][0] * n, s)
+        else:
+            out.append((n, s))
+    return out
+
+
 def _rows(logits: torch.Tensor, targets: torch.Tensor):
-    """(logits as [rows, vocab], their row stride, targets as [rows])."""
+    """(dtype code, address, rows, vocab, row stride, rows of a group or 0, stride
+    of groups, targets as [rows])."""
     code = _DTYPES.get(logits.dtype)
     if code is None:
         raise TypeError(f"logits: float32 or bfloat16, not {logits.dtype}")
@@ -54,14 +70,25 @@ def _rows(logits: torch.Tensor, targets: torch.Tensor):
     vocab = logits.shape[-1]
     if vocab > 1 and logits.stride(-1) != 1:
         raise ValueError("logits: contiguous rows")
-    flat = logits if logits.dim() == 2 else logits.flatten(0, -2) if logits.dim() > 2 else logits[None]
-    rows = flat.shape[0]
-    ld = flat.stride(0) if rows > 1 else max(1, vocab)
-    if flat.data_ptr() != logits.data_ptr() or (rows > 1 and ld < vocab):
-        raise ValueError("logits: rows at one stride, not overlapping")
+    lead = [(n, s) for n, s in zip(logits.shape[:-1], logits.stride()[:-1]) if n != 1] if logits.dim() != 2 else \
+        ((logits.shape[0], logits.stride(0)),)
+    if len(lead) > 1:
+        lead = _joined(lead)
+    rows, ld, group, group_stride = 1, max(1, vocab), 0, 0
+    if lead:
+        rows, stride = lead[-1]
+        if rows > 1:
+            ld = stride
+            if ld < vocab:
+                raise ValueError("logits: rows must not overlap")
+        if len(lead) == 2 and rows:
+            group, group_stride = rows, lead[0][1]
+            rows *= lead[0][0]
+        elif len(lead) > 1:
+            raise ValueError("logits: rows at one stride, or in groups at a second")
     if targets.dim() != 1 or not targets.is_contiguous():
         targets = targets.reshape(-1).contiguous()
-    return code, flat, ld, targets
+    return code, logits.data_ptr(), rows, vocab, ld, group, group_stride, targets
 
 
 def _on(device):
@@ -69,15 +96,15 @@ def _on(device):
     return _HERE if device.index == torch.cuda.current_device() else torch.cuda.device(device)
 
 
-def _struct(code, flat, ld, targets, ignore_index, temperature):
-    rows, vocab = flat.shape
-    return microadam_logits(flat.data_ptr(), targets.data_ptr(), rows, vocab, ld, int(ignore_index),
-                            float(temperature), code, 0)
+def _struct(rows, ignore_index, temperature):
+    code, address, n, vocab, ld, group, group_stride, targets = rows
+    return microadam_logits(address, targets.data_ptr(), n, vocab, ld, int(ignore_index), float(temperature), code, 0,
+                            group, group_stride)
 
 
 def _values(logits, targets, top_k, temperature, ignore_index):
-    code, flat, ld, t = _rows(logits, targets)
-    lead, rows, dev = targets.shape, flat.shape[0], logits.device
+    given = _rows(logits, targets)
+    lead, rows, dev = targets.shape, given[2], logits.device
     values = torch.empty((2, rows), dtype=torch.float32, device=dev)
     logp, entropy = values[0], values[1]
     top_v = top_i = None
@@ -85,7 +112,7 @@ def _values(logits, targets, top_k, temperature, ignore_index):
         top_v = torch.empty((rows, top_k), dtype=torch.float32, device=dev)
         top_i = torch.empty((rows, top_k), dtype=torch.int64, device=dev)
     with _on(dev):
-        microadam_token_logprobs(_struct(code, flat, ld, t, ignore_index, temperature), int(top_k), logp.data_ptr(),
+        microadam_token_logprobs(_struct(given, ignore_index, temperature), int(top_k), logp.data_ptr(),
                                  entropy.data_ptr(), top_v.data_ptr() if top_k else None,
                                  top_i.data_ptr() if top_k else None, torch.cuda.current_stream(dev.index).cuda_stream)
     if top_k:
@@ -96,18 +123,18 @@ def _values(logits, targets, top_k, temperature, ignore_index):
     return TokenLogprobs(logp, entropy, top_v, top_i)
 
 
-def _grad_rows(flat: torch.Tensor, ld: int) -> torch.Tensor:
+def _grad_rows(logits: torch.Tensor, given) -> torch.Tensor:
     """[rows, vocab] for the gradient, whose rows start at the same place in 16
     bytes as the logits' rows: at most 15 bytes of a row and of the start are
     left unused, none where the logits are dense and start aligned."""
-    rows, vocab = flat.shape
-    size = flat.element_size()
+    _, address, rows, vocab, ld = given[:5]
+    size = logits.element_size()
     per = 16 // size
-    start = flat.data_ptr() % 16 // size
+    start = address % 16 // size
     gld = vocab + (ld - vocab) % per
     if not start and gld == vocab:
-        return torch.empty((rows, vocab), dtype=flat.dtype, device=flat.device)
-    store = torch.empty(start + rows * gld, dtype=flat.dtype, device=flat.device)
+        return torch.empty((rows, vocab), dtype=logits.dtype, device=logits.device)
+    store = torch.empty(start + rows * gld, dtype=logits.dtype, device=logits.device)
     return store.as_strided((rows, vocab), (gld, 1), start)
 
 
@@ -128,7 +155,7 @@ def token_logprobs_and_grad(logits: torch.Tensor, targets: torch.Tensor, grad_lo
     ``out``: where the gradient goes (``logits`` itself is allowed)."""
     if logits.requires_grad:
         logits = logits.detach()
-    code, flat, ld, t = _rows(logits, targets)
+    given = _rows(logits, targets)
     lead, dev = targets.shape, logits.device
     gp = _upstream(grad_logp, lead, "grad_logp")
     ge = None if grad_entropy is None else _upstream(grad_entropy, lead, "grad_entropy")
@@ -136,19 +163,22 @@ def token_logprobs_and_grad(logits: torch.Tensor, targets: torch.Tensor, grad_lo
         if g is not None and g.device != dev:
             raise ValueError("grad_logp and grad_entropy: the logits' device")
     if out is None:
-        grad = _grad_rows(flat, ld)
+        grad = _grad_rows(logits, given)
         gld, shaped = grad.stride(0), grad if logits.dim() == 2 else grad.view(logits.shape)
+        grad_address = grad.data_ptr()
     else:
         if out.shape != logits.shape or out.dtype != logits.dtype:
             raise ValueError("out: the logits' shape and dtype")
-        _, grad, gld, _ = _rows(out, targets)
+        _, grad_address, _, _, gld, group, _, _ = _rows(out, targets)
+        if group:
+            raise ValueError("out: rows at one stride")
         shaped = out
-    values = torch.empty((2, flat.shape[0]), dtype=torch.float32, device=dev)
+    values = torch.empty((2, given[2]), dtype=torch.float32, device=dev)
     logp, entropy = values[0], values[1]
     with _on(dev):
-        microadam_token_logprobs_grad(_struct(code, flat, ld, t, ignore_index, temperature), gp.data_ptr(),
+        microadam_token_logprobs_grad(_struct(given, ignore_index, temperature), gp.data_ptr(),
                                       None if ge is None else ge.data_ptr(), logp.data_ptr(), entropy.data_ptr(),
-                                      grad.data_ptr(), gld, torch.cuda.current_stream(dev.index).cuda_stream)
+                                      grad_address, gld, torch.cuda.current_stream(dev.index).cuda_stream)
     if len(lead) != 1:
         logp, entropy = logp.view(lead), entropy.view(lead)
     return TokenLogprobsGrad(logp, entropy, shaped)

@@ -231,6 +231,49 @@ def test_strides_starts_and_in_place(dtype):
     assert e.logp.shape == (0,) and e.top_indices.shape == (0, 2)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("vocab,pad", [(4000, 0), (4001, 0), (1003, 5), (70001, 0)])
+def test_rows_in_groups(vocab, pad, dtype):
+    """Views of a batch of sequences whose rows have no one stride."""
+    print(f"[logprobs] groups {vocab} + {pad} {dtype}", flush=True)
+    g = torch.Generator(device="cuda").manual_seed(vocab)
+    base = (torch.randn(3, 9, vocab + pad, generator=g, device="cuda") * 3).to(dtype)[:, :, :vocab]
+    for x in (base[:, :-1], base[:, 1:], base.transpose(0, 1), base[::2, ::3], base[:, None, :4], base[:2, 5:6]):
+        lead = x.shape[:-1]
+        t = torch.randint(0, vocab, lead, generator=g, device="cuda")
+        gp, gh = torch.randn(2, *lead, generator=g, device="cuda")
+        flat, ft = x.reshape(-1, vocab), t.reshape(-1)
+        check_values(flat, ft, 5)
+        r = token_logprobs(x, t, top_k=5)
+        lp, _, logp, h, _ = exact(flat, ft)
+        assert r.logp.shape == lead and close(r.logp.reshape(-1), logp) and close(r.entropy.reshape(-1), h)
+        order = torch.sort(flat.float(), dim=1, descending=True, stable=True).indices[:, :5]
+        assert torch.equal(r.top_indices.reshape(-1, 5), order)
+        assert close(r.top_logprobs.reshape(-1, 5), lp.gather(1, order))
+        out = torch.empty(x.shape, dtype=dtype, device="cuda")
+        want = exact_grad(flat, ft, gp.reshape(-1), gh.reshape(-1))
+        tol = 4e-5 * want.abs().amax(1, keepdim=True) + (want.abs() * 2 ** -8 if dtype == torch.bfloat16 else 0) + 1e-38
+        for z in (token_logprobs_and_grad(x, t, gp, gh), token_logprobs_and_grad(x, t, gp, gh, out=out)):
+            assert z.grad.shape == x.shape
+            assert bool(((z.grad.reshape(-1, vocab).double() - want).abs() <= tol).all())
+    # through autograd, the shift of a causal model's loss
+    leaf = base.clone().requires_grad_()
+    t = torch.randint(0, vocab, (3, 8), generator=g, device="cuda")
+    token_logprobs(leaf[:, :-1], t).logp.sum().backward()
+    assert bool((leaf.grad[:, -1] == 0).all())
+    want = exact_grad(base[:, :-1].reshape(-1, vocab), t.reshape(-1), torch.ones(24, device="cuda"), None)
+    tol = 4e-5 * want.abs().amax(1, keepdim=True) + (want.abs() * 2 ** -8 if dtype == torch.bfloat16 else 0) + 1e-38
+    assert bool(((leaf.grad[:, :-1].reshape(-1, vocab).double() - want).abs() <= tol).all())
+    x, t = base[:, :-1], t
+    with pytest.raises(ValueError):
+        token_logprobs_and_grad(x, t, torch.ones(3, 8, device="cuda"), out=x)   # in place takes one stride
+    with pytest.raises(ValueError):
+        token_logprobs(base[:, :, None].expand(3, 9, 2, vocab), torch.zeros(3, 9, 2, dtype=torch.int64, device="cuda"))
+    four = base.clone().view(3, 3, 3, vocab)[:, :2, :2]
+    with pytest.raises(ValueError):
+        token_logprobs(four, torch.zeros(3, 2, 2, dtype=torch.int64, device="cuda"))
+
+
 def test_rows_past_32_bits():
     """Row offsets above 2^31 elements."""
     print("[logprobs] long strides", flush=True)

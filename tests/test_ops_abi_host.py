@@ -203,6 +203,30 @@ def test_gradient_that_overlaps_the_logits(dtype, size):
             g(x, 256, None, 257, 256, at + off * size, ld)
 
 
+@pytest.mark.parametrize("kw,code", [(dict(group_rows=3, group_stride=400), INVALID),
+                                     (dict(group_rows=-2, group_stride=400), INVALID),
+                                     (dict(group_rows=2, group_stride=-1), INVALID),
+                                     (dict(group_rows=0, group_stride=400), INVALID),
+                                     (dict(group_rows=2, group_stride=1 << 41), UNSUPPORTED)], ids=str)
+def test_groups_of_rows(kw, code):
+    refused(code, ma.microadam_token_logprobs, logits(**kw), 0, 256, 256, None, None)
+    refused(code, ma.microadam_token_logprobs_grad, logits(**kw), 256, None, 256, 256, 65536, 1 << 26)
+
+
+def test_a_gradient_among_groups():
+    """Rows in groups: no gradient in place, nor where the groups reach."""
+    g = ma.microadam_token_logprobs_grad
+    at = 1 << 20
+    x = logits(data=at, group_rows=2, group_stride=300)
+    refused(INVALID, g, x, 256, None, 256, 256, at, 100)
+    for off in (1, 250, 499, -1, -399):
+        with pytest.raises(ma.MicroAdamError, match="overlaps"):
+            g(x, 256, None, 256, 256, at + off * 4, 100)
+    for off in (500, -400):
+        with pytest.raises(ma.MicroAdamError, match="an argument is not aligned"):
+            g(x, 256, None, 257, 256, at + off * 4, 100)
+
+
 def test_a_matrix_twice():
     a = dict(grad=4096, momentum=None, out=8192, rows=8, cols=16, grad_ld=16, momentum_ld=0, out_ld=16)
     twice = matrices(tuple(a.values()), tuple(dict(a, grad=1 << 16).values()))
