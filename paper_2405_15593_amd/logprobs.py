@@ -20,6 +20,7 @@ import contextlib
 from typing import NamedTuple, Optional
 
 import torch
+from torch.autograd.graph import increment_version
 
 from . import (MICROADAM_BF16, MICROADAM_F32, microadam_logits, microadam_token_logprobs,
                microadam_token_logprobs_grad)
@@ -152,7 +153,9 @@ def token_logprobs_and_grad(logits: torch.Tensor, targets: torch.Tensor, grad_lo
     """Log probabilities, entropies and, in the same pass, the gradient with
     respect to the logits of sum(grad_logp * logp + grad_entropy * entropy).
     For the mean negative log likelihood of n tokens, grad_logp is -1/n.
-    ``out``: where the gradient goes (``logits`` itself is allowed)."""
+    ``out``: where the gradient goes (``logits`` itself is allowed; autograd
+    sees the write as one in place, so a backward that saved what was there
+    raises)."""
     if logits.requires_grad:
         logits = logits.detach()
     given = _rows(logits, targets)
@@ -169,6 +172,8 @@ def token_logprobs_and_grad(logits: torch.Tensor, targets: torch.Tensor, grad_lo
     else:
         if out.shape != logits.shape or out.dtype != logits.dtype:
             raise ValueError("out: the logits' shape and dtype")
+        if torch.is_grad_enabled() and out.requires_grad and (out if out._base is None else out._base).is_leaf:
+            raise ValueError("out: a leaf that requires grad, or a view of one")
         _, grad_address, _, _, gld, group, _, _ = _rows(out, targets)
         if group:
             raise ValueError("out: rows at one stride")
@@ -179,6 +184,8 @@ def token_logprobs_and_grad(logits: torch.Tensor, targets: torch.Tensor, grad_lo
         microadam_token_logprobs_grad(_struct(given, ignore_index, temperature), gp.data_ptr(),
                                       None if ge is None else ge.data_ptr(), logp.data_ptr(), entropy.data_ptr(),
                                       grad_address, gld, torch.cuda.current_stream(dev.index).cuda_stream)
+    if out is not None:
+        increment_version(out)
     if len(lead) != 1:
         logp, entropy = logp.view(lead), entropy.view(lead)
     return TokenLogprobsGrad(logp, entropy, shaped)

@@ -17,6 +17,7 @@ from __future__ import annotations
 import contextlib
 
 import torch
+from torch.autograd.graph import increment_version
 
 from . import (MICROADAM_BF16, MICROADAM_F32, MICROADAM_PRECISION_AUTO, MICROADAM_PRECISION_F16,
                MICROADAM_PRECISION_SPLIT, MICROADAM_SCALE_MATCH_RMS, MICROADAM_SCALE_NONE, MICROADAM_SCALE_SPECTRAL,
@@ -104,8 +105,8 @@ def orthogonalize(grad: torch.Tensor, *, steps: int = 5, coefficients=None, eps:
                   precision: str = "auto", out: torch.Tensor | None = None,
                   workspace: torch.Tensor | None = None) -> torch.Tensor:
     """The orthogonalised matrix (or stack of matrices) of `grad`, in `out` if
-    given (float32 or bfloat16; `grad` itself is allowed), else in a new tensor
-    of grad's dtype."""
+    given (float32 or bfloat16; `grad` itself is allowed; autograd sees a write
+    in place), else in a new tensor of grad's dtype."""
     cfg = _schulz(steps, coefficients, eps, precision)
     gcode = _code(grad, "grad")
     if not grad.is_cuda:
@@ -114,6 +115,8 @@ def orthogonalize(grad: torch.Tensor, *, steps: int = 5, coefficients=None, eps:
         out = torch.empty(grad.shape, dtype=grad.dtype, device=grad.device)
     elif out.shape != grad.shape or out.device != grad.device:
         raise ValueError("out: grad's shape and device")
+    elif out.requires_grad and torch.is_grad_enabled():
+        raise ValueError("out: a tensor that requires grad")
     ocode = _code(out, "out")
     g, o = _matrices(grad, "grad", written=False), _matrices(out, "out")
     if grad.numel() == 0:
@@ -124,6 +127,7 @@ def orthogonalize(grad: torch.Tensor, *, steps: int = 5, coefficients=None, eps:
         ptr, size, keep = _workspace(cfg, array, len(g), ocode, grad.device, workspace)
         microadam_orthogonalize(cfg, array, len(g), gcode, ocode, ptr, size,
                                 torch.cuda.current_stream(grad.device.index).cuda_stream)
+    increment_version(out)
     return out
 
 
@@ -132,7 +136,9 @@ def muon_step(params, grads, momenta, *, lr: float, momentum: float = 0.95, nest
               eps: float = 1e-7, precision: str = "auto", workspace: torch.Tensor | None = None) -> None:
     """One Muon step: `params` and `momenta` (zeros before the first step) are
     updated in place from `grads`.  Three lists of equal length and shapes;
-    one dtype per list."""
+    one dtype per list.  Like an optimizer's step it is not recorded for
+    autograd, whether the parameters require grad or not; a backward that saved
+    what a parameter was before raises."""
     params, grads, momenta = list(params), list(grads), list(momenta)
     if not params or not len(params) == len(grads) == len(momenta):
         raise ValueError("params, grads and momenta: three lists of equal length")
@@ -169,6 +175,8 @@ def muon_step(params, grads, momenta, *, lr: float, momentum: float = 0.95, nest
         ptr, size, keep = _workspace(cfg.schulz, array, len(rows), codes[2], device, workspace)
         microadam_muon_step(cfg, array, len(rows), *codes, lr, ptr, size,
                             torch.cuda.current_stream(device.index).cuda_stream)
+    increment_version(params)
+    increment_version(momenta)
 
 
 class Muon(torch.optim.Optimizer):
