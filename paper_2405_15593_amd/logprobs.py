@@ -24,6 +24,7 @@ from torch.autograd.graph import increment_version
 
 from . import (MICROADAM_BF16, MICROADAM_F32, microadam_logits, microadam_token_logprobs,
                microadam_token_logprobs_grad)
+from ._autograd import refuse_tangents
 
 _HERE = contextlib.nullcontext()
 _DTYPES = {torch.float32: MICROADAM_F32, torch.bfloat16: MICROADAM_BF16}
@@ -156,6 +157,7 @@ def token_logprobs_and_grad(logits: torch.Tensor, targets: torch.Tensor, grad_lo
     ``out``: where the gradient goes (``logits`` itself is allowed; autograd
     sees the write as one in place, so a backward that saved what was there
     raises)."""
+    refuse_tangents("token_logprobs_and_grad", (logits, grad_logp, grad_entropy, out))
     if logits.requires_grad:
         logits = logits.detach()
     given = _rows(logits, targets)
@@ -221,7 +223,8 @@ def token_logprobs(logits: torch.Tensor, targets: torch.Tensor, *, top_k: int = 
     of the distribution and, with ``top_k`` > 0 (at most 64), the ``top_k`` most
     probable tokens with their log probabilities, ties to the lowest index.
     Ignored rows give zeros (alternatives 0 and -1) and no gradient.  The
-    alternatives carry no gradient."""
+    alternatives carry no gradient, and there is no derivative in forward mode."""
+    refuse_tangents("token_logprobs", (logits,))
     if torch.is_grad_enabled() and logits.requires_grad:
         return TokenLogprobs(*_TokenLogprobs.apply(logits, targets, top_k, temperature, ignore_index))
     return _values(logits, targets, top_k, temperature, ignore_index)

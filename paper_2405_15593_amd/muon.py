@@ -23,6 +23,7 @@ from . import (MICROADAM_BF16, MICROADAM_F32, MICROADAM_PRECISION_AUTO, MICROADA
                MICROADAM_PRECISION_SPLIT, MICROADAM_SCALE_MATCH_RMS, MICROADAM_SCALE_NONE, MICROADAM_SCALE_SPECTRAL,
                make_schulz_config, microadam_matrix, microadam_matrix_workspace, microadam_muon_config,
                microadam_muon_step, microadam_orthogonalize)
+from ._autograd import refuse_tangents
 
 _DTYPES = {torch.float32: MICROADAM_F32, torch.bfloat16: MICROADAM_BF16}
 _PRECISIONS = {"auto": MICROADAM_PRECISION_AUTO, "f16": MICROADAM_PRECISION_F16, "split": MICROADAM_PRECISION_SPLIT}
@@ -107,6 +108,7 @@ def orthogonalize(grad: torch.Tensor, *, steps: int = 5, coefficients=None, eps:
     """The orthogonalised matrix (or stack of matrices) of `grad`, in `out` if
     given (float32 or bfloat16; `grad` itself is allowed; autograd sees a write
     in place), else in a new tensor of grad's dtype."""
+    refuse_tangents("orthogonalize", (grad, out))
     cfg = _schulz(steps, coefficients, eps, precision)
     gcode = _code(grad, "grad")
     if not grad.is_cuda:
@@ -142,6 +144,7 @@ def muon_step(params, grads, momenta, *, lr: float, momentum: float = 0.95, nest
     params, grads, momenta = list(params), list(grads), list(momenta)
     if not params or not len(params) == len(grads) == len(momenta):
         raise ValueError("params, grads and momenta: three lists of equal length")
+    refuse_tangents("muon_step", params + grads + momenta)
     if scale not in _SCALES:
         raise ValueError(f"scale must be one of {sorted(_SCALES)}")
     cfg = microadam_muon_config(_schulz(steps, coefficients, eps, precision), float(momentum), float(weight_decay),

@@ -3,6 +3,7 @@ are seen by it, derivatives that they do not have are refused, and their
 outputs are tensors of their own."""
 import pytest
 import torch
+import torch.autograd.forward_ad as forward_ad
 
 import paper_2405_15593_amd as ma
 from paper_2405_15593_amd.logprobs import token_logprobs, token_logprobs_and_grad
@@ -113,3 +114,27 @@ def test_backward_after_the_step():
     opt.step()
     with pytest.raises(RuntimeError, match=CHANGED):
         loss.backward()
+
+
+def test_tangents_are_refused():
+    """No derivative in forward mode: an error, not a result without a tangent."""
+    print("[autograd] tangents", flush=True)
+    x, t, gp = rows()
+    with forward_ad.dual_level():
+        dual = forward_ad.make_dual(x, torch.ones_like(x))
+        dual_gp = forward_ad.make_dual(gp, torch.ones_like(gp))
+        calls = (lambda: token_logprobs(dual, t, top_k=2), lambda: token_logprobs_and_grad(dual, t, gp),
+                 lambda: token_logprobs_and_grad(x, t, dual_gp), lambda: token_logprobs_and_grad(x, t, gp, dual_gp),
+                 lambda: token_logprobs_and_grad(x, t, gp, out=dual), lambda: orthogonalize(dual),
+                 lambda: orthogonalize(x, out=dual), lambda: muon_step([dual], [x], [gp], lr=0.1),
+                 lambda: muon_step([x.clone()], [dual], [torch.zeros_like(x)], lr=0.1))
+        for call in calls:
+            with pytest.raises(NotImplementedError, match="forward mode"):
+                call()
+        with torch.no_grad(), pytest.raises(NotImplementedError, match="forward mode"):
+            token_logprobs(dual, t)
+        # others in the same level go on
+        plain = token_logprobs(x, t)
+    assert torch.equal(plain.logp, token_logprobs(x, t).logp)
+    with pytest.raises(RuntimeError):
+        torch.func.jvp(lambda z: token_logprobs(z, t).logp, (x,), (x,))
