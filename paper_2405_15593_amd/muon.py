@@ -107,12 +107,15 @@ def orthogonalize(grad: torch.Tensor, *, steps: int = 5, coefficients=None, eps:
                   workspace: torch.Tensor | None = None) -> torch.Tensor:
     """The orthogonalised matrix (or stack of matrices) of `grad`, in `out` if
     given (float32 or bfloat16; `grad` itself is allowed; autograd sees a write
-    in place), else in a new tensor of grad's dtype."""
+    in place), else in a new tensor of grad's dtype.  It has no derivative:
+    detach a tensor that requires grad."""
     refuse_tangents("orthogonalize", (grad, out))
     cfg = _schulz(steps, coefficients, eps, precision)
     gcode = _code(grad, "grad")
     if not grad.is_cuda:
         raise ValueError("grad: a tensor on a ROCm device")
+    if grad.requires_grad and torch.is_grad_enabled():
+        raise NotImplementedError("orthogonalize: no derivative; grad requires grad")
     if out is None:
         out = torch.empty(grad.shape, dtype=grad.dtype, device=grad.device)
     elif out.shape != grad.shape or out.device != grad.device:

@@ -138,3 +138,19 @@ def test_tangents_are_refused():
     assert torch.equal(plain.logp, token_logprobs(x, t).logp)
     with pytest.raises(RuntimeError):
         torch.func.jvp(lambda z: token_logprobs(z, t).logp, (x,), (x,))
+
+
+def test_orthogonalize_has_no_derivative():
+    """A tensor that requires grad is refused where its graph would be lost."""
+    print("[autograd] orthogonalize", flush=True)
+    x = rows()[0]
+    leaf = x.clone().requires_grad_()
+    for t in (leaf, leaf * 2.0):
+        with pytest.raises(NotImplementedError, match="no derivative"):
+            orthogonalize(t)
+        with torch.no_grad():
+            orthogonalize(t)
+    assert torch.equal(orthogonalize(leaf.detach()), orthogonalize(x))
+    # a step is not recorded
+    muon_step([leaf], [x.clone().requires_grad_()], [torch.zeros_like(x)], lr=0.1)
+    assert leaf.is_leaf and not torch.equal(leaf, x)
