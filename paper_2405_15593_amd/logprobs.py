@@ -106,22 +106,19 @@ def _struct(rows, ignore_index, temperature):
 
 def _values(logits, targets, top_k, temperature, ignore_index):
     given = _rows(logits, targets)
-    lead, rows, dev = targets.shape, given[2], logits.device
-    values = torch.empty((2, rows), dtype=torch.float32, device=dev)
-    logp, entropy = values[0], values[1]
+    lead, dev = targets.shape, logits.device
+    # tensors of their own, no views: what the autograd function returns may be
+    # changed in place
+    logp = torch.empty(lead, dtype=torch.float32, device=dev)
+    entropy = torch.empty(lead, dtype=torch.float32, device=dev)
     top_v = top_i = None
     if top_k:
-        top_v = torch.empty((rows, top_k), dtype=torch.float32, device=dev)
-        top_i = torch.empty((rows, top_k), dtype=torch.int64, device=dev)
+        top_v = torch.empty((*lead, top_k), dtype=torch.float32, device=dev)
+        top_i = torch.empty((*lead, top_k), dtype=torch.int64, device=dev)
     with _on(dev):
         microadam_token_logprobs(_struct(given, ignore_index, temperature), int(top_k), logp.data_ptr(),
                                  entropy.data_ptr(), top_v.data_ptr() if top_k else None,
                                  top_i.data_ptr() if top_k else None, torch.cuda.current_stream(dev.index).cuda_stream)
-    if top_k:
-        if len(lead) != 1:
-            top_v, top_i = top_v.view(*lead, top_k), top_i.view(*lead, top_k)
-    if len(lead) != 1:
-        logp, entropy = logp.view(lead), entropy.view(lead)
     return TokenLogprobs(logp, entropy, top_v, top_i)
 
 
@@ -180,16 +177,14 @@ def token_logprobs_and_grad(logits: torch.Tensor, targets: torch.Tensor, grad_lo
         if group:
             raise ValueError("out: rows at one stride")
         shaped = out
-    values = torch.empty((2, given[2]), dtype=torch.float32, device=dev)
-    logp, entropy = values[0], values[1]
+    logp = torch.empty(lead, dtype=torch.float32, device=dev)
+    entropy = torch.empty(lead, dtype=torch.float32, device=dev)
     with _on(dev):
         microadam_token_logprobs_grad(_struct(given, ignore_index, temperature), gp.data_ptr(),
                                       None if ge is None else ge.data_ptr(), logp.data_ptr(), entropy.data_ptr(),
                                       grad_address, gld, torch.cuda.current_stream(dev.index).cuda_stream)
     if out is not None:
         increment_version(out)
-    if len(lead) != 1:
-        logp, entropy = logp.view(lead), entropy.view(lead)
     return TokenLogprobsGrad(logp, entropy, shaped)
 
 

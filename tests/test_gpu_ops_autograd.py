@@ -154,3 +154,44 @@ def test_orthogonalize_has_no_derivative():
     # a step is not recorded
     muon_step([leaf], [x.clone().requires_grad_()], [torch.zeros_like(x)], lr=0.1)
     assert leaf.is_leaf and not torch.equal(leaf, x)
+
+
+@pytest.mark.parametrize("lead", [(), (6,), (2, 3)], ids=str)
+def test_outputs_are_tensors_of_their_own(lead):
+    """Each can be changed in place without touching the others' backward."""
+    print(f"[autograd] outputs {lead}", flush=True)
+    x, t, _ = rows()
+    n = 6 if lead else 1
+    x, t = x[:n].reshape(*lead, 101), t[:n].reshape(lead)
+    keep = torch.arange(n, device="cuda").reshape(lead) % 2 == 0
+
+    def grad(change):
+        leaf = x.clone().requires_grad_()
+        r = token_logprobs(leaf, t, top_k=2)
+        change(r)
+        return leaf.grad
+
+    def in_place(r):
+        r.logp.masked_fill_(~keep, 0.0).mul_(3.0)
+        r.entropy.add_(r.logp.detach())
+        r.top_logprobs.exp_()
+        r.top_indices.add_(1)
+        (r.logp.sum() + r.entropy.sum()).backward()
+
+    def plain(r):
+        ((r.logp * keep).sum() * 3.0 + r.entropy.sum()).backward()
+
+    assert torch.equal(grad(in_place), grad(plain))
+
+    def saved(r):
+        loss = r.logp.square().sum()      # saves logp
+        with torch.no_grad():
+            r.entropy.mul_(2.0)
+            r.top_logprobs.zero_()
+        loss.backward()
+
+    assert torch.equal(grad(saved), grad(lambda r: r.logp.square().sum().backward()))
+    g = token_logprobs_and_grad(x, t, torch.ones(lead, device="cuda"))
+    version = g.logp._version
+    g.entropy.mul_(2.0)
+    assert g.logp._version == version and g.logp.shape == g.entropy.shape == lead
