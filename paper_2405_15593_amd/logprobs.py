@@ -104,13 +104,17 @@ def _struct(rows, ignore_index, temperature):
                             group, group_stride)
 
 
+def _outputs(targets):
+    """logp and entropy: tensors of their own, no views, since what the autograd
+    function returns may be changed in place."""
+    return (torch.empty_like(targets, dtype=torch.float32, memory_format=torch.contiguous_format),
+            torch.empty_like(targets, dtype=torch.float32, memory_format=torch.contiguous_format))
+
+
 def _values(logits, targets, top_k, temperature, ignore_index):
     given = _rows(logits, targets)
     lead, dev = targets.shape, logits.device
-    # tensors of their own, no views: what the autograd function returns may be
-    # changed in place
-    logp = torch.empty(lead, dtype=torch.float32, device=dev)
-    entropy = torch.empty(lead, dtype=torch.float32, device=dev)
+    logp, entropy = _outputs(targets)
     top_v = top_i = None
     if top_k:
         top_v = torch.empty((*lead, top_k), dtype=torch.float32, device=dev)
@@ -177,8 +181,7 @@ def token_logprobs_and_grad(logits: torch.Tensor, targets: torch.Tensor, grad_lo
         if group:
             raise ValueError("out: rows at one stride")
         shaped = out
-    logp = torch.empty(lead, dtype=torch.float32, device=dev)
-    entropy = torch.empty(lead, dtype=torch.float32, device=dev)
+    logp, entropy = _outputs(targets)
     with _on(dev):
         microadam_token_logprobs_grad(_struct(given, ignore_index, temperature), gp.data_ptr(),
                                       None if ge is None else ge.data_ptr(), logp.data_ptr(), entropy.data_ptr(),
