@@ -365,8 +365,8 @@ typedef struct microadam_schulz_config {
  * that start at multiples of 16 bytes are read and written in vectors.
  *   grad      read only.
  *   momentum  updated in place (microadam_muon_step; else NULL).
- *   out       microadam_orthogonalize: the result, which may be grad itself
- *             when dtypes and strides agree; microadam_muon_step: the
+ *   out       microadam_orthogonalize: the result, which may lie where grad
+ *             does (grad has been read by then); microadam_muon_step: the
  *             parameter, updated in place.
  * At most 2^20 rows and columns and 2^33 elements.
  */
@@ -400,8 +400,8 @@ int microadam_matrix_workspace(const microadam_schulz_config* cfg, const microad
  * until the queued work is done.  The same list in a workspace of the same size
  * gives the same bits (batches of other matrices may be summed in another
  * order).
- * Outputs must not overlap each other, nor any grad but their own; one address
- * twice is refused.
+ * Outputs must not share bytes with each other, nor with any grad but their own
+ * (interleaved rows do not): such a list is refused.
  * A matrix that holds NaN or an infinity gives NaN throughout; the others of
  * the list are not touched by it.
  */
@@ -418,8 +418,9 @@ int microadam_orthogonalize(const microadam_schulz_config* cfg, const microadam_
  * mean square of an Adam update, so that Adam's learning rates carry over),
  * sqrt(max(1, rows / cols)) for MICROADAM_SCALE_SPECTRAL and 1 for
  * MICROADAM_SCALE_NONE.  V starts as zeros, which the caller provides.
- * Workspace, order and non-finite values as for microadam_orthogonalize.  The
- * matrices of one list must not overlap, and none is in it twice.
+ * Workspace, order and non-finite values as for microadam_orthogonalize.  A
+ * parameter or momentum must not share bytes with anything else of the list,
+ * but for a parameter and its own grad: such a list is refused.
  */
 enum { MICROADAM_SCALE_MATCH_RMS = 0, MICROADAM_SCALE_SPECTRAL = 1, MICROADAM_SCALE_NONE = 2 };
 

@@ -71,14 +71,87 @@ int check_operand(const void* p, int64_t ld, int64_t cols, int32_t dtype, const 
   return MICROADAM_OK;
 }
 
-// What is written must not be in the list twice: its tiles would race.
-int check_once(const microadam_matrix* mats, int32_t n, bool momentum) {
-  std::vector<uintptr_t> at((size_t)n);
-  for (int pass = 0; pass < (momentum ? 2 : 1); ++pass) {
-    for (int32_t i = 0; i < n; ++i) at[i] = (uintptr_t)(pass ? mats[i].momentum : mats[i].out);
-    std::sort(at.begin(), at.end());
-    if (std::adjacent_find(at.begin(), at.end()) != at.end())
-      return report(MICROADAM_ERR_INVALID_ARG, pass ? "a momentum is in the list twice" : "an output is in the list twice");
+// The bytes of a matrix: rows of `width` at `stride` (at least width).
+struct Region {
+  uint64_t at, end, width, stride;
+  int64_t rows;
+  int32_t matrix;
+  enum Kind : int32_t { kGrad, kMomentum, kOut } kind;
+};
+
+Region region(const void* p, const microadam_matrix& a, int64_t ld, int32_t dtype, int32_t matrix,
+              Region::Kind kind) {
+  const uint64_t size = dtype == MICROADAM_BF16 ? 2 : 4;
+  Region r;
+  r.at = (uint64_t)(uintptr_t)p;
+  r.rows = a.rows;
+  r.width = (uint64_t)a.cols * size;
+  r.stride = (uint64_t)ld * size;
+  if (r.rows == 1 || r.width == r.stride) {  // one run of bytes
+    r.width = r.stride = r.width * (uint64_t)r.rows;
+    r.rows = 1;
+  }
+  r.end = r.at + (uint64_t)(r.rows - 1) * r.stride + r.width;
+  r.matrix = matrix;
+  r.kind = kind;
+  return r;
+}
+
+// Whether [from, to) holds a byte of one of r's rows.
+bool holds(const Region& r, uint64_t from, uint64_t to) {
+  if (from >= r.end || to <= r.at) return false;
+  // the first row that ends after `from`
+  const uint64_t row = from < r.at + r.width ? 0 : (from - r.at - r.width) / r.stride + 1;
+  return r.at + row * r.stride < to;
+}
+
+bool share_bytes(const Region& a, const Region& b) {
+  if (a.at >= b.end || b.at >= a.end) return false;
+  if (a.rows > 1 && b.rows > 1 && a.stride == b.stride) {
+    // row i of the first and row i + k of the second are `apart` + k * stride
+    // from each other, so that only the two k around 0 matter
+    const Region &x = a.at <= b.at ? a : b, &y = a.at <= b.at ? b : a;
+    const uint64_t apart = y.at - x.at, place = apart % x.stride;
+    const int64_t rows = (int64_t)(apart / x.stride);  // of x before y's first
+    return (place < x.width && rows < x.rows) || (place + y.width > x.stride && rows + 1 < x.rows);
+  }
+  const Region &few = a.rows <= b.rows ? a : b, &many = a.rows <= b.rows ? b : a;
+  for (int64_t i = 0; i < few.rows; ++i) {
+    const uint64_t from = few.at + (uint64_t)i * few.stride;
+    if (holds(many, from, from + few.width)) return true;
+  }
+  return false;
+}
+
+// What is written shares no byte with anything else of the list: tiles would
+// race, and whether a grad is read before it is overwritten would go by the
+// batch.  Only a matrix's own grad, which its last product comes after, may lie
+// where its output goes.
+int check_apart(const microadam_matrix* mats, int32_t n, int32_t grad_dtype, int32_t momentum_dtype, int32_t out_dtype,
+                bool momentum) {
+  std::vector<Region> all;
+  all.reserve((size_t)n * (momentum ? 3 : 2));
+  for (int32_t i = 0; i < n; ++i) {
+    const microadam_matrix& a = mats[i];
+    all.push_back(region(a.grad, a, a.grad_ld, grad_dtype, i, Region::kGrad));
+    if (momentum) all.push_back(region(a.momentum, a, a.momentum_ld, momentum_dtype, i, Region::kMomentum));
+    all.push_back(region(a.out, a, a.out_ld, out_dtype, i, Region::kOut));
+  }
+  std::sort(all.begin(), all.end(), [](const Region& a, const Region& b) { return a.at < b.at; });
+  std::vector<const Region*> open;  // those that end after the current one starts
+  for (const Region& r : all) {
+    size_t kept = 0;
+    for (const Region* o : open) {
+      if (o->end <= r.at) continue;
+      open[kept++] = o;
+      if (r.kind == Region::kGrad && o->kind == Region::kGrad) continue;
+      if (r.matrix == o->matrix && r.kind != Region::kMomentum && o->kind != Region::kMomentum) continue;
+      if (share_bytes(r, *o))
+        return report(MICROADAM_ERR_INVALID_ARG,
+                      "an output or momentum overlaps another of the list, or a grad that is not its own");
+    }
+    open.resize(kept);
+    open.push_back(&r);
   }
   return MICROADAM_OK;
 }
@@ -208,14 +281,14 @@ int make_items(const microadam_matrix* mats, int32_t n, std::vector<Item>& items
 int run(const Call& c, int32_t n, void* workspace, uint64_t workspace_bytes, hipStream_t s) {
   std::vector<Item> items;
   make_items(c.mats, n, items);
-  if (!workspace) return report(MICROADAM_ERR_INVALID_ARG, "workspace is NULL");
-  if ((uintptr_t)workspace % kAlign) return report(MICROADAM_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
   const bool split = use_split(c.cfg, c.out_dtype);
   for (const Item& it : items)
     if (kPartialBytes + group_of(it.m, it.n, split).record > workspace_bytes)
       return report(MICROADAM_ERR_STATE_SIZE, "workspace smaller than microadam_matrix_workspace's minimum");
-  const int twice = check_once(c.mats, n, c.momentum);
-  if (twice) return twice;
+  const int shared = check_apart(c.mats, n, c.grad_dtype, c.momentum_dtype, c.out_dtype, c.momentum);
+  if (shared) return shared;
+  if (!workspace) return report(MICROADAM_ERR_INVALID_ARG, "workspace is NULL");
+  if ((uintptr_t)workspace % kAlign) return report(MICROADAM_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
   int32_t begin = 0;
   while (begin < n) {
     uint64_t bytes = kPartialBytes;
