@@ -53,20 +53,17 @@ def _schulz(steps, coefficients, eps, precision):
 
 
 def _matrices(t: torch.Tensor, what: str, written: bool = True) -> list:
-    """(address, row stride) of each matrix of `t`; what is written must not
-    overlap itself."""
+    """(address, row stride) of each matrix of `t`.  Matrices that are written
+    may lie between each other's rows, but not on each other: the library
+    decides that for the whole list."""
     if t.dim() < 2:
         raise ValueError(f"{what}: a matrix or a stack of matrices, not {t.dim()} dimensions")
     r, c = t.shape[-2:]
     if (c > 1 and t.stride(-1) != 1) or (r > 1 and t.stride(-2) < c):
         raise ValueError(f"{what}: rows must be contiguous and not overlap")
     ld = t.stride(-2) if r > 1 else c
-    if written and t.dim() > 2:
-        reach = (r - 1) * ld + c
-        for stride, n in sorted((s, n) for s, n in zip(t.stride()[:-2], t.shape[:-2]) if n > 1):
-            if stride < reach:
-                raise ValueError(f"{what}: matrices of a stack must not overlap")
-            reach += (n - 1) * stride
+    if written and any(s == 0 and n > 1 for s, n in zip(t.stride()[:-2], t.shape[:-2])):
+        raise ValueError(f"{what}: one matrix more than once in a stack")
     base, size = t.data_ptr(), t.element_size()
     if t.dim() == 2:
         return [(base, ld)]
