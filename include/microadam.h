@@ -446,7 +446,7 @@ int microadam_muon_step(const microadam_muon_config* cfg, const microadam_matrix
  * sequences, say.  With z = x / temperature, lp_v = z_v - log sum exp z and
  * p = exp lp:
  *     logp = lp at the row's token,   entropy = -sum p lp  (0 where p = 0),
- * all sums in binary32, each exponent taken from the row's maximum.  vocab is
+ * all sums in binary32 or more, each exponent taken from the row's maximum.  vocab is
  * at most 2^24, rows at most 2^20; addresses are aligned to their element
  * type (rows may start anywhere; 16 bytes at a time are read either way).
  *   - A row whose token is ignore_index is not read: logp and entropy 0,

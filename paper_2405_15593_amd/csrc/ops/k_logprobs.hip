@@ -80,6 +80,18 @@ struct Sums {
   float m, s, w;  // maximum of x, sum of 2^d2, sum of 2^d2 d2
 };
 
+// What a thread adds up over the segments of a row, of which 2^24 logits have
+// up to 2048: in binary32 the chain's rounding, one way where the terms are
+// alike, reached 5e-4 of log s.
+template <bool MULTI>
+struct Running {
+  typedef float type;
+};
+template <>
+struct Running<true> {
+  typedef double type;
+};
+
 // The sums of x's against `from` taken against the larger maximum `to`.
 __device__ inline void rebase(Sums& a, float to, float c) {
   const float delta = (a.m - to) * c;
@@ -211,6 +223,8 @@ __global__ __launch_bounds__(kMaxThreads) void row_kernel(const LogprobArgs a) {
     t.s = exp2_fast(d);
     t.w = t.s * fmaxf(d, -1000.0f);
   }
+  typedef typename Running<MULTI>::type Wide;
+  Wide all_s = t.s, all_w = t.w;  // of the segments before
   for (int seg = 0; seg < segments; ++seg) {
     load(seg);
     float m = t.m;
@@ -218,7 +232,16 @@ __global__ __launch_bounds__(kMaxThreads) void row_kernel(const LogprobArgs a) {
     for (int i = 0; i < NV; ++i)
 #pragma unroll
       for (int e = 0; e < E; ++e) m = fmaxf(m, r[i].get(e));
-    rebase(t, m, a.c);
+    if constexpr (MULTI) {
+      if (m != t.m) {
+        const float delta = (t.m - m) * a.c, f = exp2_fast(delta);
+        all_w = f * (all_w + fmaxf(delta, -1000.0f) * all_s);
+        all_s *= f;
+      }
+      t = {m, 0.0f, 0.0f};
+    } else {
+      rebase(t, m, a.c);
+    }
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
@@ -228,6 +251,14 @@ __global__ __launch_bounds__(kMaxThreads) void row_kernel(const LogprobArgs a) {
         t.s += p;
         t.w = __builtin_fmaf(p, fmaxf(d, -1000.0f), t.w);
       }
+    if constexpr (MULTI) {
+      all_s += t.s;
+      all_w += t.w;
+    }
+  }
+  if constexpr (MULTI) {
+    t.s = (float)all_s;
+    t.w = (float)all_w;
   }
   const float thread_max = t.m;
   const bool known = target >= 0 && target < V;
@@ -259,7 +290,7 @@ __global__ __launch_bounds__(kMaxThreads) void row_kernel(const LogprobArgs a) {
     if (holds) {
       const int owner = __ffsll((unsigned long long)holds) - 1;
       auto other = [&](float v) { return v < t.m ? exp2_fast((v - t.m) * a.c) : 0.0f; };
-      float sum = lane == owner ? other(xe) : lane_s;
+      Wide wide = lane == owner ? other(xe) : lane_s;
       for (int seg = 0; seg < segments; ++seg) {
         if (MULTI) load(seg);
         if (lane == owner) {
@@ -274,11 +305,12 @@ __global__ __launch_bounds__(kMaxThreads) void row_kernel(const LogprobArgs a) {
           float v = one.get(0);
 #pragma unroll
           for (int e = 1; e < E; ++e) v = i % E == e ? one.get(e) : v;
-          sum += other(v);
+          wide += other(v);
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
       }
+      float sum = (float)wide;
 #pragma unroll
       for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
       if (lane == 0) sh.rest = sum;
