@@ -457,7 +457,7 @@ int microadam_muon_step(const microadam_muon_config* cfg, const microadam_matrix
  *   - A row with NaN or +inf: logp, entropy and gradient NaN, alternatives NaN
  *     and -1.
  *   - A token outside [0, vocab) that is not ignore_index: logp NaN, gradient
- *     NaN (nothing outside the row is read).
+ *     NaN, whatever the row holds (nothing outside the row is read).
  * The same inputs give the same bits (rows that start elsewhere within 16
  * bytes are summed in another order).
  */

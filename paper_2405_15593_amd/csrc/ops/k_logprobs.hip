@@ -343,17 +343,18 @@ __global__ __launch_bounds__(kMaxThreads) void row_kernel(const LogprobArgs a) {
     const float Ah = ENTGRAD ? -gh * below * inv : 0.0f;
     const float A = Ah - gp * inv;
     const float B = -gh * kLn2 * inv;
+    const float none = known ? 0.0f : gp;  // of a row with no possible token
     auto part = [&](float v, float factor) {
       const float d = (v - t.m) * a.c;
       const float p = exp2_fast(d);
       const float g = ENTGRAD ? p * __builtin_fmaf(B, fmaxf(d, -1000.0f), factor) : p * factor;
-      return empty ? 0.0f : g;
+      return empty ? none : g;
     };
     auto grad = [&](float v) { return part(v, A); };
     // g_p (1 - p) without the difference where p is nearly 1
     auto grad_target = [&](float v) {
       const float others = v == t.m ? rest : t.s - exp2_fast((v - t.m) * a.c);
-      return empty ? 0.0f : part(v, Ah) + gp * others * inv;
+      return empty ? none : part(v, Ah) + gp * others * inv;
     };
     const bool aligned = (((uintptr_t)x ^ (uintptr_t)dx) & 15) == 0;
     uint4v* const dbody = (uint4v*)(dx + head * C::kSize);
