@@ -346,7 +346,7 @@ int microadam_step_noalloc(const microadam_config* cfg, const int64_t* numels, i
  *                   3e-3 in the Frobenius norm.
  *                 MICROADAM_PRECISION_SPLIT  a sum of two binary16 numbers
  *                   (22 bits); three products for one; results are good to
- *                   1e-6.
+ *                   1e-6 to 2e-6.
  *                 MICROADAM_PRECISION_AUTO   SPLIT for binary32 results or
  *                   parameters, else F16.
  */
@@ -458,8 +458,9 @@ int microadam_muon_step(const microadam_muon_config* cfg, const microadam_matrix
  *     and -1.
  *   - A token outside [0, vocab) that is not ignore_index: logp NaN, gradient
  *     NaN, whatever the row holds (nothing outside the row is read).
- * The same inputs give the same bits (rows that start elsewhere within 16
- * bytes are summed in another order).
+ * The same call gives the same bits.  The order of a row's sums, and so their
+ * last bits, goes by where the row starts within 16 bytes, by whether the call
+ * has more than 128 rows, by top_k, and by which of the two functions it is.
  */
 typedef struct microadam_logits {
   const void* data;

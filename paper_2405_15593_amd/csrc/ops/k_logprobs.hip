@@ -15,9 +15,11 @@
 // alternatives and the gradient come from the registers.  A row too long for
 // them is taken in segments, and read again for the alternatives or the
 // gradient.  The bound is memory, a row's bytes once and once more for the
-// gradient: 8192 x 32000 bf16 with the gradient takes 158 us (6.6 TB/s).  4096 x 32000 with 8 alternatives and no gradient takes 69
-// us (3.8 TB/s): 13 vector operations and an exponential per element, and two
-// rows a CU to overlap them with the loads.
+// gradient: 8192 x 32000 bf16 with the gradient takes 185 us (5.7 TB/s), 157 to
+// 161 us with a fifth of the rows ignored, which are not read (5.9 to 6.0 TB/s).
+// 4096 x 32000 with 8 alternatives and no gradient takes 69 us (3.8 TB/s): 13
+// vector operations and an exponential per element, and two rows a CU to
+// overlap them with the loads.
 #include "logprobs_device.h"
 
 namespace microadam {

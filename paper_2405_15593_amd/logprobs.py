@@ -129,7 +129,11 @@ def _values(logits, targets, top_k, temperature, ignore_index):
 def _grad_rows(logits: torch.Tensor, given) -> torch.Tensor:
     """[rows, vocab] for the gradient, whose rows start at the same place in 16
     bytes as the logits' rows: at most 15 bytes of a row and of the start are
-    left unused, none where the logits are dense and start aligned."""
+    left unused, none where the logits are dense and start aligned.  Rows in
+    groups: only as far as the groups' stride allows.  Of logits[:, :-1] with a
+    vocabulary that is no multiple of 16 bytes most groups start elsewhere, and
+    their gradient is stored element by element (4 x 2047 x 50257 bf16: 446 us;
+    of a dense copy 396, and 272 for the copy)."""
     _, address, rows, vocab, ld = given[:5]
     size = logits.element_size()
     per = 16 // size
@@ -157,7 +161,7 @@ def token_logprobs_and_grad(logits: torch.Tensor, targets: torch.Tensor, grad_lo
     For the mean negative log likelihood of n tokens, grad_logp is -1/n.
     ``out``: where the gradient goes (``logits`` itself is allowed; autograd
     sees the write as one in place, so a backward that saved what was there
-    raises)."""
+    raises).  Nothing else is recorded for autograd."""
     refuse_tangents("token_logprobs_and_grad", (logits, grad_logp, grad_entropy, out))
     if logits.requires_grad:
         logits = logits.detach()

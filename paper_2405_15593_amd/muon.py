@@ -185,7 +185,9 @@ def muon_step(params, grads, momenta, *, lr: float, momentum: float = 0.95, nest
 class Muon(torch.optim.Optimizer):
     """Muon for weight matrices on a ROCm device (float32 or bfloat16, two or
     more dimensions; a parameter with more than two is a stack of matrices over
-    its last two).  ``momentum_dtype`` is the dtype of the one state tensor per
+    its last two).  A convolution's weight is not such a stack, and nothing
+    tells the two apart: its kernels would be orthogonalised one by one.  Give
+    it to another optimizer.  ``momentum_dtype`` is the dtype of the one state tensor per
     parameter (None: the parameter's)."""
 
     def __init__(self, params, lr: float = 1e-3, momentum: float = 0.95, nesterov: bool = True,
