@@ -494,6 +494,41 @@ int microadam_token_logprobs_grad(const microadam_logits* logits, const float* g
                                   const float* grad_entropy, float* logp, float* entropy, void* grad,
                                   int64_t grad_ld, void* stream);
 
+/*
+ * ------------------------------------------------- gradient norm and clipping
+ *
+ * The 2-norm n = sqrt(sum g^2) over a list of n_grads gradients, each of
+ * numels[i] contiguous elements of dtypes[i] (MICROADAM_F32 or MICROADAM_BF16,
+ * mixed as they come; at most 2^40 elements, none allowed) at an address
+ * aligned to its elements.  Squares are taken and summed in binary64, in an
+ * order fixed by sizes and addresses within 16 bytes: the same list gives the
+ * same bits.  *norm (device memory) is n rounded to binary32; an empty list
+ * gives 0, NaN or infinite gradients give NaN or an infinity.
+ * Nothing is allocated on the device: the workspace (8-byte aligned, of any
+ * content; microadam_clip_workspace says how many bytes) belongs to the caller
+ * and is in use until the queued work is done.  The three arrays are read
+ * before the call returns.  A list takes 2 launches, and one (clipping: two)
+ * more for every further 160 gradients.
+ */
+int microadam_clip_workspace(uint64_t* bytes);
+
+int microadam_grad_norm(const void* const* grads, const int64_t* numels, const int32_t* dtypes,
+                        int32_t n_grads, float* norm, void* workspace, uint64_t workspace_bytes,
+                        void* stream);
+
+/*
+ * The same norm, and g <- c g in place with c = max_norm / (n + eps) where
+ * n + eps > max_norm (n in binary64; products are rounded once to binary32,
+ * then to the gradient's dtype); elsewhere nothing is written.  max_norm >= 0
+ * (infinity: no limit), eps >= 0.  A norm of NaN makes every gradient NaN, an
+ * infinite one makes the finite elements zero and the infinite ones NaN: *norm
+ * tells.  Gradients must not share bytes with each other, the norm or the
+ * workspace: such a list is refused.
+ */
+int microadam_clip_grads(void* const* grads, const int64_t* numels, const int32_t* dtypes,
+                         int32_t n_grads, double max_norm, double eps, float* norm, void* workspace,
+                         uint64_t workspace_bytes, void* stream);
+
 const char* microadam_error_string(int code);
 
 /* The calling thread's most recent error message ("" if none). */

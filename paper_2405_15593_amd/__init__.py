@@ -139,6 +139,7 @@ EXPORTS = (
     "microadam_kernel_times_total", "microadam_step_noalloc", "microadam_error_string",
     "microadam_last_error", "microadam_matrix_workspace", "microadam_orthogonalize", "microadam_muon_step",
     "microadam_token_logprobs", "microadam_token_logprobs_grad",
+    "microadam_clip_workspace", "microadam_grad_norm", "microadam_clip_grads",
 )
 
 
@@ -184,6 +185,9 @@ def load(path: str = LIBRARY):
                                         ctypes.c_double, vp, u64, vp]
     lib.microadam_token_logprobs.argtypes = [P(microadam_logits), i32, vp, vp, vp, vp, vp]
     lib.microadam_token_logprobs_grad.argtypes = [P(microadam_logits), vp, vp, vp, vp, vp, i64, vp]
+    lib.microadam_clip_workspace.argtypes = [P(u64)]
+    lib.microadam_grad_norm.argtypes = [vp, vp, vp, i32, vp, vp, u64, vp]
+    lib.microadam_clip_grads.argtypes = [vp, vp, vp, i32, ctypes.c_double, ctypes.c_double, vp, vp, u64, vp]
     lib.microadam_error_string.argtypes = [ctypes.c_int]
     lib.microadam_error_string.restype = ctypes.c_char_p
     lib.microadam_last_error.argtypes = []
@@ -193,7 +197,8 @@ def load(path: str = LIBRARY):
               "microadam_step_kernels", "microadam_set_profiling", "microadam_kernel_times",
               "microadam_kernel_times_total", "microadam_step_noalloc", "microadam_matrix_workspace",
               "microadam_orthogonalize", "microadam_muon_step", "microadam_token_logprobs",
-              "microadam_token_logprobs_grad"):
+              "microadam_token_logprobs_grad", "microadam_clip_workspace", "microadam_grad_norm",
+              "microadam_clip_grads"):
         getattr(lib, f).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -364,6 +369,25 @@ def microadam_token_logprobs_grad(logits: microadam_logits, grad_logp_ptr: int, 
     _check(load().microadam_token_logprobs_grad(ctypes.byref(logits), grad_logp_ptr, grad_entropy_ptr, logp_ptr,
                                                 entropy_ptr, grad_ptr, grad_ld, stream),
            "microadam_token_logprobs_grad")
+
+
+def microadam_clip_workspace() -> int:
+    out = ctypes.c_uint64(0)
+    _check(load().microadam_clip_workspace(ctypes.byref(out)), "microadam_clip_workspace")
+    return out.value
+
+
+def microadam_grad_norm(grads, numels, dtypes, n: int, norm_ptr: int, workspace_ptr: int, workspace_bytes: int,
+                        stream: int = 0) -> None:
+    """`grads`, `numels`, `dtypes`: ctypes arrays of c_void_p, c_int64, c_int32."""
+    _check(load().microadam_grad_norm(grads, numels, dtypes, n, norm_ptr, workspace_ptr, workspace_bytes, stream),
+           "microadam_grad_norm")
+
+
+def microadam_clip_grads(grads, numels, dtypes, n: int, max_norm: float, eps: float, norm_ptr: int,
+                         workspace_ptr: int, workspace_bytes: int, stream: int = 0) -> None:
+    _check(load().microadam_clip_grads(grads, numels, dtypes, n, float(max_norm), float(eps), norm_ptr, workspace_ptr,
+                                       workspace_bytes, stream), "microadam_clip_grads")
 
 
 def microadam_error_string(code: int) -> str:
