@@ -529,6 +529,54 @@ int microadam_clip_grads(void* const* grads, const int64_t* numels, const int32_
                          int32_t n_grads, double max_norm, double eps, float* norm, void* workspace,
                          uint64_t workspace_bytes, void* stream);
 
+/*
+ * ------------------------------------------------- layer norm
+ *
+ * `rows` rows of `cols` elements x, ld elements apart (at least cols), with
+ * weight w and bias b of cols elements (either may be NULL: ones, zeros):
+ *     m = mean x,  r = 1 / sqrt(mean (x - m)^2 + eps),  h = (x - m) r,
+ *     y = h w + b
+ * in binary32 or more, y rounded once to x's dtype.  cols is at most 2^24, rows
+ * at most 2^31; addresses are aligned to their element type, and rows may start
+ * anywhere.  A row with NaN or an infinity gives NaN in its own y.
+ */
+typedef struct microadam_rows {
+  const void* x;
+  const void* weight;
+  const void* bias;
+  int64_t rows, cols, ld;
+  double eps;           /* >= 0 */
+  int32_t dtype;        /* of x, y and their gradients: MICROADAM_F32 or MICROADAM_BF16 */
+  int32_t weight_dtype; /* of weight, bias and their gradients */
+} microadam_rows;
+
+/*
+ * y, y_ld elements from row to row, and for the backward pass mean[rows] and
+ * rstd[rows] (both or neither; m and r in binary32).  What is written shares no
+ * byte with what is read.
+ */
+int microadam_layer_norm(const microadam_rows* rows, void* y, int64_t y_ld, float* mean, float* rstd,
+                         void* stream);
+
+/*
+ * The gradients for dy (of x's shape and dtype, dy_ld elements from row to
+ * row), with g = dy w:
+ *     dx = r (g - mean g - h mean(g h)),  dweight = sum dy h,  dbias = sum dy
+ * (sums over the rows; zeros without rows), from the x, weight and eps of the
+ * forward call and the mean and rstd that it wrote.  Each of dx, dweight and
+ * dbias may be NULL.  Sums are held in binary32, partly first per workgroup,
+ * and joined in an order that goes by the sizes: the same call gives the same
+ * bits.  The workspace (16-byte aligned, of any content;
+ * microadam_layer_norm_workspace, which reads the sizes and dtypes alone) is
+ * needed for dweight and dbias; it belongs to the caller and is in use until
+ * the queued work is done.  What is written shares no byte with what is read.
+ */
+int microadam_layer_norm_workspace(const microadam_rows* rows, uint64_t* bytes);
+
+int microadam_layer_norm_grad(const microadam_rows* rows, const float* mean, const float* rstd,
+                              const void* dy, int64_t dy_ld, void* dx, int64_t dx_ld, void* dweight,
+                              void* dbias, void* workspace, uint64_t workspace_bytes, void* stream);
+
 const char* microadam_error_string(int code);
 
 /* The calling thread's most recent error message ("" if none). */

@@ -131,6 +131,20 @@ class microadam_logits(ctypes.Structure):
     ]
 
 
+class microadam_rows(ctypes.Structure):
+    _fields_ = [
+        ("x", ctypes.c_void_p),
+        ("weight", ctypes.c_void_p),
+        ("bias", ctypes.c_void_p),
+        ("rows", ctypes.c_int64),
+        ("cols", ctypes.c_int64),
+        ("ld", ctypes.c_int64),
+        ("eps", ctypes.c_double),
+        ("dtype", ctypes.c_int32),
+        ("weight_dtype", ctypes.c_int32),
+    ]
+
+
 # every symbol include/microadam.h declares
 EXPORTS = (
     "microadam_state_bytes", "microadam_init", "microadam_step", "microadam_destroy",
@@ -140,6 +154,7 @@ EXPORTS = (
     "microadam_last_error", "microadam_matrix_workspace", "microadam_orthogonalize", "microadam_muon_step",
     "microadam_token_logprobs", "microadam_token_logprobs_grad",
     "microadam_clip_workspace", "microadam_grad_norm", "microadam_clip_grads",
+    "microadam_layer_norm", "microadam_layer_norm_workspace", "microadam_layer_norm_grad",
 )
 
 
@@ -188,6 +203,9 @@ def load(path: str = LIBRARY):
     lib.microadam_clip_workspace.argtypes = [P(u64)]
     lib.microadam_grad_norm.argtypes = [vp, vp, vp, i32, vp, vp, u64, vp]
     lib.microadam_clip_grads.argtypes = [vp, vp, vp, i32, ctypes.c_double, ctypes.c_double, vp, vp, u64, vp]
+    lib.microadam_layer_norm.argtypes = [P(microadam_rows), vp, i64, vp, vp, vp]
+    lib.microadam_layer_norm_workspace.argtypes = [P(microadam_rows), P(u64)]
+    lib.microadam_layer_norm_grad.argtypes = [P(microadam_rows), vp, vp, vp, i64, vp, i64, vp, vp, vp, u64, vp]
     lib.microadam_error_string.argtypes = [ctypes.c_int]
     lib.microadam_error_string.restype = ctypes.c_char_p
     lib.microadam_last_error.argtypes = []
@@ -198,7 +216,8 @@ def load(path: str = LIBRARY):
               "microadam_kernel_times_total", "microadam_step_noalloc", "microadam_matrix_workspace",
               "microadam_orthogonalize", "microadam_muon_step", "microadam_token_logprobs",
               "microadam_token_logprobs_grad", "microadam_clip_workspace", "microadam_grad_norm",
-              "microadam_clip_grads"):
+              "microadam_clip_grads", "microadam_layer_norm", "microadam_layer_norm_workspace",
+              "microadam_layer_norm_grad"):
         getattr(lib, f).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -388,6 +407,27 @@ def microadam_clip_grads(grads, numels, dtypes, n: int, max_norm: float, eps: fl
                          workspace_ptr: int, workspace_bytes: int, stream: int = 0) -> None:
     _check(load().microadam_clip_grads(grads, numels, dtypes, n, float(max_norm), float(eps), norm_ptr, workspace_ptr,
                                        workspace_bytes, stream), "microadam_clip_grads")
+
+
+def microadam_layer_norm(rows: microadam_rows, y_ptr: int, y_ld: int, mean_ptr: int, rstd_ptr: int,
+                         stream: int = 0) -> None:
+    _check(load().microadam_layer_norm(ctypes.byref(rows), y_ptr, y_ld, mean_ptr, rstd_ptr, stream),
+           "microadam_layer_norm")
+
+
+def microadam_layer_norm_workspace(rows: microadam_rows) -> int:
+    out = ctypes.c_uint64(0)
+    _check(load().microadam_layer_norm_workspace(ctypes.byref(rows), ctypes.byref(out)),
+           "microadam_layer_norm_workspace")
+    return out.value
+
+
+def microadam_layer_norm_grad(rows: microadam_rows, mean_ptr: int, rstd_ptr: int, dy_ptr: int, dy_ld: int,
+                              dx_ptr: int, dx_ld: int, dweight_ptr: int, dbias_ptr: int, workspace_ptr: int,
+                              workspace_bytes: int, stream: int = 0) -> None:
+    _check(load().microadam_layer_norm_grad(ctypes.byref(rows), mean_ptr, rstd_ptr, dy_ptr, dy_ld, dx_ptr, dx_ld,
+                                            dweight_ptr, dbias_ptr, workspace_ptr, workspace_bytes, stream),
+           "microadam_layer_norm_grad")
 
 
 def microadam_error_string(code: int) -> str:

@@ -1,0 +1,130 @@
+"""Layer norm over the last dimension, over the C ABI
+(``microadam_layer_norm``, ``microadam_layer_norm_grad``).
+
+``layer_norm`` is differentiable in the input, the weight and the bias.  The
+input is float32 or bfloat16 on a ROCm device, weight and bias are of one of
+these dtypes too, the input's or the other (float32 weights of bfloat16
+activations).  Rows at one stride are read where they lie; any other layout is
+copied first.  Work is queued on torch's current stream.
+"""
+from __future__ import annotations
+
+import contextlib
+from typing import Optional
+
+import torch
+
+from . import (MICROADAM_BF16, MICROADAM_F32, microadam_layer_norm, microadam_layer_norm_grad,
+               microadam_layer_norm_workspace, microadam_rows)
+from ._autograd import refuse_tangents
+
+_HERE = contextlib.nullcontext()
+_DTYPES = {torch.float32: MICROADAM_F32, torch.bfloat16: MICROADAM_BF16}
+
+
+def _on(device):
+    """The device as the current one; nothing to do where it is."""
+    return _HERE if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+
+
+def _matrix(t: torch.Tensor):
+    """(t, or a copy of it, that lies in rows at one stride; rows; row stride)."""
+    cols = t.shape[-1]
+    rows = t.numel() // cols
+    if t.is_contiguous():
+        return t, rows, cols
+    if cols == 1 or t.stride(-1) == 1:
+        lead = [(n, s) for n, s in zip(t.shape[:-1], t.stride()[:-1]) if n != 1]
+        if not lead:
+            return t, rows, cols
+        if lead[-1][1] >= cols and all(a[1] == b[0] * b[1] for a, b in zip(lead, lead[1:])):
+            return t, rows, lead[-1][1]
+    return t.contiguous(), rows, cols
+
+
+def _check(x, weight, bias):
+    code = _DTYPES.get(x.dtype)
+    if code is None:
+        raise TypeError(f"x: float32 or bfloat16, not {x.dtype}")
+    if not x.is_cuda:
+        raise ValueError("x: a tensor on a ROCm device")
+    if x.dim() < 1 or x.shape[-1] < 1:
+        raise ValueError("x: at least one element in the last dimension")
+    side = None
+    for t, what in ((weight, "weight"), (bias, "bias")):
+        if t is None:
+            continue
+        if t.dtype not in _DTYPES:
+            raise TypeError(f"{what}: float32 or bfloat16, not {t.dtype}")
+        if side is not None and t.dtype is not side:
+            raise TypeError("weight and bias: one dtype")
+        side = t.dtype
+        if t.shape != x.shape[-1:] or t.device != x.device:
+            raise ValueError(f"{what}: one element for each of x's last dimension, on x's device")
+    return code, code if side is None else _DTYPES[side]
+
+
+def _address(t):
+    return None if t is None else t.data_ptr()
+
+
+def _forward(x, weight, bias, eps, keep):
+    codes = _check(x, weight, bias)
+    given, rows, ld = _matrix(x)
+    w, b = (t if t is None else t.contiguous() for t in (weight, bias))
+    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    mean = rstd = None
+    if keep:
+        mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=x.device).unbind(0)
+    with _on(x.device):
+        microadam_layer_norm(microadam_rows(given.data_ptr(), _address(w), _address(b), rows, x.shape[-1], ld, eps, *codes),
+                             y.data_ptr(), x.shape[-1], _address(mean), _address(rstd),
+                             torch.cuda.current_stream(x.device.index).cuda_stream)
+    return y, mean, rstd
+
+
+class _LayerNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, eps):
+        y, mean, rstd = _forward(x, weight, bias, eps, True)
+        # (the bias itself is not needed, its dtype is)
+        ctx.save_for_backward(x, weight, mean, rstd)
+        ctx.settings = (eps, None if bias is None else bias.dtype)
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        x, weight, mean, rstd = ctx.saved_tensors
+        eps, bias_dtype = ctx.settings
+        want_x, want_w, want_b, _ = ctx.needs_input_grad
+        side_dtype = weight.dtype if weight is not None else bias_dtype or x.dtype
+        cols, dev = x.shape[-1], x.device
+        given, rows, ld = _matrix(x)
+        dy, _, dy_ld = _matrix(dy)
+        w = weight if weight is None else weight.contiguous()
+        dx = torch.empty(x.shape, dtype=x.dtype, device=dev) if want_x else None
+        dw = torch.empty(cols, dtype=side_dtype, device=dev) if want_w else None
+        db = torch.empty(cols, dtype=side_dtype, device=dev) if want_b else None
+        r = microadam_rows(given.data_ptr(), _address(w), None, rows, cols, ld, eps, _DTYPES[x.dtype],
+                           _DTYPES[side_dtype])
+        with _on(dev):
+            need = microadam_layer_norm_workspace(r) if want_w or want_b else 0
+            workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+            microadam_layer_norm_grad(r, mean.data_ptr(), rstd.data_ptr(), dy.data_ptr(), dy_ld, _address(dx), cols,
+                                      _address(dw), _address(db), _address(workspace), need,
+                                      torch.cuda.current_stream(dev.index).cuda_stream)
+        return dx, dw, db, None
+
+
+def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, *,
+               eps: float = 1e-5) -> torch.Tensor:
+    """Rows (the last dimension) of ``x`` with their mean taken off, divided by
+    the root of their variance plus ``eps``, times ``weight``, plus ``bias``; of
+    x's shape and dtype.  There is no derivative of the backward pass, nor one
+    in forward mode."""
+    refuse_tangents("layer_norm", (x, weight, bias))
+    if torch.is_grad_enabled() and (x.requires_grad or (weight is not None and weight.requires_grad) or
+                                    (bias is not None and bias.requires_grad)):
+        return _LayerNorm.apply(x, weight, bias, eps)
+    return _forward(x, weight, bias, eps, False)[0]
