@@ -577,6 +577,69 @@ int microadam_layer_norm_grad(const microadam_rows* rows, const float* mean, con
                               const void* dy, int64_t dy_ld, void* dx, int64_t dx_ld, void* dweight,
                               void* dbias, void* workspace, uint64_t workspace_bytes, void* stream);
 
+/*
+ * ------------------------------------------------- attention
+ *
+ * For each of `batch` sequences, `heads` heads of `queries` queries and `keys`
+ * keys, of `dim` elements (a multiple of 8, at most 128); `kv_heads` divides
+ * heads, and heads / kv_heads consecutive query heads share a key head:
+ *     z = scale q k,   p = softmax z over the keys that a query sees,
+ *     out = p v
+ * A query sees the sequence's first key_lengths keys (int32, device memory;
+ * NULL: all; values are taken into [0, keys]), and with causal = 1 of these the
+ * ones up to query + keys - queries: the last query sees the last key.  A query
+ * that sees no key has out = 0 and takes no part in the gradients.  Keys and
+ * values past a length are not read.  What causality hides is multiplied by
+ * zero: keys and values before the length are expected to be finite.
+ * Scores, their maxima, sums and all accumulators are binary32.  Products are
+ * of the operands' dtype: p and the scores' gradients are rounded to bfloat16
+ * before their products with bfloat16 operands (half a step, 2^-8 of each),
+ * binary32 operands are multiplied in binary32.
+ *
+ * An operand is addressed by the elements from sequence to sequence, position
+ * to position and head to head (>= 0, at most 2^40; addresses are aligned to
+ * the element type); the elements of dim are contiguous.  What is written has
+ * no two elements in one place, and shares no byte with what is read.
+ */
+typedef struct microadam_heads {
+  void* data;
+  int64_t batch_stride, pos_stride, head_stride;
+} microadam_heads;
+
+typedef struct microadam_attention {
+  microadam_heads q, k, v; /* read only */
+  const int32_t* key_lengths;
+  int64_t batch, queries, keys, heads, kv_heads, dim;
+  double scale;   /* finite, > 0 */
+  int32_t dtype;  /* MICROADAM_F32 or MICROADAM_BF16 */
+  int32_t causal; /* 0 or 1 */
+} microadam_attention;
+
+/*
+ * Bytes of workspace for the forward call (grad = 0) and for the gradients
+ * (grad = 1), by the sizes and dtype alone.  It is 256-byte aligned, of any
+ * content, belongs to the caller and is in use until the queued work is done;
+ * where the bytes are 0 it may be NULL.
+ */
+int microadam_attention_workspace(const microadam_attention* attention, int32_t grad, uint64_t* bytes);
+
+/*
+ * out, and for the backward pass lse[batch][heads][queries] (NULL: not
+ * wanted): log2 of the sum of 2^(z log2 e), +infinity where no key is seen.
+ */
+int microadam_attention_forward(const microadam_attention* attention, const microadam_heads* out,
+                                float* lse, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/*
+ * dq, dk and dv for dout, from the operands of the forward call and the out and
+ * lse that it wrote.  The gradients of shared heads are summed in registers,
+ * in binary32, in one order: the same call gives the same bits.
+ */
+int microadam_attention_grad(const microadam_attention* attention, const microadam_heads* out,
+                             const float* lse, const microadam_heads* dout, const microadam_heads* dq,
+                             const microadam_heads* dk, const microadam_heads* dv, void* workspace,
+                             uint64_t workspace_bytes, void* stream);
+
 const char* microadam_error_string(int code);
 
 /* The calling thread's most recent error message ("" if none). */

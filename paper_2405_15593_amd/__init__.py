@@ -145,6 +145,33 @@ class microadam_rows(ctypes.Structure):
     ]
 
 
+class microadam_heads(ctypes.Structure):
+    _fields_ = [
+        ("data", ctypes.c_void_p),
+        ("batch_stride", ctypes.c_int64),
+        ("pos_stride", ctypes.c_int64),
+        ("head_stride", ctypes.c_int64),
+    ]
+
+
+class microadam_attention(ctypes.Structure):
+    _fields_ = [
+        ("q", microadam_heads),
+        ("k", microadam_heads),
+        ("v", microadam_heads),
+        ("key_lengths", ctypes.c_void_p),
+        ("batch", ctypes.c_int64),
+        ("queries", ctypes.c_int64),
+        ("keys", ctypes.c_int64),
+        ("heads", ctypes.c_int64),
+        ("kv_heads", ctypes.c_int64),
+        ("dim", ctypes.c_int64),
+        ("scale", ctypes.c_double),
+        ("dtype", ctypes.c_int32),
+        ("causal", ctypes.c_int32),
+    ]
+
+
 # every symbol include/microadam.h declares
 EXPORTS = (
     "microadam_state_bytes", "microadam_init", "microadam_step", "microadam_destroy",
@@ -155,6 +182,7 @@ EXPORTS = (
     "microadam_token_logprobs", "microadam_token_logprobs_grad",
     "microadam_clip_workspace", "microadam_grad_norm", "microadam_clip_grads",
     "microadam_layer_norm", "microadam_layer_norm_workspace", "microadam_layer_norm_grad",
+    "microadam_attention_workspace", "microadam_attention_forward", "microadam_attention_grad",
 )
 
 
@@ -206,6 +234,10 @@ def load(path: str = LIBRARY):
     lib.microadam_layer_norm.argtypes = [P(microadam_rows), vp, i64, vp, vp, vp]
     lib.microadam_layer_norm_workspace.argtypes = [P(microadam_rows), P(u64)]
     lib.microadam_layer_norm_grad.argtypes = [P(microadam_rows), vp, vp, vp, i64, vp, i64, vp, vp, vp, u64, vp]
+    lib.microadam_attention_workspace.argtypes = [P(microadam_attention), i32, P(u64)]
+    lib.microadam_attention_forward.argtypes = [P(microadam_attention), P(microadam_heads), vp, vp, u64, vp]
+    lib.microadam_attention_grad.argtypes = [P(microadam_attention), P(microadam_heads), vp, P(microadam_heads),
+                                             P(microadam_heads), P(microadam_heads), P(microadam_heads), vp, u64, vp]
     lib.microadam_error_string.argtypes = [ctypes.c_int]
     lib.microadam_error_string.restype = ctypes.c_char_p
     lib.microadam_last_error.argtypes = []
@@ -217,7 +249,8 @@ def load(path: str = LIBRARY):
               "microadam_orthogonalize", "microadam_muon_step", "microadam_token_logprobs",
               "microadam_token_logprobs_grad", "microadam_clip_workspace", "microadam_grad_norm",
               "microadam_clip_grads", "microadam_layer_norm", "microadam_layer_norm_workspace",
-              "microadam_layer_norm_grad"):
+              "microadam_layer_norm_grad", "microadam_attention_workspace", "microadam_attention_forward",
+              "microadam_attention_grad"):
         getattr(lib, f).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -428,6 +461,27 @@ def microadam_layer_norm_grad(rows: microadam_rows, mean_ptr: int, rstd_ptr: int
     _check(load().microadam_layer_norm_grad(ctypes.byref(rows), mean_ptr, rstd_ptr, dy_ptr, dy_ld, dx_ptr, dx_ld,
                                             dweight_ptr, dbias_ptr, workspace_ptr, workspace_bytes, stream),
            "microadam_layer_norm_grad")
+
+
+def microadam_attention_workspace(attention: microadam_attention, grad: bool) -> int:
+    out = ctypes.c_uint64(0)
+    _check(load().microadam_attention_workspace(ctypes.byref(attention), 1 if grad else 0, ctypes.byref(out)),
+           "microadam_attention_workspace")
+    return out.value
+
+
+def microadam_attention_forward(attention: microadam_attention, out: microadam_heads, lse_ptr: int,
+                                workspace_ptr: int, workspace_bytes: int, stream: int = 0) -> None:
+    _check(load().microadam_attention_forward(ctypes.byref(attention), ctypes.byref(out), lse_ptr, workspace_ptr,
+                                              workspace_bytes, stream), "microadam_attention_forward")
+
+
+def microadam_attention_grad(attention: microadam_attention, out: microadam_heads, lse_ptr: int,
+                             dout: microadam_heads, dq: microadam_heads, dk: microadam_heads, dv: microadam_heads,
+                             workspace_ptr: int, workspace_bytes: int, stream: int = 0) -> None:
+    _check(load().microadam_attention_grad(ctypes.byref(attention), ctypes.byref(out), lse_ptr, ctypes.byref(dout),
+                                           ctypes.byref(dq), ctypes.byref(dk), ctypes.byref(dv), workspace_ptr,
+                                           workspace_bytes, stream), "microadam_attention_grad")
 
 
 def microadam_error_string(code: int) -> str:

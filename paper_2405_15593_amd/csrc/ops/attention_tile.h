@@ -1,0 +1,241 @@
+// What the attention kernels share: fragments of the matrix instruction, tiles
+// in LDS, rows and their limits.
+//
+// All products run on the 32x32 matrix instructions in one form, D = A B with D's
+// column in lane % 32: its rows 8 (i / 4) + 4 (lane / 32) + i % 4 are the lane's
+// sixteen results i.  A product's results are then the next one's B as they lie,
+// eight of them a step of sixteen, when its A is read with the rows of the sum in
+// that order: scores never leave the registers.  A fragment is eight elements a
+// lane for both types: one 32x32x16 instruction of bfloat16, eight 32x32x2 of
+// binary32.
+//
+// Tiles keep the rows of q, k, v or dout.  A row's 16-byte chunks c lie at
+// c ^ (row / 4 % 4), and rows are padded to 4 or 12 chunks modulo 16, so that
+// neither sixteen rows' same chunk (a fragment along the row) nor four rows' four
+// chunks (the transposing read) meet on a bank.
+#pragma once
+#include "attention_device.h"
+#include "elements.h"
+
+namespace microadam {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float float4v __attribute__((ext_vector_type(4)));
+typedef float float16v __attribute__((ext_vector_type(16)));
+typedef uint32_t uint2v __attribute__((ext_vector_type(2)));
+typedef short short4v __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) short4v* lds_short4;
+
+__device__ inline float infinity() { return __uint_as_float(0x7f800000u); }
+__device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+template <bool BF16>
+struct Frag;
+template <>
+struct Frag<true> {
+  bf16x8 v;
+};
+template <>
+struct Frag<false> {
+  float v[8];
+};
+
+__device__ inline void multiply(float16v& d, const Frag<true>& a, const Frag<true>& b) {
+  d = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, b.v, d, 0, 0, 0);
+}
+
+__device__ inline void multiply(float16v& d, const Frag<false>& a, const Frag<false>& b) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) d = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[j], b.v[j], d, 0, 0, 0);
+}
+
+__device__ inline float16v zeros() {
+  float16v z;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) z[i] = 0.0f;
+  return z;
+}
+
+// Results 8 HALF to 8 HALF + 7 as a fragment.
+template <bool BF16, int HALF>
+__device__ inline Frag<BF16> as_frag(const float16v& d) {
+  Frag<BF16> f;
+  if constexpr (BF16) {
+    uint4v q;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) q[i] = pack_bf16(d[8 * HALF + 2 * i], d[8 * HALF + 2 * i + 1]);
+    f.v = __builtin_bit_cast(bf16x8, q);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f.v[i] = d[8 * HALF + i];
+  }
+  return f;
+}
+
+// Eight elements of memory, zeros where there are none.
+template <bool BF16>
+__device__ inline Frag<BF16> load_frag(const void* p, int64_t at, bool there) {
+  Frag<BF16> f;
+  if constexpr (BF16) {
+    f.v = __builtin_bit_cast(bf16x8, there ? Elements<true>::load(p, at) : uint4v{0, 0, 0, 0});
+  } else {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const uint4v q = there ? Elements<false>::load(p, at + 4 * u) : uint4v{0, 0, 0, 0};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) f.v[4 * u + i] = __uint_as_float(q[i]);
+    }
+  }
+  return f;
+}
+
+// ROWS rows of D elements in LDS.
+template <bool BF16, int D, int ROWS>
+struct Tile {
+  static constexpr int kSize = BF16 ? 2 : 4;
+  static constexpr int kChunks = D * kSize / 16;
+  static constexpr int kMod = kChunks % 16;
+  static constexpr int kPad = kMod == 0 ? 4 : kMod == 8 ? 4 : 0;
+  static_assert((kChunks + kPad) % 16 == 4 || (kChunks + kPad) % 16 == 12, "rows' places");
+  static constexpr int kStride = (kChunks + kPad) * 16;
+  static constexpr int kBytes = ROWS * kStride;
+
+  __device__ static int place(int row, int chunk) { return row * kStride + ((chunk ^ ((row >> 2) & 3)) << 4); }
+
+  // Row m = lane % 32 (of rows from `row`), elements 16 step + 8 (lane / 32) + j.
+  __device__ static Frag<BF16> along(const uint8_t* tile, int row, int step, int lane) {
+    const int r = row + (lane & 31), h = lane >> 5;
+    Frag<BF16> f;
+    if constexpr (BF16) {
+      f.v = __builtin_bit_cast(bf16x8, *(const uint4v*)(tile + place(r, 2 * step + h)));
+    } else {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const float4v q = *(const float4v*)(tile + place(r, 4 * step + 2 * h + u));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f.v[4 * u + i] = q[i];
+      }
+    }
+    return f;
+  }
+
+  // Element 32 part + lane % 32 of rows row + 8 (j / 4) + 4 (lane / 32) + j % 4.
+  __device__ static Frag<BF16> across(const uint8_t* tile, int row, int part, int lane) {
+    const int h = lane >> 5;
+    Frag<BF16> f;
+    if constexpr (BF16) {
+      // sixteen lanes address four rows' four times four elements, and receive
+      // one element of four rows each
+      const int r = row + 4 * h + ((lane & 15) >> 2), chunk = 4 * part + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+      const uint8_t* lo = tile + place(r, chunk) + (lane & 1) * 8;
+      const uint8_t* hi = tile + place(r + 8, chunk) + (lane & 1) * 8;
+      const short4v a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4)lo);
+      const short4v b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4)hi);
+      f.v = __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+    } else {
+      const int d = 32 * part + (lane & 31);
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        f.v[j] = *(const float*)(tile + place(row + 8 * (j / 4) + 4 * h + j % 4, d >> 2) + (d & 3) * 4);
+    }
+    return f;
+  }
+};
+
+// A tile on its way from memory to LDS through THREADS threads' registers.
+template <bool BF16, int D, int ROWS, int THREADS>
+struct Staged {
+  typedef Tile<BF16, D, ROWS> T;
+  typedef Elements<BF16> E;
+  static constexpr int kCount = (ROWS * T::kChunks + THREADS - 1) / THREADS;
+  uint4v q[kCount];
+
+  // `at(row)`: a row's first element, negative where there is no such row.
+  template <class F>
+  __device__ void load(const void* base, int dim, int thread, F at) {
+#pragma unroll
+    for (int i = 0; i < kCount; ++i) {
+      const int n = thread + i * THREADS, row = n / T::kChunks, chunk = n % T::kChunks;
+      q[i] = uint4v{0, 0, 0, 0};
+      if (ROWS * T::kChunks % THREADS != 0 && row >= ROWS) continue;
+      const int64_t from = at(row);
+      if (from >= 0 && chunk * E::kPer < dim) q[i] = E::load(base, from + chunk * E::kPer);
+    }
+  }
+  __device__ void store(uint8_t* tile, int thread) const {
+#pragma unroll
+    for (int i = 0; i < kCount; ++i) {
+      const int n = thread + i * THREADS, row = n / T::kChunks, chunk = n % T::kChunks;
+      if (ROWS * T::kChunks % THREADS != 0 && row >= ROWS) continue;
+      *(uint4v*)(tile + T::place(row, chunk)) = q[i];
+    }
+  }
+};
+
+struct __attribute__((packed, aligned(2))) Four2 {
+  uint2v q;
+};
+struct __attribute__((packed, aligned(4))) Four4 {
+  float4v q;
+};
+
+// A lane's sixteen results of 32 elements from `at` on, its column's row in
+// memory: four runs of four.
+template <bool BF16>
+__device__ inline void store_column(void* p, int64_t at, int left, const float16v& d, float factor, int lane) {
+  const int h = lane >> 5;
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    const int e = 8 * g + 4 * h;
+    if (e >= left) continue;
+    const float a = d[4 * g] * factor, b = d[4 * g + 1] * factor, c = d[4 * g + 2] * factor, f = d[4 * g + 3] * factor;
+    if (BF16)
+      ((Four2*)((uint16_t*)p + at + e))->q = uint2v{pack_bf16(a, b), pack_bf16(c, f)};
+    else
+      ((Four4*)((float*)p + at + e))->q = float4v{a, b, c, f};
+  }
+}
+
+// Workgroups go to the eight XCDs in turn: each XCD takes one run of the work,
+// so that the tiles of a head share their keys (or queries) in its L2.
+__device__ inline int run_of_xcd(int block, int total) {
+  const int xcd = block & 7, each = total >> 3, more = total & 7;
+  return xcd * each + (xcd < more ? xcd : more) + (block >> 3);
+}
+
+// A row of the rows that share a key head: its query head and query.
+struct RowAt {
+  int head, query;
+};
+__device__ inline RowAt row_at(const AttentionArgs& a, int kv_head, int row) {
+  const int h = row / a.queries;
+  return {kv_head * a.group + h, row - h * a.queries};
+}
+
+__device__ inline int keys_of(const AttentionArgs& a, int batch) {
+  if (!a.lengths) return a.keys;
+  const int n = a.lengths[batch];
+  return n < 0 ? 0 : n < a.keys ? n : a.keys;
+}
+
+// How many of the first keys a query sees.
+__device__ inline int limit_of(const AttentionArgs& a, int query, int length) {
+  if (!a.causal) return length;
+  const int n = query + 1 + a.keys - a.queries;
+  return n < 0 ? 0 : n < length ? n : length;
+}
+
+__device__ inline int wave_min(int x) {
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) {
+    const int y = __shfl_xor(x, d);
+    x = x < y ? x : y;
+  }
+  return uniform(x);
+}
+__device__ inline int wave_max(int x) { return -wave_min(-x); }
+
+}  // namespace
+}  // namespace microadam

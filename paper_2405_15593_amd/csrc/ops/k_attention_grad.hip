@@ -1,0 +1,294 @@
+// Softmax attention, backward: the probabilities are computed again from q, k
+// and each row's log sum.
+//
+//   p = 2^(c q k - lse),  ds = p (dout v - delta),  delta = sum dout out
+//   dq = scale ds k,  dk = scale ds^T q,  dv = p^T dout
+//
+// Two kernels, each with its sums in registers, so that nothing is added in an
+// order that changes: dq by rows, as forward, in z^T = k q^T, dp^T = v dout^T and
+// dq^T += k^T ds^T; then dk and dv by keys, in z = q k^T, dp = dout v^T, dv^T +=
+// dout^T p and dk^T += q^T ds, over all rows of the query heads that share the
+// keys.  Seven products where one kernel with shared sums would take five.
+#include "attention_tile.h"
+
+namespace microadam {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kRows = 128;      // of a workgroup, rows or keys
+constexpr int kTile = 32;       // keys or rows of a tile
+
+template <bool BF16, int D>
+__global__ __launch_bounds__(kThreads, 1) void attention_dq_kernel(const AttentionArgs a) {
+  typedef Tile<BF16, D, kTile> T;
+  __shared__ __align__(16) uint8_t lds[2][2][T::kBytes];  // [turn][keys, values]
+  const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
+  const int tiles = (a.rows + kRows - 1) / kRows;
+  const int work = run_of_xcd(blockIdx.x, gridDim.x);
+  const int tile = tiles - 1 - work % tiles, head_of = work / tiles;
+  const int kv_head = head_of % a.kv_heads, batch = head_of / a.kv_heads;
+  const int length = keys_of(a, batch);
+
+  const int row = tile * kRows + wave * 32 + (lane & 31);
+  const bool live = row < a.rows;
+  const RowAt at = row_at(a, kv_head, live ? row : 0);
+  const int limit = live ? limit_of(a, at.query, length) : 0;
+  const int most = wave_max(limit), least = wave_min(live ? limit : a.keys);
+  Frag<BF16> q[D / 16], dout[D / 16];
+  const int64_t q_at = batch * a.q.batch + at.head * a.q.head + at.query * a.q.pos;
+  const int64_t do_at = batch * a.dout.batch + at.head * a.dout.head + at.query * a.dout.pos;
+  const int64_t o_at = batch * a.out.batch + at.head * a.out.head + at.query * a.out.pos;
+  float delta = 0.0f;
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s) {
+    const int d = 16 * s + 8 * (lane >> 5);
+    const bool there = live && d < a.dim;
+    q[s] = load_frag<BF16>(a.q.at, q_at + d, there);
+    dout[s] = load_frag<BF16>(a.dout.at, do_at + d, there);
+    const Frag<BF16> o = load_frag<BF16>(a.out.at, o_at + d, there);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) delta = __builtin_fmaf((float)dout[s].v[j], (float)o.v[j], delta);
+  }
+  delta += __shfl_xor(delta, 32);
+  const int64_t stat = ((int64_t)batch * a.heads + at.head) * a.queries + at.query;
+  const float lse = live ? a.lse[stat] : infinity();
+  if (live && lane < 32) a.delta[stat] = delta;
+
+  int end;
+  {
+    const int first = tile * kRows, last = first + kRows < a.rows ? first + kRows - 1 : a.rows - 1;
+    const int whole = first / a.queries != last / a.queries;
+    end = limit_of(a, whole ? a.queries - 1 : last % a.queries, length);
+  }
+  const int turns = (end + kTile - 1) / kTile;
+
+  Staged<BF16, D, kTile, kThreads> next_k, next_v;
+  const int64_t k_at = batch * a.k.batch + kv_head * a.k.head, v_at = batch * a.v.batch + kv_head * a.v.head;
+  auto load = [&](int turn) {
+    const int first = turn * kTile;
+    next_k.load(a.k.at, a.dim, threadIdx.x,
+                [&](int r) { return first + r < length ? k_at + (first + r) * a.k.pos : (int64_t)-1; });
+    next_v.load(a.v.at, a.dim, threadIdx.x,
+                [&](int r) { return first + r < length ? v_at + (first + r) * a.v.pos : (int64_t)-1; });
+  };
+  auto store = [&](int turn) {
+    next_k.store(lds[turn & 1][0], threadIdx.x);
+    next_v.store(lds[turn & 1][1], threadIdx.x);
+  };
+
+  float16v dq[D / 32];
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) dq[i] = zeros();
+  if (turns > 0) {
+    load(0);
+    store(0);
+  }
+  __syncthreads();
+  for (int turn = 0; turn < turns; ++turn) {
+    if (turn + 1 < turns) load(turn + 1);
+    const int first = turn * kTile;
+    const uint8_t *keys = lds[turn & 1][0], *values = lds[turn & 1][1];
+    if (first < most) {
+      float16v s = zeros(), dp = zeros();
+#pragma unroll
+      for (int step = 0; step < D / 16; ++step) {
+        multiply(s, T::along(keys, 0, step, lane), q[step]);
+        multiply(dp, T::along(values, 0, step, lane), dout[step]);
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float p = exp2_fast(__builtin_fmaf(s[r], a.c, -lse));
+        s[r] = p * (dp[r] - delta);
+      }
+      if (first + kTile > least) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = first + 8 * (r / 4) + 4 * (lane >> 5) + r % 4 < limit ? s[r] : 0.0f;
+      }
+      const Frag<BF16> d0 = as_frag<BF16, 0>(s), d1 = as_frag<BF16, 1>(s);
+#pragma unroll
+      for (int part = 0; part < D / 32; ++part) {
+        multiply(dq[part], T::across(keys, 0, part, lane), d0);
+        multiply(dq[part], T::across(keys, 16, part, lane), d1);
+      }
+    }
+    if (turn + 1 < turns) store(turn + 1);
+    __syncthreads();
+  }
+  if (!live) return;
+  const int64_t dq_at = batch * a.dq.batch + at.head * a.dq.head + at.query * a.dq.pos;
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) store_column<BF16>(a.dq.at, dq_at + 32 * i, a.dim - 32 * i, dq[i], a.scale, lane);
+}
+
+template <bool BF16, int D>
+__global__ __launch_bounds__(kThreads, 1) void attention_dkv_kernel(const AttentionArgs a) {
+  typedef Tile<BF16, D, kTile> T;
+  __shared__ __align__(16) uint8_t lds[2][2][T::kBytes];  // [turn][queries, dout]
+  __shared__ float lses[2][kTile], deltas[2][kTile];
+  __shared__ int limits[2][kTile];
+  const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), h = lane >> 5;
+  const int tiles = (a.keys + kRows - 1) / kRows;
+  const int work = run_of_xcd(blockIdx.x, gridDim.x);
+  const int tile = work % tiles, head_of = work / tiles;  // (the first keys are seen by the most rows)
+  const int kv_head = head_of % a.kv_heads, batch = head_of / a.kv_heads;
+  const int length = keys_of(a, batch);
+
+  const int key0 = tile * kRows, wave_key = key0 + wave * 32, key = wave_key + (lane & 31);
+  const bool live = key < length;
+  Frag<BF16> k[D / 16], v[D / 16];
+  const int64_t k_at = batch * a.k.batch + kv_head * a.k.head + key * a.k.pos;
+  const int64_t v_at = batch * a.v.batch + kv_head * a.v.head + key * a.v.pos;
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s) {
+    const int d = 16 * s + 8 * h;
+    k[s] = load_frag<BF16>(a.k.at, k_at + d, live && d < a.dim);
+    v[s] = load_frag<BF16>(a.v.at, v_at + d, live && d < a.dim);
+  }
+
+  // the first query that sees one of the workgroup's keys
+  int from = 0;
+  if (a.causal) {
+    from = key0 - (a.keys - a.queries);
+    from = from < 0 ? 0 : from;
+  }
+  const int turns = key0 < length && from < a.queries ? (a.rows + kTile - 1) / kTile : 0;
+  // the first turn from `turn` on with a row that sees a key
+  auto seen = [&](int turn) {
+    if (from == 0) return turn;
+    while (turn < turns) {
+      const int first = turn * kTile, last = first + kTile < a.rows ? first + kTile - 1 : a.rows - 1;
+      if (first % a.queries + (last - first) >= from) break;  // (rows of two heads: past the last query)
+      ++turn;
+    }
+    return turn;
+  };
+
+  Staged<BF16, D, kTile, kThreads> next_q, next_do;
+  float next_lse = 0.0f, next_delta = 0.0f;
+  int next_limit = 0;
+  const int64_t q_at = batch * a.q.batch, do_at = batch * a.dout.batch;
+  auto load = [&](int turn) {
+    const int first = turn * kTile;
+    next_q.load(a.q.at, a.dim, threadIdx.x, [&](int r) {
+      if (first + r >= a.rows) return (int64_t)-1;
+      const RowAt at = row_at(a, kv_head, first + r);
+      return q_at + at.head * a.q.head + at.query * a.q.pos;
+    });
+    next_do.load(a.dout.at, a.dim, threadIdx.x, [&](int r) {
+      if (first + r >= a.rows) return (int64_t)-1;
+      const RowAt at = row_at(a, kv_head, first + r);
+      return do_at + at.head * a.dout.head + at.query * a.dout.pos;
+    });
+    if (threadIdx.x < kTile) {
+      const int r = first + threadIdx.x;
+      const bool there = r < a.rows;
+      const RowAt at = row_at(a, kv_head, there ? r : 0);
+      const int64_t stat = ((int64_t)batch * a.heads + at.head) * a.queries + at.query;
+      next_lse = there ? a.lse[stat] : infinity();
+      next_delta = there ? a.delta[stat] : 0.0f;
+      next_limit = there ? limit_of(a, at.query, length) : 0;
+    }
+  };
+  auto store = [&](int place) {
+    next_q.store(lds[place][0], threadIdx.x);
+    next_do.store(lds[place][1], threadIdx.x);
+    if (threadIdx.x < kTile) {
+      lses[place][threadIdx.x] = next_lse;
+      deltas[place][threadIdx.x] = next_delta;
+      limits[place][threadIdx.x] = next_limit;
+    }
+  };
+
+  float16v dk[D / 32], dv[D / 32];
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) dk[i] = dv[i] = zeros();
+  int turn = seen(0), place = 0;
+  if (turn < turns) {
+    load(turn);
+    store(0);
+  }
+  __syncthreads();
+  while (turn < turns) {
+    const int next = seen(turn + 1);
+    if (next < turns) load(next);
+    const uint8_t *queries = lds[place][0], *douts = lds[place][1];
+    {
+      float16v s = zeros(), dp = zeros();
+#pragma unroll
+      for (int step = 0; step < D / 16; ++step) {
+        multiply(s, T::along(queries, 0, step, lane), k[step]);
+        multiply(dp, T::along(douts, 0, step, lane), v[step]);
+      }
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const float4v lse = *(const float4v*)&lses[place][8 * g + 4 * h];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[4 * g + i] = exp2_fast(__builtin_fmaf(s[4 * g + i], a.c, -lse[i]));
+      }
+      if (a.causal) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = key < limits[place][8 * (r / 4) + 4 * h + r % 4] ? s[r] : 0.0f;
+      }
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const float4v delta = *(const float4v*)&deltas[place][8 * g + 4 * h];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) dp[4 * g + i] = s[4 * g + i] * (dp[4 * g + i] - delta[i]);
+      }
+      const Frag<BF16> p0 = as_frag<BF16, 0>(s), p1 = as_frag<BF16, 1>(s);
+      const Frag<BF16> d0 = as_frag<BF16, 0>(dp), d1 = as_frag<BF16, 1>(dp);
+#pragma unroll
+      for (int part = 0; part < D / 32; ++part) {
+        multiply(dv[part], T::across(douts, 0, part, lane), p0);
+        multiply(dv[part], T::across(douts, 16, part, lane), p1);
+        multiply(dk[part], T::across(queries, 0, part, lane), d0);
+        multiply(dk[part], T::across(queries, 16, part, lane), d1);
+      }
+    }
+    if (next < turns) store(place ^ 1);
+    __syncthreads();
+    turn = next;
+    place ^= 1;
+  }
+  if (key >= a.keys) return;
+  // (a key behind the length has scores of its zeros: no gradient)
+  const float one = live ? 1.0f : 0.0f;
+  const int64_t dk_at = batch * a.dk.batch + kv_head * a.dk.head + key * a.dk.pos;
+  const int64_t dv_at = batch * a.dv.batch + kv_head * a.dv.head + key * a.dv.pos;
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) {
+    store_column<BF16>(a.dk.at, dk_at + 32 * i, a.dim - 32 * i, live ? dk[i] : zeros(), a.scale, lane);
+    store_column<BF16>(a.dv.at, dv_at + 32 * i, a.dim - 32 * i, live ? dv[i] : zeros(), one, lane);
+  }
+}
+
+template <bool BF16, int D>
+void launch_both(const AttentionArgs& a, hipStream_t s) {
+  const int heads = a.kv_heads * a.batch, rows = (a.rows + kRows - 1) / kRows, keys = (a.keys + kRows - 1) / kRows;
+  if (rows) attention_dq_kernel<BF16, D><<<dim3((unsigned)(rows * heads)), dim3(kThreads), 0, s>>>(a);
+  if (keys) attention_dkv_kernel<BF16, D><<<dim3((unsigned)(keys * heads)), dim3(kThreads), 0, s>>>(a);
+}
+
+template <bool BF16>
+void launch_dim(const AttentionArgs& a, hipStream_t s) {
+  if (a.dim <= 32)
+    launch_both<BF16, 32>(a, s);
+  else if (a.dim <= 64)
+    launch_both<BF16, 64>(a, s);
+  else if (a.dim <= 96)
+    launch_both<BF16, 96>(a, s);
+  else
+    launch_both<BF16, 128>(a, s);
+}
+
+}  // namespace
+
+hipError_t launch_attention_grad(const AttentionArgs& a, hipStream_t s) {
+  if (a.bf16)
+    launch_dim<true>(a, s);
+  else
+    launch_dim<false>(a, s);
+  return hipGetLastError();
+}
+
+}  // namespace microadam

@@ -1,0 +1,259 @@
+"""attention and its gradients against binary64 on the CPU; tolerances as
+attention_reference.py derives them."""
+import math
+
+import pytest
+import torch
+
+import paper_2405_15593_amd as ma
+from attention_reference import check, reference
+from paper_2405_15593_amd.attention import attention
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def inputs(b, sq, sk, h, hk, d, dtype, seed=0, scale=1.0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+
+    def make(s, heads):
+        return (torch.randn(b, s, heads, d, generator=g, device="cuda") * scale).to(dtype)
+
+    return make(sq, h), make(sk, hk), make(sk, hk), make(sq, h)
+
+
+def some_lengths(b, sk):
+    """Whole, none, more than there are, fewer than none, and between."""
+    n = [sk, 0, sk + 5, -3, (sk + 1) // 2, max(1, sk - 1), 1]
+    return torch.tensor((n * (b // len(n) + 1))[:b], dtype=torch.int32, device="cuda")
+
+
+def run(q, k, v, dout, **kw):
+    q, k, v = (t.detach().requires_grad_() for t in (q, k, v))
+    out = attention(q, k, v, **kw)
+    return (out, *torch.autograd.grad(out, (q, k, v), dout))
+
+
+def check_all(q, k, v, dout, causal=False, lengths=None, scale=None):
+    got = run(q, k, v, dout, causal=causal, key_lengths=lengths, scale=scale)
+    n = None if lengths is None else lengths.clamp(0, k.shape[1])
+    want = reference(q, k, v, dout, causal, n, scale or q.shape[3] ** -0.5, q.dtype)
+    check(got, *want, q.dtype)
+    plain = attention(q, k, v, causal=causal, key_lengths=lengths, scale=scale)
+    check((plain,), want[0][:1], want[1][:1], q.dtype)
+    return got
+
+
+SHAPES = [
+    (1, 1, 1, 1, 1, 8), (2, 1, 33, 2, 2, 16), (1, 5, 7, 3, 1, 24), (2, 31, 32, 2, 1, 32), (1, 33, 33, 2, 2, 40),
+    (7, 64, 64, 2, 1, 64), (2, 128, 128, 4, 4, 64), (1, 129, 127, 2, 2, 72), (7, 100, 130, 6, 2, 80), (1, 257, 96, 4, 2, 88),
+    (2, 3, 300, 8, 1, 96), (1, 200, 200, 4, 4, 104), (7, 1, 515, 8, 2, 128), (1, 300, 515, 2, 2, 128), (2, 515, 300, 4, 1, 128),
+    (1, 700, 700, 2, 1, 120), (3, 17, 1, 4, 4, 56), (1, 2, 2049, 32, 4, 64), (300, 4, 4, 2, 2, 16),
+]
+
+
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("causal", [False, True], ids=["full", "causal"])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, s)))
+def test_shapes(shape, causal, types):
+    print(f"[attention] {shape} causal {causal} {types}", flush=True)
+    given = inputs(*shape, TYPES[types], seed=sum(shape))
+    check_all(*given, causal=causal)
+    if shape[0] > 1:
+        check_all(*given, causal=causal, lengths=some_lengths(shape[0], shape[2]))
+
+
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("scale", [1e-3, 0.3, 4.0])
+def test_scales(scale, types):
+    """From even probabilities to ones of a single key."""
+    print(f"[attention] scale {scale} {types}", flush=True)
+    check_all(*inputs(1, 70, 130, 2, 1, 64, TYPES[types]), causal=True, scale=scale)
+
+
+def test_large_scores():
+    """Scores of thousands, alike and apart: no overflow, no NaN."""
+    print("[attention] large scores", flush=True)
+    q, k, v, dout = inputs(1, 40, 200, 1, 1, 32, torch.float32)
+    q, k = q.abs() * 30, k.abs() * 30
+    out = attention(q, k, v, scale=1.0)
+    z = (q[0, :, 0].cpu().double() @ k[0, :, 0].cpu().double().t())
+    want = torch.softmax(z, 1) @ v[0, :, 0].cpu().double()
+    # the exponent's argument of some 2^14 is known to 2^-9
+    sure = z.topk(2, 1).values
+    sure = sure[:, 0] - sure[:, 1] > 20
+    assert bool(sure.any()) and bool(torch.isfinite(out).all())
+    assert float((out[0, :, 0].cpu().double() - want).abs()[sure].max()) < 2.0 ** -20
+    assert all(bool(torch.isfinite(t).all()) for t in run(q, k, v, dout, scale=1.0))
+    low = run(q, -k, v, dout, scale=1.0)
+    assert all(bool(torch.isfinite(t).all()) for t in low) and bool(low[0].any())
+
+
+@pytest.mark.parametrize("types", TYPES)
+def test_layouts(types):
+    """Views of one projection, (batch, heads, positions, dim) in memory, odd
+    addresses, expanded and transposed operands."""
+    print(f"[attention] layouts {types}", flush=True)
+    dtype = TYPES[types]
+    q, k, v, dout = inputs(2, 70, 70, 4, 4, 64, dtype)
+    want = run(q, k, v, dout, causal=True)
+    packed = torch.stack((q, k, v), 2)
+    heads_first = [t.transpose(1, 2).contiguous().transpose(1, 2) for t in (q, k, v, dout)]
+    odd = [torch.cat((torch.full_like(t[..., :3], math.nan), t, t[..., :6]), -1)[..., 3:67] for t in (q, k, v, dout)]
+    last = [t.transpose(2, 3).contiguous().transpose(2, 3) for t in (q, k, v, dout)]
+    for given in ((*packed.unbind(2), dout), heads_first, odd, last):
+        for g, w in zip(run(*given, causal=True), want):
+            assert torch.equal(g, w)
+    one = torch.ones((), device="cuda", dtype=dtype).expand(q.shape)
+    for g, w in zip(run(q, k, v, one, causal=True), run(q, k, v, one.contiguous(), causal=True)):
+        assert torch.equal(g, w)
+    k1, v1 = (t[:1].expand(2, 70, 4, 64) for t in (k, v))
+    for g, w in zip(run(q, k1, v1, dout), run(q, k1.contiguous(), v1.contiguous(), dout)):
+        assert torch.equal(g, w)
+    # gradients of what was expanded are summed by autograd
+    leaf = k[:1].clone().requires_grad_()
+    torch.autograd.grad(attention(q, leaf.expand(2, 70, 4, 64), v), leaf, dout)
+
+
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("sq", [1, 90])
+def test_nothing_past_the_length_is_read(sq, types):
+    print(f"[attention] past the length {types}", flush=True)
+    q, k, v, dout = inputs(7, sq, 200, 4, 2, 64, TYPES[types])
+    lengths = some_lengths(7, 200)
+    want = run(q, k, v, dout, key_lengths=lengths)
+    bad_k, bad_v = k.clone(), v.clone()
+    for i, n in enumerate(lengths.clamp(0, 200).tolist()):
+        bad_k[i, n:], bad_v[i, n:] = math.nan, math.inf
+    got = run(q, bad_k, bad_v, dout, key_lengths=lengths)
+    assert all(torch.equal(g, w) for g, w in zip(got, want))
+    for i, n in enumerate(lengths.clamp(0, 200).tolist()):
+        assert not got[2][i, n:].any() and not got[3][i, n:].any()
+        if n == 0:
+            assert not got[0][i].any() and not got[1][i].any()
+
+
+def test_not_finite():
+    """NaN in a query is that query's alone."""
+    print("[attention] not finite", flush=True)
+    q, k, v, _ = inputs(1, 50, 60, 2, 1, 32, torch.float32)
+    want = attention(q, k, v)
+    q[0, 7, 1, 3] = math.nan
+    got = attention(q, k, v)
+    assert bool(got[0, 7, 1].isnan().all())
+    got[0, 7, 1] = want[0, 7, 1]
+    assert torch.equal(got, want)
+    k[0, 5, 0, 0] = math.nan
+    assert bool(attention(q, k, v).isnan().all())
+
+
+def test_empty():
+    print("[attention] empty", flush=True)
+    for b, sq, sk in ((0, 3, 4), (2, 0, 4), (2, 3, 0), (0, 0, 0)):
+        got = run(*inputs(b, sq, sk, 4, 2, 64, torch.bfloat16), causal=True)
+        assert [t.shape for t in got] == [(b, sq, 4, 64)] * 2 + [(b, sk, 2, 64)] * 2
+        assert not any(t.any() for t in got)
+
+
+def test_same_bits():
+    """Of calls alike, and of a sequence alone and in a batch."""
+    print("[attention] same bits", flush=True)
+    for dtype in TYPES.values():
+        given = inputs(3, 300, 300, 8, 2, 128, dtype)
+        first = run(*given, causal=True)
+        for _ in range(3):
+            assert all(torch.equal(a, b) for a, b in zip(run(*given, causal=True), first))
+        alone = run(*(t[1:2] for t in given), causal=True)
+        assert all(torch.equal(a, b[1:2]) for a, b in zip(alone, first))
+
+
+@pytest.mark.parametrize("types", TYPES)
+def test_against_differences(types):
+    """Central differences of the binary64 formula at a step of 2^-10 (third
+    derivatives of O(10): 2^-17), beside the kernel's tolerance."""
+    print(f"[attention] differences {types}", flush=True)
+    q, k, v, dout = inputs(1, 9, 13, 2, 1, 16, TYPES[types])
+    got = run(q, k, v, dout, causal=True)
+    tolerance = reference(q, k, v, dout, True, None, 0.25, q.dtype)[1]
+    step = 2.0 ** -10
+    given = [t.cpu().double() for t in (q, k, v)]
+    for which in range(3):
+        for i in range(0, given[which].numel(), 37):
+            s = []
+            for sign in (1, -1):
+                moved = [t.clone() for t in given]
+                moved[which].view(-1)[i] += sign * step
+                out = reference(*moved, dout, True, None, 0.25, torch.float32)[0][0]
+                s.append(float((out * dout.cpu().double()).sum()))
+            want, g = (s[0] - s[1]) / (2 * step), float(got[1 + which].reshape(-1)[i])
+            half = 2.0 ** -24 if types == "f32" else 2.0 ** -8
+            assert abs(g - want) <= float(tolerance[1 + which].reshape(-1)[i]) + half * abs(want) * 1.01 + 2.0 ** -15
+
+
+def test_graph_and_streams():
+    print("[attention] graph", flush=True)
+    for sq, sk in ((150, 150), (1, 3000)):
+        q, k, v, dout = inputs(2, sq, sk, 4, 2, 64, torch.bfloat16)
+        lengths = torch.tensor([sk, sk // 3], dtype=torch.int32, device="cuda")
+        leaves = [t.clone().requires_grad_() for t in (q, k, v)]
+
+        def step():
+            out = attention(*leaves, causal=True, key_lengths=lengths)
+            with torch.no_grad():
+                again = attention(*leaves, causal=True, key_lengths=lengths)
+            return (out, *torch.autograd.grad(out, leaves, dout), again)
+
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            step()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            captured = step()
+        for seed in range(4):
+            given = inputs(2, sq, sk, 4, 2, 64, torch.bfloat16, seed=seed + 1)
+            with torch.no_grad():
+                for t, n in zip((*leaves, dout), given):
+                    t.copy_(n)
+                lengths.copy_(torch.tensor([sk - seed, seed], dtype=torch.int32))
+            graph.replay()
+            torch.cuda.synchronize()
+            eager = run(*given, causal=True, key_lengths=lengths)
+            assert all(torch.equal(a, b) for a, b in zip(captured, eager))
+            assert torch.equal(captured[4], attention(*given[:3], causal=True, key_lengths=lengths))
+
+
+def test_refusals():
+    print("[attention] refusals", flush=True)
+    q, k, v, _ = inputs(2, 5, 6, 4, 2, 32, torch.float32)
+    n = torch.tensor([3, 3], dtype=torch.int32, device="cuda")
+    for args, kind in (((q.half(), k.half(), v.half()), TypeError), ((q, k.bfloat16(), v), TypeError),
+                       ((q.cpu(), k.cpu(), v.cpu()), ValueError), ((q, k.cpu(), v), ValueError), ((q[0], k, v), ValueError),
+                       ((q, k, v[:, :5]), ValueError), ((q[:1], k, v), ValueError), ((q[..., :24], k, v), ValueError),
+                       ((q[:, :, :3], k, v), ma.MicroAdamError), ((q[..., :12], k[..., :12], v[..., :12]), ma.MicroAdamError),
+                       (inputs(1, 2, 2, 1, 1, 136, torch.float32)[:3], ma.MicroAdamError)):
+        with pytest.raises(kind):
+            attention(*args)
+    for bad, kind in ((n.long(), TypeError), (n[:1], ValueError), (n.cpu(), ValueError)):
+        with pytest.raises(kind):
+            attention(q, k, v, key_lengths=bad)
+    for scale in (0.0, -1.0, math.nan, math.inf, 1e39, 1e-46):
+        with pytest.raises(ma.MicroAdamError):
+            attention(q, k, v, scale=scale)
+    leaf = q.clone().requires_grad_()
+    out = attention(leaf, k, v)
+    (g,) = torch.autograd.grad(out, leaf, torch.ones_like(out), create_graph=True)
+    with pytest.raises(RuntimeError):
+        g.sum().backward()
+    import torch.autograd.forward_ad as forward_ad
+    with forward_ad.dual_level(), pytest.raises(NotImplementedError):
+        attention(forward_ad.make_dual(q, q), k, v)
+    for change in (0, 1):
+        out = attention(leaf * 1.0, k, v)
+        if change:
+            with torch.no_grad():
+                out.mul_(2.0)
+            with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+                out.sum().backward()
