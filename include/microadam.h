@@ -597,8 +597,8 @@ int microadam_layer_norm_grad(const microadam_rows* rows, const float* mean, con
  * binary32 operands are multiplied in binary32.
  *
  * An operand is addressed by the elements from sequence to sequence, position
- * to position and head to head (>= 0, at most 2^40; addresses are aligned to
- * the element type); the elements of dim are contiguous.  What is written has
+ * to position (dim to 2^23) and head to head (>= 0, at most 2^40; addresses are
+ * aligned to the element type); the elements of dim are contiguous.  What is written has
  * no two elements in one place, and shares no byte with what is read.
  */
 typedef struct microadam_heads {

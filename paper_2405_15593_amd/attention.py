@@ -31,8 +31,10 @@ def _on(device):
     return _HERE if device.index == torch.cuda.current_device() else torch.cuda.device(device)
 
 
-def _contiguous_dim(t: torch.Tensor) -> torch.Tensor:
-    return t if t.stride(-1) == 1 else t.contiguous()
+def _rows(t: torch.Tensor) -> torch.Tensor:
+    """t, or a copy where its rows are not contiguous or share elements."""
+    _, pos, _, one = t.stride()
+    return t if one == 1 and (pos >= t.shape[3] or t.shape[1] <= 1) else t.contiguous()
 
 
 def _heads(t: torch.Tensor) -> microadam_heads:
@@ -88,7 +90,7 @@ def _forward(q, k, v, key_lengths, causal, scale, keep):
 class _Attention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, key_lengths, causal, scale):
-        out, lse = _forward(*(_contiguous_dim(t) for t in (q, k, v)), key_lengths, causal, scale, True)
+        out, lse = _forward(*(_rows(t) for t in (q, k, v)), key_lengths, causal, scale, True)
         ctx.save_for_backward(q, k, v, key_lengths, out, lse)
         ctx.settings = (causal, scale)
         return out
@@ -98,7 +100,7 @@ class _Attention(torch.autograd.Function):
     def backward(ctx, dout):
         q, k, v, key_lengths, out, lse = ctx.saved_tensors
         causal, scale = ctx.settings
-        q, k, v, dout = (_contiguous_dim(t) for t in (q, k, v, dout))
+        q, k, v, dout = (_rows(t) for t in (q, k, v, dout))
         dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
         given = _struct(q, k, v, key_lengths, causal, scale)
         with _on(q.device):
@@ -126,4 +128,4 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, causal: bool
         key_lengths = key_lengths.contiguous()
     if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad):
         return _Attention.apply(q, k, v, key_lengths, causal, float(scale))
-    return _forward(*(_contiguous_dim(t) for t in (q, k, v)), key_lengths, causal, float(scale), False)[0]
+    return _forward(*(_rows(t) for t in (q, k, v)), key_lengths, causal, float(scale), False)[0]

@@ -18,6 +18,7 @@ namespace {
 
 constexpr int64_t kMaxSide = (int64_t)1 << 30;     // queries of a key head's query heads, keys
 constexpr int64_t kMaxStride = (int64_t)1 << 40;
+constexpr int64_t kMaxPosition = (int64_t)1 << 23;  // a tile's 64 rows are reached by 31 bits of bytes
 constexpr int64_t kMaxGroups = (int64_t)1 << 30;   // workgroups
 constexpr uint64_t kAlign = 256;
 
@@ -76,7 +77,12 @@ int operand(const microadam_heads* h, int64_t batch, int64_t positions, int64_t 
   if (!h->data) return report(MICROADAM_ERR_INVALID_ARG, "an operand's address is NULL");
   if ((uintptr_t)h->data % size_of(dtype))
     return report(MICROADAM_ERR_INVALID_ARG, "an operand is not aligned to its element type");
+  if (positions == 1) to.pos = dim;
   std::pair<int64_t, int64_t> d[3] = {{h->batch_stride, batch}, {h->pos_stride, positions}, {h->head_stride, heads}};
+  if (positions > 1 && h->pos_stride >= 0 && h->pos_stride < dim)
+    return report(MICROADAM_ERR_INVALID_ARG, "a position stride is below dim");
+  if (positions > 1 && h->pos_stride > kMaxPosition)
+    return report(MICROADAM_ERR_UNSUPPORTED, "a position stride is above 2^23");
   int64_t reach = dim;
   for (const auto& s : d) {
     if (s.second == 1) continue;

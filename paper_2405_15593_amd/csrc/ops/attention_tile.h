@@ -29,6 +29,8 @@ typedef __attribute__((address_space(3))) short4v* lds_short4;
 
 __device__ inline float infinity() { return __uint_as_float(0x7f800000u); }
 __device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+// All loads are back: the loop after it waits for its own alone.
+__device__ inline void wait_all() { __builtin_amdgcn_s_waitcnt(0); }
 __device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
 template <bool BF16>
@@ -144,31 +146,39 @@ struct Tile {
   }
 };
 
-// A tile on its way from memory to LDS through THREADS threads' registers.
+// A tile on its way from memory to LDS through THREADS threads' registers: rows
+// of one head, `pos` bytes apart.  The buffer's size ends with the last row that
+// there is, so that rows past it read as zeros without a branch.
 template <bool BF16, int D, int ROWS, int THREADS>
 struct Staged {
   typedef Tile<BF16, D, ROWS> T;
-  typedef Elements<BF16> E;
   static constexpr int kCount = (ROWS * T::kChunks + THREADS - 1) / THREADS;
+  static constexpr bool kEven = ROWS * T::kChunks % THREADS == 0;
   uint4v q[kCount];
+  uint32_t from[kCount];
 
-  // `at(row)`: a row's first element, negative where there is no such row.
-  template <class F>
-  __device__ void load(const void* base, int dim, int thread, F at) {
+  __device__ void start(int dim, int pos, int thread) {
 #pragma unroll
     for (int i = 0; i < kCount; ++i) {
       const int n = thread + i * THREADS, row = n / T::kChunks, chunk = n % T::kChunks;
-      q[i] = uint4v{0, 0, 0, 0};
-      if (ROWS * T::kChunks % THREADS != 0 && row >= ROWS) continue;
-      const int64_t from = at(row);
-      if (from >= 0 && chunk * E::kPer < dim) q[i] = E::load(base, from + chunk * E::kPer);
+      // (2^31: past the end of any tile)
+      from[i] = row < ROWS && chunk * (16 / T::kSize) < dim ? (uint32_t)(row * pos + chunk * 16) : 0x80000000u;
     }
+  }
+  // The rows [first, first + ROWS) of which those below `end` are there.
+  __device__ void load(const void* base, int64_t pos, int dim, int first, int end) {
+    const int rows = end - first < ROWS ? end - first : ROWS;
+    const int bytes = rows > 0 ? (rows - 1) * (int)pos + dim * T::kSize : 0;
+    const auto buffer =
+        __builtin_amdgcn_make_buffer_rsrc((void*)((const uint8_t*)base + first * pos), 0, bytes, 0x00020000);
+#pragma unroll
+    for (int i = 0; i < kCount; ++i) q[i] = __builtin_amdgcn_raw_buffer_load_b128(buffer, (int)from[i], 0, 0);
   }
   __device__ void store(uint8_t* tile, int thread) const {
 #pragma unroll
     for (int i = 0; i < kCount; ++i) {
       const int n = thread + i * THREADS, row = n / T::kChunks, chunk = n % T::kChunks;
-      if (ROWS * T::kChunks % THREADS != 0 && row >= ROWS) continue;
+      if (!kEven && row >= ROWS) continue;
       *(uint4v*)(tile + T::place(row, chunk)) = q[i];
     }
   }

@@ -40,8 +40,14 @@ __device__ inline void mask(float16v (&s)[N], int first, int limit, int lane, fl
     for (int r = 0; r < 16; ++r) s[i][r] = first + 32 * i + 8 * (r / 4) + 4 * h + r % 4 < limit ? s[i][r] : with;
 }
 
-// The running maximum (in units of ln 2) and the lane's part of the sum, and
-// out^T: a tile's scores and values added.
+// out^T += v^T p^T of a tile, with the running maximum m (in units of ln 2) and
+// the lane's part l of the sum.  m follows a row's maximum only where that is
+// more than kAhead above it: the probabilities' common factor cancels, and most
+// tiles pass without a factor for sum and output.  Each row decides for itself
+// (its factor is 1 where another row's is not), so that no row's bits go by its
+// neighbours.
+constexpr float kAhead = 8.0f;
+
 template <bool BF16, int D, int KEYS>
 __device__ inline void add_tile(float16v (&s)[KEYS / 32], const uint8_t* values, float c, float& m, float& l,
                                 float16v (&out)[D / 32], int lane) {
@@ -50,22 +56,24 @@ __device__ inline void add_tile(float16v (&s)[KEYS / 32], const uint8_t* values,
   for (int i = 0; i < KEYS / 32; ++i)
 #pragma unroll
     for (int r = 0; r < 16; ++r) top = fmaxf(top, s[i][r]);
-  top = fmaxf(top, __shfl_xor(top, 32));
-  const float next = fmaxf(m, top * c), from = next == -infinity() ? 0.0f : next;
-  const float factor = exp2_fast(m - from);
-  m = next;
-  l *= factor;
+  top = fmaxf(top, __shfl_xor(top, 32)) * c;
+  const bool ahead = top > m + kAhead;  // (of -infinity: any score)
+  if (__any(ahead)) {
+    const float next = ahead ? top : m;
+    const float factor = ahead ? exp2_fast(m - next) : 1.0f;
+    m = next;
+    l *= factor;
 #pragma unroll
-  for (int i = 0; i < D / 32; ++i) out[i] *= factor;
-#pragma unroll
-  for (int i = 0; i < KEYS / 32; ++i)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      s[i][r] = exp2_fast(__builtin_fmaf(s[i][r], c, -from));
-      l += s[i][r];
-    }
+    for (int i = 0; i < D / 32; ++i) out[i] *= factor;
+  }
+  const float from = m == -infinity() ? 0.0f : -m;
 #pragma unroll
   for (int i = 0; i < KEYS / 32; ++i) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      s[i][r] = exp2_fast(__builtin_fmaf(s[i][r], c, from));
+      l += s[i][r];
+    }
     const Frag<BF16> p0 = as_frag<BF16, 0>(s[i]), p1 = as_frag<BF16, 1>(s[i]);
 #pragma unroll
     for (int part = 0; part < D / 32; ++part) {
@@ -76,7 +84,7 @@ __device__ inline void add_tile(float16v (&s)[KEYS / 32], const uint8_t* values,
 }
 
 template <bool BF16, int D>
-__global__ __launch_bounds__(kThreads, 1) void attention_kernel(const AttentionArgs a) {
+__global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attention_kernel(const AttentionArgs a) {
   constexpr int keys = kKeys<BF16>;
   typedef Tile<BF16, D, keys> T;
   __shared__ __align__(16) uint8_t lds[2][2][T::kBytes];  // [turn][keys, values]
@@ -111,13 +119,15 @@ __global__ __launch_bounds__(kThreads, 1) void attention_kernel(const AttentionA
   const int turns = (end + keys - 1) / keys;
 
   Staged<BF16, D, keys, kThreads> next_k, next_v;
-  const int64_t k_at = batch * a.k.batch + kv_head * a.k.head, v_at = batch * a.v.batch + kv_head * a.v.head;
+  constexpr int size = T::kSize;
+  const int64_t k_pos = a.k.pos * size, v_pos = a.v.pos * size;
+  const uint8_t* k_at = (const uint8_t*)a.k.at + (batch * a.k.batch + kv_head * a.k.head) * size;
+  const uint8_t* v_at = (const uint8_t*)a.v.at + (batch * a.v.batch + kv_head * a.v.head) * size;
+  next_k.start(a.dim, (int)k_pos, threadIdx.x);
+  next_v.start(a.dim, (int)v_pos, threadIdx.x);
   auto load = [&](int turn) {
-    const int first = turn * keys;
-    next_k.load(a.k.at, a.dim, threadIdx.x,
-                [&](int r) { return first + r < length ? k_at + (first + r) * a.k.pos : (int64_t)-1; });
-    next_v.load(a.v.at, a.dim, threadIdx.x,
-                [&](int r) { return first + r < length ? v_at + (first + r) * a.v.pos : (int64_t)-1; });
+    next_k.load(k_at, k_pos, a.dim, turn * keys, length);
+    next_v.load(v_at, v_pos, a.dim, turn * keys, length);
   };
   auto store = [&](int turn) {
     next_k.store(lds[turn & 1][0], threadIdx.x);
@@ -132,6 +142,7 @@ __global__ __launch_bounds__(kThreads, 1) void attention_kernel(const AttentionA
     load(0);
     store(0);
   }
+  wait_all();
   __syncthreads();
   for (int turn = 0; turn < turns; ++turn) {
     if (turn + 1 < turns) load(turn + 1);

@@ -19,7 +19,7 @@ constexpr int kRows = 128;      // of a workgroup, rows or keys
 constexpr int kTile = 32;       // keys or rows of a tile
 
 template <bool BF16, int D>
-__global__ __launch_bounds__(kThreads, 1) void attention_dq_kernel(const AttentionArgs a) {
+__global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attention_dq_kernel(const AttentionArgs a) {
   typedef Tile<BF16, D, kTile> T;
   __shared__ __align__(16) uint8_t lds[2][2][T::kBytes];  // [turn][keys, values]
   const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
@@ -63,13 +63,15 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dq_kernel(const Attenti
   const int turns = (end + kTile - 1) / kTile;
 
   Staged<BF16, D, kTile, kThreads> next_k, next_v;
-  const int64_t k_at = batch * a.k.batch + kv_head * a.k.head, v_at = batch * a.v.batch + kv_head * a.v.head;
+  constexpr int size = T::kSize;
+  const int64_t k_pos = a.k.pos * size, v_pos = a.v.pos * size;
+  const uint8_t* k_at = (const uint8_t*)a.k.at + (batch * a.k.batch + kv_head * a.k.head) * size;
+  const uint8_t* v_at = (const uint8_t*)a.v.at + (batch * a.v.batch + kv_head * a.v.head) * size;
+  next_k.start(a.dim, (int)k_pos, threadIdx.x);
+  next_v.start(a.dim, (int)v_pos, threadIdx.x);
   auto load = [&](int turn) {
-    const int first = turn * kTile;
-    next_k.load(a.k.at, a.dim, threadIdx.x,
-                [&](int r) { return first + r < length ? k_at + (first + r) * a.k.pos : (int64_t)-1; });
-    next_v.load(a.v.at, a.dim, threadIdx.x,
-                [&](int r) { return first + r < length ? v_at + (first + r) * a.v.pos : (int64_t)-1; });
+    next_k.load(k_at, k_pos, a.dim, turn * kTile, length);
+    next_v.load(v_at, v_pos, a.dim, turn * kTile, length);
   };
   auto store = [&](int turn) {
     next_k.store(lds[turn & 1][0], threadIdx.x);
@@ -83,6 +85,7 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dq_kernel(const Attenti
     load(0);
     store(0);
   }
+  wait_all();
   __syncthreads();
   for (int turn = 0; turn < turns; ++turn) {
     if (turn + 1 < turns) load(turn + 1);
@@ -121,11 +124,10 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dq_kernel(const Attenti
 }
 
 template <bool BF16, int D>
-__global__ __launch_bounds__(kThreads, 1) void attention_dkv_kernel(const AttentionArgs a) {
+__global__ __launch_bounds__(kThreads, BF16 && D < 128 ? 2 : 1) void attention_dkv_kernel(const AttentionArgs a) {
   typedef Tile<BF16, D, kTile> T;
   __shared__ __align__(16) uint8_t lds[2][2][T::kBytes];  // [turn][queries, dout]
   __shared__ float lses[2][kTile], deltas[2][kTile];
-  __shared__ int limits[2][kTile];
   const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), h = lane >> 5;
   const int tiles = (a.keys + kRows - 1) / kRows;
   const int work = run_of_xcd(blockIdx.x, gridDim.x);
@@ -145,48 +147,41 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dkv_kernel(const Attent
     v[s] = load_frag<BF16>(a.v.at, v_at + d, live && d < a.dim);
   }
 
-  // the first query that sees one of the workgroup's keys
+  // The query heads one after the other, each from the first tile of queries
+  // that see one of the workgroup's keys.
   int from = 0;
   if (a.causal) {
     from = key0 - (a.keys - a.queries);
-    from = from < 0 ? 0 : from;
+    from = (from < 0 ? 0 : from) / kTile;
   }
-  const int turns = key0 < length && from < a.queries ? (a.rows + kTile - 1) / kTile : 0;
-  // the first turn from `turn` on with a row that sees a key
-  auto seen = [&](int turn) {
-    if (from == 0) return turn;
-    while (turn < turns) {
-      const int first = turn * kTile, last = first + kTile < a.rows ? first + kTile - 1 : a.rows - 1;
-      if (first % a.queries + (last - first) >= from) break;  // (rows of two heads: past the last query)
-      ++turn;
-    }
-    return turn;
-  };
+  const int of_head = (a.queries + kTile - 1) / kTile - from;
+  const int turns = key0 < length && of_head > 0 ? of_head * a.group : 0;
 
   Staged<BF16, D, kTile, kThreads> next_q, next_do;
   float next_lse = 0.0f, next_delta = 0.0f;
-  int next_limit = 0;
-  const int64_t q_at = batch * a.q.batch, do_at = batch * a.dout.batch;
-  auto load = [&](int turn) {
-    const int first = turn * kTile;
-    next_q.load(a.q.at, a.dim, threadIdx.x, [&](int r) {
-      if (first + r >= a.rows) return (int64_t)-1;
-      const RowAt at = row_at(a, kv_head, first + r);
-      return q_at + at.head * a.q.head + at.query * a.q.pos;
-    });
-    next_do.load(a.dout.at, a.dim, threadIdx.x, [&](int r) {
-      if (first + r >= a.rows) return (int64_t)-1;
-      const RowAt at = row_at(a, kv_head, first + r);
-      return do_at + at.head * a.dout.head + at.query * a.dout.pos;
-    });
+  constexpr int size = T::kSize;
+  const int64_t q_pos = a.q.pos * size, do_pos = a.dout.pos * size;
+  next_q.start(a.dim, (int)q_pos, threadIdx.x);
+  next_do.start(a.dim, (int)do_pos, threadIdx.x);
+  const uint8_t *q_at = (const uint8_t*)a.q.at + (batch * a.q.batch + (int64_t)kv_head * a.group * a.q.head) * size,
+                *do_at = (const uint8_t*)a.dout.at +
+                         (batch * a.dout.batch + (int64_t)kv_head * a.group * a.dout.head) * size;
+  int64_t stat = ((int64_t)batch * a.heads + kv_head * a.group) * a.queries;
+  int next_tile = from;  // of the head, of what is loaded next
+  auto load = [&]() {
+    const int first = next_tile * kTile;
+    next_q.load(q_at, q_pos, a.dim, first, a.queries);
+    next_do.load(do_at, do_pos, a.dim, first, a.queries);
     if (threadIdx.x < kTile) {
-      const int r = first + threadIdx.x;
-      const bool there = r < a.rows;
-      const RowAt at = row_at(a, kv_head, there ? r : 0);
-      const int64_t stat = ((int64_t)batch * a.heads + at.head) * a.queries + at.query;
-      next_lse = there ? a.lse[stat] : infinity();
-      next_delta = there ? a.delta[stat] : 0.0f;
-      next_limit = there ? limit_of(a, at.query, length) : 0;
+      const int query = first + threadIdx.x;
+      next_lse = query < a.queries ? a.lse[stat + query] : infinity();
+      next_delta = query < a.queries ? a.delta[stat + query] : 0.0f;
+    }
+    if (++next_tile == from + of_head) {
+      next_tile = from;
+      q_at += a.q.head * size;
+      do_at += a.dout.head * size;
+      stat += a.queries;
     }
   };
   auto store = [&](int place) {
@@ -195,22 +190,21 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dkv_kernel(const Attent
     if (threadIdx.x < kTile) {
       lses[place][threadIdx.x] = next_lse;
       deltas[place][threadIdx.x] = next_delta;
-      limits[place][threadIdx.x] = next_limit;
     }
   };
 
   float16v dk[D / 32], dv[D / 32];
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) dk[i] = dv[i] = zeros();
-  int turn = seen(0), place = 0;
-  if (turn < turns) {
-    load(turn);
+  if (turns > 0) {
+    load();
     store(0);
   }
+  wait_all();
   __syncthreads();
-  while (turn < turns) {
-    const int next = seen(turn + 1);
-    if (next < turns) load(next);
+  int in_head = from, place = 0;
+  for (int turn = 0; turn < turns; ++turn) {
+    if (turn + 1 < turns) load();
     const uint8_t *queries = lds[place][0], *douts = lds[place][1];
     {
       float16v s = zeros(), dp = zeros();
@@ -225,9 +219,12 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dkv_kernel(const Attent
 #pragma unroll
         for (int i = 0; i < 4; ++i) s[4 * g + i] = exp2_fast(__builtin_fmaf(s[4 * g + i], a.c, -lse[i]));
       }
-      if (a.causal) {
+      // the tile's first query does not see the wave's last key
+      const int hidden = wave_key + 31 - (in_head * kTile + a.keys - a.queries);
+      if (a.causal && hidden > 0) {
+        const int at = (lane & 31) - 31 + hidden - 4 * h;  // rows below it do not see the lane's key
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = key < limits[place][8 * (r / 4) + 4 * h + r % 4] ? s[r] : 0.0f;
+        for (int r = 0; r < 16; ++r) s[r] = 8 * (r / 4) + r % 4 < at ? 0.0f : s[r];
       }
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
@@ -245,9 +242,9 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dkv_kernel(const Attent
         multiply(dk[part], T::across(queries, 16, part, lane), d1);
       }
     }
-    if (next < turns) store(place ^ 1);
+    if (turn + 1 < turns) store(place ^ 1);
     __syncthreads();
-    turn = next;
+    if (++in_head == from + of_head) in_head = from;
     place ^= 1;
   }
   if (key >= a.keys) return;

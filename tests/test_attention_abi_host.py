@@ -73,7 +73,8 @@ def test_sizes(kw, code):
 @pytest.mark.parametrize("name,positions,count,at", [("q", SQ, H, Q), ("k", SK, HK, K), ("v", SK, HK, V)])
 @pytest.mark.parametrize("kw,code", [
     (dict(data=None), INVALID), (dict(data=Q + 2), INVALID), (dict(batch_stride=-1), INVALID),
-    (dict(pos_stride=-16), INVALID), (dict(head_stride=-1), INVALID), (dict(pos_stride=(1 << 40) + 1), UNSUPPORTED)],
+    (dict(pos_stride=-16), INVALID), (dict(head_stride=-1), INVALID), (dict(pos_stride=(1 << 23) + 1), UNSUPPORTED),
+    (dict(pos_stride=15), INVALID), (dict(pos_stride=0), INVALID), (dict(head_stride=(1 << 40) + 1), UNSUPPORTED)],
     ids=str)
 def test_inputs(name, positions, count, at, kw, code):
     if kw.get("data"):
@@ -85,7 +86,7 @@ def test_inputs(name, positions, count, at, kw, code):
 
 def test_inputs_with_shared_elements_are_allowed():
     """Where nothing is written, strides may be zero: up to the next refusal."""
-    a = given(k=heads(K, SK, HK, batch_stride=0, pos_stride=0, head_stride=0))
+    a = given(k=heads(K, SK, HK, batch_stride=0, head_stride=0))
     refused(INVALID, forward, a, lse=LSE + 2)
 
 
