@@ -58,7 +58,7 @@ int check(const microadam_attention* t, AttentionArgs& a) {
   a.scale = (float)t->scale;
   a.c = c;
   a.lengths = t->key_lengths;
-  attention_parts(a, a.parts, a.part_keys);
+  a.parts = attention_parts(a);
   return MICROADAM_OK;
 }
 

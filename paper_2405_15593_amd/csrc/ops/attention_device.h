@@ -28,11 +28,13 @@ struct AttentionArgs {
   // sum) and the unnormalised output
   float* part_out;    // [batch][kv_heads][parts][rows][dim]
   float* part_stats;  // [batch][kv_heads][parts][rows][2]
-  int32_t parts, part_keys;
+  int32_t parts;      // 0: not split
 };
 
-// How a forward call is split: 0 parts: by rows alone.
-void attention_parts(const AttentionArgs& a, int32_t& parts, int32_t& part_keys);
+constexpr int kMostParts = 256;
+
+// How many parts a forward call's keys are split into; 0: not at all.
+int32_t attention_parts(const AttentionArgs& a);
 
 hipError_t launch_attention(const AttentionArgs& a, hipStream_t s);
 hipError_t launch_attention_grad(const AttentionArgs& a, hipStream_t s);

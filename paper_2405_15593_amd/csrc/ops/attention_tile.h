@@ -31,7 +31,32 @@ __device__ inline float infinity() { return __uint_as_float(0x7f800000u); }
 __device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 // All loads are back: the loop after it waits for its own alone.
 __device__ inline void wait_all() { __builtin_amdgcn_s_waitcnt(0); }
+// What a wave's lanes wrote to LDS before is there for its other lanes after (a
+// wave's accesses to LDS are done in order; this keeps the compiler to it).
+__device__ inline void wave_order() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
 __device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// The order of the instructions since the last scheduling barrier: AHEAD reads
+// from LDS, then with each of the matrix instructions EACH more of what is left
+// of READS, and WORK vector operations.  A read is then on its way for some
+// instructions before its data is used; left to itself the compiler reads a
+// fragment, waits and multiplies.
+template <int AHEAD, int READS, int MFMAS, int EACH = 1, int WORK = 0>
+__device__ inline void interleave() {
+  int left = READS - AHEAD;
+  if (AHEAD > 0) __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
+#pragma unroll
+  for (int i = 0; i < MFMAS; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    if (WORK > 0) __builtin_amdgcn_sched_group_barrier(0x002, WORK, 0);
+    if (left > 0) __builtin_amdgcn_sched_group_barrier(0x100, EACH, 0);
+    left -= EACH;
+  }
+}
+__device__ inline void schedule_here() { __builtin_amdgcn_sched_barrier(0); }
 
 template <bool BF16>
 struct Frag;
@@ -106,16 +131,33 @@ struct Tile {
 
   __device__ static int place(int row, int chunk) { return row * kStride + ((chunk ^ ((row >> 2) & 3)) << 4); }
 
-  // Row m = lane % 32 (of rows from `row`), elements 16 step + 8 (lane / 32) + j.
-  __device__ static Frag<BF16> along(const uint8_t* tile, int row, int step, int lane) {
-    const int r = row + (lane & 31), h = lane >> 5;
+  // What a lane adds to a tile's address for the reads below; the rest of their
+  // places is the same for all lanes.
+  struct Lane {
+    int along[2], across[2];
+    __device__ explicit Lane(int lane) {
+      const int r = lane & 31, h = lane >> 5;
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        along[u] = place(r, BF16 ? 2 * u + h : 2 * h + u);
+        // (sixteen lanes address four rows' four times four elements, and
+        // receive one element of four rows each)
+        across[u] = BF16 ? place(8 * u + 4 * h + ((lane & 15) >> 2), 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) + (lane & 1) * 8
+                         : place(8 * u + 4 * h, r >> 2) + (r & 3) * 4;
+      }
+    }
+  };
+
+  // Row lane % 32 of the rows from `row` on (a multiple of 16), elements 16 step
+  // + 8 (lane / 32) + j.
+  __device__ static Frag<BF16> along(const uint8_t* tile, const Lane& at, int row, int step) {
     Frag<BF16> f;
     if constexpr (BF16) {
-      f.v = __builtin_bit_cast(bf16x8, *(const uint4v*)(tile + place(r, 2 * step + h)));
+      f.v = __builtin_bit_cast(bf16x8, *(const uint4v*)(tile + at.along[step & 1] + (row * kStride + (step >> 1) * 64)));
     } else {
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const float4v q = *(const float4v*)(tile + place(r, 4 * step + 2 * h + u));
+        const float4v q = *(const float4v*)(tile + at.along[u] + (row * kStride + step * 64));
 #pragma unroll
         for (int i = 0; i < 4; ++i) f.v[4 * u + i] = q[i];
       }
@@ -124,23 +166,17 @@ struct Tile {
   }
 
   // Element 32 part + lane % 32 of rows row + 8 (j / 4) + 4 (lane / 32) + j % 4.
-  __device__ static Frag<BF16> across(const uint8_t* tile, int row, int part, int lane) {
-    const int h = lane >> 5;
+  __device__ static Frag<BF16> across(const uint8_t* tile, const Lane& at, int row, int part) {
     Frag<BF16> f;
     if constexpr (BF16) {
-      // sixteen lanes address four rows' four times four elements, and receive
-      // one element of four rows each
-      const int r = row + 4 * h + ((lane & 15) >> 2), chunk = 4 * part + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-      const uint8_t* lo = tile + place(r, chunk) + (lane & 1) * 8;
-      const uint8_t* hi = tile + place(r + 8, chunk) + (lane & 1) * 8;
-      const short4v a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4)lo);
-      const short4v b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4)hi);
+      const uint8_t* p = tile + (row * kStride + part * 64);
+      const short4v a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4)(p + at.across[0]));
+      const short4v b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4)(p + at.across[1]));
       f.v = __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
     } else {
-      const int d = 32 * part + (lane & 31);
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        f.v[j] = *(const float*)(tile + place(row + 8 * (j / 4) + 4 * h + j % 4, d >> 2) + (d & 3) * 4);
+        f.v[j] = *(const float*)(tile + at.across[j / 4] + ((row + j % 4) * kStride + part * 128));
     }
     return f;
   }
@@ -208,11 +244,30 @@ __device__ inline void store_column(void* p, int64_t at, int left, const float16
   }
 }
 
-// Workgroups go to the eight XCDs in turn: each XCD takes one run of the work,
-// so that the tiles of a head share their keys (or queries) in its L2.
-__device__ inline int run_of_xcd(int block, int total) {
-  const int xcd = block & 7, each = total >> 3, more = total & 7;
-  return xcd * each + (xcd < more ? xcd : more) + (block >> 3);
+// The value of the lane 32 away joined with one's own (a lane and that one hold
+// the halves of a column).
+__device__ inline float max_halves(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ inline float add_halves(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// Which tile (by its work, the largest first) of which head (of all sequences') a
+// workgroup takes.  Workgroups go to the eight XCDs in turn: where the heads are
+// a multiple of eight a head's tiles stay on one, in whose L2 they find its keys
+// (or queries).  The longest go first, of all heads: a long one that starts last
+// would be waited for (causal, 64 heads of 32 tiles, head by head: 20% of the
+// time the average CU had nothing to do).
+struct Work {
+  int order, head;
+};
+__device__ inline Work work_of(int block, int heads) {
+  if (heads % 8) return {block / heads, block % heads};
+  const int per = heads / 8, n = block >> 3;
+  return {n / per, (block & 7) * per + n % per};
 }
 
 // A row of the rows that share a key head: its query head and query.
@@ -235,6 +290,14 @@ __device__ inline int limit_of(const AttentionArgs& a, int query, int length) {
   if (!a.causal) return length;
   const int n = query + 1 + a.keys - a.queries;
   return n < 0 ? 0 : n < length ? n : length;
+}
+
+// How many of the first keys the rows [first, first + count) see together.
+__device__ inline int last_key(const AttentionArgs& a, int first, int count, int length) {
+  const int last = first + count < a.rows ? first + count - 1 : a.rows - 1;
+  // rows of two heads: the last query is among them
+  const bool two = first / a.queries != last / a.queries;
+  return limit_of(a, two ? a.queries - 1 : last % a.queries, length);
 }
 
 __device__ inline int wave_min(int x) {

@@ -20,15 +20,20 @@ constexpr int kRows = 128;  // of a workgroup
 template <bool BF16>
 constexpr int kKeys = BF16 ? 64 : 32;  // of a tile
 
-// z^T of a tile, masked by the lane's limit where asked.
+// z^T of a tile.
 template <bool BF16, int D, int KEYS>
-__device__ inline void scores(float16v (&s)[KEYS / 32], const uint8_t* tile, const Frag<BF16> (&q)[D / 16], int lane) {
+__device__ inline void scores(float16v (&s)[KEYS / 32], const uint8_t* tile, const typename Tile<BF16, D, KEYS>::Lane& at,
+                              const Frag<BF16> (&q)[D / 16]) {
+  constexpr int n = KEYS / 32;
+  schedule_here();
 #pragma unroll
-  for (int i = 0; i < KEYS / 32; ++i) s[i] = zeros();
+  for (int i = 0; i < n; ++i) s[i] = zeros();
 #pragma unroll
   for (int step = 0; step < D / 16; ++step)
 #pragma unroll
-    for (int i = 0; i < KEYS / 32; ++i) multiply(s[i], Tile<BF16, D, KEYS>::along(tile, 32 * i, step, lane), q[step]);
+    for (int i = 0; i < n; ++i) multiply(s[i], Tile<BF16, D, KEYS>::along(tile, at, 32 * i, step), q[step]);
+  if (BF16) interleave<4, D / 16 * n, D / 16 * n>();
+  schedule_here();
 }
 
 template <int N>
@@ -49,14 +54,15 @@ __device__ inline void mask(float16v (&s)[N], int first, int limit, int lane, fl
 constexpr float kAhead = 8.0f;
 
 template <bool BF16, int D, int KEYS>
-__device__ inline void add_tile(float16v (&s)[KEYS / 32], const uint8_t* values, float c, float& m, float& l,
-                                float16v (&out)[D / 32], int lane) {
+__device__ inline void add_tile(float16v (&s)[KEYS / 32], const uint8_t* values,
+                                const typename Tile<BF16, D, KEYS>::Lane& at, float c, float& m, float& l,
+                                float16v (&out)[D / 32]) {
   float top = s[0][0];
 #pragma unroll
   for (int i = 0; i < KEYS / 32; ++i)
 #pragma unroll
     for (int r = 0; r < 16; ++r) top = fmaxf(top, s[i][r]);
-  top = fmaxf(top, __shfl_xor(top, 32)) * c;
+  top = max_halves(top) * c;
   const bool ahead = top > m + kAhead;  // (of -infinity: any score)
   if (__any(ahead)) {
     const float next = ahead ? top : m;
@@ -67,20 +73,69 @@ __device__ inline void add_tile(float16v (&s)[KEYS / 32], const uint8_t* values,
     for (int i = 0; i < D / 32; ++i) out[i] *= factor;
   }
   const float from = m == -infinity() ? 0.0f : -m;
-#pragma unroll
-  for (int i = 0; i < KEYS / 32; ++i) {
+  typedef Tile<BF16, D, KEYS> T;
+  constexpr int n = KEYS / 32, parts = D / 32;
+  auto weights = [&](float16v& x) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      s[i][r] = exp2_fast(__builtin_fmaf(s[i][r], c, from));
-      l += s[i][r];
+      x[r] = exp2_fast(__builtin_fmaf(x[r], c, from));
+      l += x[r];
     }
+  };
+  Frag<BF16> v[2 * parts];
+  auto read = [&](int i) {
+#pragma unroll
+    for (int k = 0; k < 2 * parts; ++k) v[k] = T::across(values, at, 32 * i + 16 * (k % 2), k / 2);
+  };
+  schedule_here();
+  read(0);
+  weights(s[0]);
+  schedule_here();
+#pragma unroll
+  for (int i = 0; i < n; ++i) {
     const Frag<BF16> p0 = as_frag<BF16, 0>(s[i]), p1 = as_frag<BF16, 1>(s[i]);
 #pragma unroll
-    for (int part = 0; part < D / 32; ++part) {
-      multiply(out[part], Tile<BF16, D, KEYS>::across(values, 32 * i, part, lane), p0);
-      multiply(out[part], Tile<BF16, D, KEYS>::across(values, 32 * i + 16, part, lane), p1);
+    for (int part = 0; part < parts; ++part) {
+      multiply(out[part], v[2 * part], p0);
+      multiply(out[part], v[2 * part + 1], p1);
+    }
+    if (i + 1 < n) {
+      read(i + 1);
+      weights(s[i + 1]);
+      schedule_here();
     }
   }
+}
+
+// What a wave has of its rows when its keys are through (l the lanes' sum):
+// the result, or where the keys are split a part of it.
+template <bool BF16, int D>
+__device__ inline void finish(const AttentionArgs& a, int head_of, int batch, int row, const RowAt& at, int part, float m,
+                              float l, const float16v (&out)[D / 32], int lane) {
+  if (a.parts) {
+    const int64_t n = ((int64_t)head_of * a.parts + part) * a.rows + row;
+    if (lane < 32) *(float2v*)(a.part_stats + 2 * n) = float2v{m, l};
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+      store_column<false>(a.part_out, n * a.dim + 32 * i, a.dim - 32 * i, out[i], 1.0f, lane);
+    return;
+  }
+  const float over = l == 0.0f ? 0.0f : 1.0f / l;
+  const int64_t o_at = batch * a.out.batch + at.head * a.out.head + at.query * a.out.pos;
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) store_column<BF16>(a.out.at, o_at + 32 * i, a.dim - 32 * i, out[i], over, lane);
+  if (a.lse && lane < 32)
+    a.lse[((int64_t)batch * a.heads + at.head) * a.queries + at.query] =
+        l == 0.0f ? infinity() : m + __builtin_amdgcn_logf(l);
+}
+
+// The tiles [first, last) of a part of `tiles`.
+struct Part {
+  int first, last;
+};
+__device__ inline Part part_of(const AttentionArgs& a, int part, int tiles) {
+  if (!a.parts) return {0, tiles};
+  return {(int)((int64_t)part * tiles / a.parts), (int)((int64_t)(part + 1) * tiles / a.parts)};
 }
 
 template <bool BF16, int D>
@@ -90,9 +145,14 @@ __global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attention_kernel(const
   __shared__ __align__(16) uint8_t lds[2][2][T::kBytes];  // [turn][keys, values]
   const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
   const int tiles = (a.rows + kRows - 1) / kRows;
-  const int work = run_of_xcd(blockIdx.x, gridDim.x);
-  // (the last rows see the most keys: first)
-  const int tile = tiles - 1 - work % tiles, head_of = work / tiles;
+  int block = blockIdx.x, part = 0;
+  if (a.parts) {
+    part = block % a.parts;
+    block /= a.parts;
+  }
+  const Work work = work_of(block, a.kv_heads * a.batch);
+  const int tile = tiles - 1 - work.order, head_of = work.head;  // (the last rows see the most keys)
+  const typename T::Lane places(lane);
   const int kv_head = head_of % a.kv_heads, batch = head_of / a.kv_heads;
   const int length = keys_of(a, batch);
 
@@ -109,14 +169,7 @@ __global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attention_kernel(const
     q[s] = load_frag<BF16>(a.q.at, q_at + d, live && d < a.dim);
   }
 
-  // the workgroup's last key
-  int end;
-  {
-    const int first = tile * kRows, last = first + kRows < a.rows ? first + kRows - 1 : a.rows - 1;
-    const int whole = first / a.queries != last / a.queries;  // rows of two heads: the last query is among them
-    end = limit_of(a, whole ? a.queries - 1 : last % a.queries, length);
-  }
-  const int turns = (end + keys - 1) / keys;
+  const Part own = part_of(a, part, (last_key(a, tile * kRows, kRows, length) + keys - 1) / keys);
 
   Staged<BF16, D, keys, kThreads> next_k, next_v;
   constexpr int size = T::kSize;
@@ -138,40 +191,210 @@ __global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attention_kernel(const
   float16v out[D / 32];
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) out[i] = zeros();
-  if (turns > 0) {
-    load(0);
-    store(0);
+  if (own.first < own.last) {
+    load(own.first);
+    store(own.first);
   }
   wait_all();
   __syncthreads();
-  for (int turn = 0; turn < turns; ++turn) {
-    if (turn + 1 < turns) load(turn + 1);
+  for (int turn = own.first; turn < own.last; ++turn) {
+    if (turn + 1 < own.last) load(turn + 1);
     const int first = turn * keys;
     if (first < most) {
       float16v s[keys / 32];
-      scores<BF16, D, keys>(s, lds[turn & 1][0], q, lane);
+      scores<BF16, D, keys>(s, lds[turn & 1][0], places, q);
       if (first + keys > least) mask(s, first, limit, lane, -infinity());
-      add_tile<BF16, D, keys>(s, lds[turn & 1][1], a.c, m, l, out, lane);
+      add_tile<BF16, D, keys>(s, lds[turn & 1][1], places, a.c, m, l, out);
     }
-    if (turn + 1 < turns) store(turn + 1);
+    if (turn + 1 < own.last) store(turn + 1);
     __syncthreads();
   }
 
-  l += __shfl_xor(l, 32);
-  if (!live) return;
-  const float over = l == 0.0f ? 0.0f : 1.0f / l;
-  const int64_t o_at = batch * a.out.batch + at.head * a.out.head + at.query * a.out.pos;
+  l = add_halves(l);
+  if (live) finish<BF16, D>(a, head_of, batch, row, at, part, m, l, out, lane);
+}
+
+// Up to 32 rows of a key head, a token's or a few: the four waves take the same
+// rows and every fourth tile of the part's keys, each on its own way through its
+// own place in LDS, and are joined at the end.
+constexpr int kFewRows = 32, kFewKeys = 32;
+
+template <bool BF16, int D>
+__global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attention_few_kernel(const AttentionArgs a) {
+  typedef Tile<BF16, D, kFewKeys> T;
+  constexpr int kWaves = kThreads / 64;
+  constexpr int kSums = D / 32 * 16 + 2;  // floats that a lane hands over
+  __shared__ __align__(16) uint8_t lds[kWaves][2][T::kBytes];
+  static_assert((kWaves - 1) * kSums * 64 * sizeof(float) <= sizeof(lds), "the waves' sums");
+  const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
+  int head_of = blockIdx.x, part = 0;
+  if (a.parts) {
+    part = head_of % a.parts;
+    head_of /= a.parts;
+  }
+  const int kv_head = head_of % a.kv_heads, batch = head_of / a.kv_heads;
+  const int length = keys_of(a, batch);
+  const Part own = part_of(a, part, (last_key(a, 0, kFewRows, length) + kFewKeys - 1) / kFewKeys);
+
+  Staged<BF16, D, kFewKeys, 64> next_k, next_v;
+  constexpr int size = T::kSize;
+  const int64_t k_pos = a.k.pos * size, v_pos = a.v.pos * size;
+  const uint8_t* k_at = (const uint8_t*)a.k.at + (batch * a.k.batch + kv_head * a.k.head) * size;
+  const uint8_t* v_at = (const uint8_t*)a.v.at + (batch * a.v.batch + kv_head * a.v.head) * size;
+  next_k.start(a.dim, (int)k_pos, lane);
+  next_v.start(a.dim, (int)v_pos, lane);
+  int turn = own.first + wave;
+  auto load = [&](int t) {
+    next_k.load(k_at, k_pos, a.dim, t * kFewKeys, length);
+    next_v.load(v_at, v_pos, a.dim, t * kFewKeys, length);
+  };
+  if (turn < own.last) load(turn);
+
+  const int row = lane & 31;
+  const bool live = row < a.rows;
+  const RowAt at = row_at(a, kv_head, live ? row : 0);
+  const int limit = live ? limit_of(a, at.query, length) : 0;
+  const int least = wave_min(live ? limit : a.keys);
+  Frag<BF16> q[D / 16];
+  const int64_t q_at = batch * a.q.batch + at.head * a.q.head + at.query * a.q.pos;
 #pragma unroll
-  for (int i = 0; i < D / 32; ++i) store_column<BF16>(a.out.at, o_at + 32 * i, a.dim - 32 * i, out[i], over, lane);
-  if (a.lse && lane < 32)
+  for (int s = 0; s < D / 16; ++s) {
+    const int d = 16 * s + 8 * (lane >> 5);
+    q[s] = load_frag<BF16>(a.q.at, q_at + d, live && d < a.dim);
+  }
+  float m = -infinity(), l = 0.0f;
+  float16v out[D / 32];
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) out[i] = zeros();
+  wait_all();
+  uint8_t *keys = lds[wave][0], *values = lds[wave][1];
+  const typename T::Lane places(lane);
+  for (; turn < own.last; turn += kWaves) {
+    next_k.store(keys, lane);
+    next_v.store(values, lane);
+    if (turn + kWaves < own.last) load(turn + kWaves);
+    wave_order();
+    const int first = turn * kFewKeys;
+    float16v s[1];
+    scores<BF16, D, kFewKeys>(s, keys, places, q);
+    if (first + kFewKeys > least) mask(s, first, limit, lane, -infinity());
+    add_tile<BF16, D, kFewKeys>(s, values, places, a.c, m, l, out);
+    wave_order();
+  }
+  l = add_halves(l);
+
+  __syncthreads();
+  float* sums = (float*)&lds[0][0][0];
+  if (wave > 0) {
+    float* to = sums + (wave - 1) * kSums * 64 + lane;
+    to[0] = m;
+    to[64] = l;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) to[(2 + 16 * i + r) * 64] = out[i][r];
+  }
+  __syncthreads();
+  if (wave > 0 || !live) return;
+  float top = m;
+#pragma unroll
+  for (int w = 0; w < kWaves - 1; ++w) top = fmaxf(top, sums[w * kSums * 64 + lane]);
+  const float from = top == -infinity() ? 0.0f : top;
+  const float own_factor = exp2_fast(m - from);
+  l *= own_factor;
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) out[i] *= own_factor;
+#pragma unroll
+  for (int w = 0; w < kWaves - 1; ++w) {
+    const float* other = sums + w * kSums * 64 + lane;
+    const float factor = exp2_fast(other[0] - from);
+    l = __builtin_fmaf(other[64], factor, l);
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) out[i][r] = __builtin_fmaf(other[(2 + 16 * i + r) * 64], factor, out[i][r]);
+  }
+  finish<BF16, D>(a, head_of, batch, row, at, part, top, l, out, lane);
+}
+
+// The parts of a row's keys joined, a wave a row: lane i has the sums of parts
+// i, i + 64, .., then two elements of the row.
+template <bool BF16>
+__global__ __launch_bounds__(kThreads) void attention_join_kernel(const AttentionArgs a) {
+  constexpr int kEach = kMostParts / 64;
+  const int lane = threadIdx.x & 63;
+  const int64_t n = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
+  if (n >= (int64_t)a.batch * a.kv_heads * a.rows) return;
+  const int64_t head_of = n / a.rows;
+  const int row = (int)(n - head_of * a.rows);
+  const int batch = (int)(head_of / a.kv_heads);
+  const RowAt at = row_at(a, (int)(head_of % a.kv_heads), row);
+  const int64_t first = head_of * a.parts * a.rows + row;
+  float m[kEach], l[kEach], top = -infinity();
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const int part = 64 * i + lane;
+    const bool there = part < a.parts;
+    const float2v s = there ? *(const float2v*)(a.part_stats + 2 * (first + (int64_t)part * a.rows)) : float2v{0.0f, 0.0f};
+    m[i] = there ? s[0] : -infinity();
+    l[i] = s[1];
+    top = fmaxf(top, m[i]);
+  }
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+  const float from = top == -infinity() ? 0.0f : top;
+  float sum = 0.0f;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    m[i] = exp2_fast(m[i] - from);
+    sum = __builtin_fmaf(m[i], l[i], sum);
+  }
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+  const int d = 2 * lane;
+  float2v o = {0.0f, 0.0f};
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const int parts = a.parts - 64 * i < 64 ? a.parts - 64 * i : 64;
+    const float* from_part = a.part_out + (first + (int64_t)64 * i * a.rows) * a.dim + d;
+    for (int p = 0; p < parts; p += 8) {
+      float2v x[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        x[u] = p + u < parts && d < a.dim ? *(const float2v*)(from_part + (int64_t)(p + u) * a.rows * a.dim)
+                                          : float2v{0.0f, 0.0f};
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const float factor = __shfl(m[i], (p + u) & 63);
+        o[0] = __builtin_fmaf(factor, x[u][0], o[0]);
+        o[1] = __builtin_fmaf(factor, x[u][1], o[1]);
+      }
+    }
+  }
+  const float over = sum == 0.0f ? 0.0f : 1.0f / sum;
+  if (d < a.dim) {
+    const int64_t to = batch * a.out.batch + at.head * a.out.head + at.query * a.out.pos + d;
+    Elements<BF16>::store1(a.out.at, to, o[0] * over);
+    Elements<BF16>::store1(a.out.at, to + 1, o[1] * over);
+  }
+  if (a.lse && lane == 0)
     a.lse[((int64_t)batch * a.heads + at.head) * a.queries + at.query] =
-        l == 0.0f ? infinity() : m + __builtin_amdgcn_logf(l);
+        sum == 0.0f ? infinity() : top + __builtin_amdgcn_logf(sum);
 }
 
 template <bool BF16, int D>
 void launch_rows(const AttentionArgs& a, hipStream_t s) {
-  const int tiles = (a.rows + kRows - 1) / kRows;
-  attention_kernel<BF16, D><<<dim3((unsigned)(tiles * a.kv_heads * a.batch)), dim3(kThreads), 0, s>>>(a);
+  const int heads = a.kv_heads * a.batch, parts = a.parts ? a.parts : 1;
+  if (a.rows <= kFewRows) {
+    attention_few_kernel<BF16, D><<<dim3((unsigned)(heads * parts)), dim3(kThreads), 0, s>>>(a);
+  } else {
+    const int tiles = (a.rows + kRows - 1) / kRows;
+    attention_kernel<BF16, D><<<dim3((unsigned)(tiles * heads * parts)), dim3(kThreads), 0, s>>>(a);
+  }
+  if (a.parts) {
+    const int64_t waves = kThreads / 64, blocks = ((int64_t)heads * a.rows + waves - 1) / waves;
+    attention_join_kernel<BF16><<<dim3((unsigned)blocks), dim3(kThreads), 0, s>>>(a);
+  }
 }
 
 template <bool BF16>
@@ -188,7 +411,20 @@ void launch_dim(const AttentionArgs& a, hipStream_t s) {
 
 }  // namespace
 
-void attention_parts(const AttentionArgs&, int32_t& parts, int32_t& part_keys) { parts = part_keys = 0; }
+// Keys are split where the rows alone are too few workgroups for 256 CUs: into
+// as many parts as give two to a CU, of at least so many tiles that a part's
+// work is worth the join (4 to 5 us with its launch).
+int32_t attention_parts(const AttentionArgs& a) {
+  const bool few = a.rows <= kFewRows;
+  const int64_t heads = (int64_t)a.kv_heads * a.batch, groups = few ? heads : heads * ((a.rows + kRows - 1) / kRows);
+  if (groups < 1 || groups >= 256) return 0;
+  const int64_t tile = few ? kFewKeys : a.bf16 ? kKeys<true> : kKeys<false>;
+  const int64_t most = (a.keys + tile - 1) / tile / (few ? 8 : 4);
+  int64_t parts = (512 + groups - 1) / groups;
+  parts = parts < most ? parts : most;
+  parts = parts < kMostParts ? parts : kMostParts;
+  return parts > 1 ? (int32_t)parts : 0;
+}
 
 hipError_t launch_attention(const AttentionArgs& a, hipStream_t s) {
   if (a.bf16)

@@ -24,8 +24,9 @@ __global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attention_dq_kernel(co
   __shared__ __align__(16) uint8_t lds[2][2][T::kBytes];  // [turn][keys, values]
   const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
   const int tiles = (a.rows + kRows - 1) / kRows;
-  const int work = run_of_xcd(blockIdx.x, gridDim.x);
-  const int tile = tiles - 1 - work % tiles, head_of = work / tiles;
+  const Work work = work_of(blockIdx.x, a.kv_heads * a.batch);
+  const int tile = tiles - 1 - work.order, head_of = work.head;  // (the last rows see the most keys)
+  const typename T::Lane places(lane);
   const int kv_head = head_of % a.kv_heads, batch = head_of / a.kv_heads;
   const int length = keys_of(a, batch);
 
@@ -49,18 +50,12 @@ __global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attention_dq_kernel(co
 #pragma unroll
     for (int j = 0; j < 8; ++j) delta = __builtin_fmaf((float)dout[s].v[j], (float)o.v[j], delta);
   }
-  delta += __shfl_xor(delta, 32);
+  delta = add_halves(delta);
   const int64_t stat = ((int64_t)batch * a.heads + at.head) * a.queries + at.query;
   const float lse = live ? a.lse[stat] : infinity();
   if (live && lane < 32) a.delta[stat] = delta;
 
-  int end;
-  {
-    const int first = tile * kRows, last = first + kRows < a.rows ? first + kRows - 1 : a.rows - 1;
-    const int whole = first / a.queries != last / a.queries;
-    end = limit_of(a, whole ? a.queries - 1 : last % a.queries, length);
-  }
-  const int turns = (end + kTile - 1) / kTile;
+  const int turns = (last_key(a, tile * kRows, kRows, length) + kTile - 1) / kTile;
 
   Staged<BF16, D, kTile, kThreads> next_k, next_v;
   constexpr int size = T::kSize;
@@ -92,12 +87,19 @@ __global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attention_dq_kernel(co
     const int first = turn * kTile;
     const uint8_t *keys = lds[turn & 1][0], *values = lds[turn & 1][1];
     if (first < most) {
+      schedule_here();
       float16v s = zeros(), dp = zeros();
 #pragma unroll
       for (int step = 0; step < D / 16; ++step) {
-        multiply(s, T::along(keys, 0, step, lane), q[step]);
-        multiply(dp, T::along(values, 0, step, lane), dout[step]);
+        multiply(s, T::along(keys, places, 0, step), q[step]);
+        multiply(dp, T::along(values, places, 0, step), dout[step]);
       }
+      if (BF16) interleave<4, D / 8, D / 8>();
+      schedule_here();
+      constexpr int ahead = D < 128 ? D / 16 : D / 32;  // (fragments that there are registers for)
+      Frag<BF16> across[D / 16];
+#pragma unroll
+      for (int i = 0; i < ahead; ++i) across[i] = T::across(keys, places, 16 * (i % 2), i / 2);
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const float p = exp2_fast(__builtin_fmaf(s[r], a.c, -lse));
@@ -107,11 +109,14 @@ __global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attention_dq_kernel(co
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[r] = first + 8 * (r / 4) + 4 * (lane >> 5) + r % 4 < limit ? s[r] : 0.0f;
       }
+      schedule_here();
       const Frag<BF16> d0 = as_frag<BF16, 0>(s), d1 = as_frag<BF16, 1>(s);
 #pragma unroll
+      for (int i = ahead; i < D / 16; ++i) across[i] = T::across(keys, places, 16 * (i % 2), i / 2);
+#pragma unroll
       for (int part = 0; part < D / 32; ++part) {
-        multiply(dq[part], T::across(keys, 0, part, lane), d0);
-        multiply(dq[part], T::across(keys, 16, part, lane), d1);
+        multiply(dq[part], across[2 * part], d0);
+        multiply(dq[part], across[2 * part + 1], d1);
       }
     }
     if (turn + 1 < turns) store(turn + 1);
@@ -124,27 +129,46 @@ __global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attention_dq_kernel(co
 }
 
 template <bool BF16, int D>
-__global__ __launch_bounds__(kThreads, BF16 && D < 128 ? 2 : 1) void attention_dkv_kernel(const AttentionArgs a) {
+__global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attention_dkv_kernel(const AttentionArgs a) {
   typedef Tile<BF16, D, kTile> T;
-  __shared__ __align__(16) uint8_t lds[2][2][T::kBytes];  // [turn][queries, dout]
-  __shared__ float lses[2][kTile], deltas[2][kTile];
+  // Two sums of 128 x 32, k and v are 192 registers with bfloat16's 128 elements:
+  // two waves to a SIMD only with v in LDS.  Two workgroups fill a CU's 160 KiB to
+  // the byte, so the rows' log sums and deltas lie in v's padding.
+  constexpr bool kKeep = !(BF16 && D == 128);
+  typedef Tile<BF16, D, kRows> Own;
+  constexpr int kStats = 2 * 2 * kTile * 4, kTiles = 2 * 2 * T::kBytes;
+  static_assert(kKeep || (Own::kPad == 4 && kStats <= 8 * 64), "padding");
+  __shared__ __align__(16) uint8_t lds[kTiles + (kKeep ? kStats : Own::kBytes)];
+  auto tile_at = [&](int place, int which) { return lds + (place * 2 + which) * T::kBytes; };  // queries, dout
+  uint8_t* const values = lds + kTiles;
+  auto stats_at = [&](int place, int which, int i) {  // log sums, deltas; four from a multiple of four on
+    const int n = (place * 2 + which) * kTile + i;
+    return (float*)(kKeep ? values + n * 4 : values + (n >> 4) * Own::kStride + Own::kChunks * 16 + (n & 15) * 4);
+  };
   const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), h = lane >> 5;
-  const int tiles = (a.keys + kRows - 1) / kRows;
-  const int work = run_of_xcd(blockIdx.x, gridDim.x);
-  const int tile = work % tiles, head_of = work / tiles;  // (the first keys are seen by the most rows)
+  const Work work = work_of(blockIdx.x, a.kv_heads * a.batch);
+  const int tile = work.order, head_of = work.head;  // (the first keys are seen by the most rows)
+  const typename T::Lane places(lane);
   const int kv_head = head_of % a.kv_heads, batch = head_of / a.kv_heads;
   const int length = keys_of(a, batch);
 
   const int key0 = tile * kRows, wave_key = key0 + wave * 32, key = wave_key + (lane & 31);
   const bool live = key < length;
-  Frag<BF16> k[D / 16], v[D / 16];
+  Frag<BF16> k[D / 16], v[kKeep ? D / 16 : 1];
   const int64_t k_at = batch * a.k.batch + kv_head * a.k.head + key * a.k.pos;
   const int64_t v_at = batch * a.v.batch + kv_head * a.v.head + key * a.v.pos;
 #pragma unroll
   for (int s = 0; s < D / 16; ++s) {
     const int d = 16 * s + 8 * h;
     k[s] = load_frag<BF16>(a.k.at, k_at + d, live && d < a.dim);
-    v[s] = load_frag<BF16>(a.v.at, v_at + d, live && d < a.dim);
+    if (kKeep) v[kKeep ? s : 0] = load_frag<BF16>(a.v.at, v_at + d, live && d < a.dim);
+  }
+  if (!kKeep) {
+    Staged<BF16, D, kRows, kThreads> all;
+    const int64_t pos = a.v.pos * T::kSize;
+    all.start(a.dim, (int)pos, threadIdx.x);
+    all.load((const uint8_t*)a.v.at + (batch * a.v.batch + kv_head * a.v.head) * T::kSize, pos, a.dim, key0, length);
+    all.store(values, threadIdx.x);
   }
 
   // The query heads one after the other, each from the first tile of queries
@@ -185,14 +209,16 @@ __global__ __launch_bounds__(kThreads, BF16 && D < 128 ? 2 : 1) void attention_d
     }
   };
   auto store = [&](int place) {
-    next_q.store(lds[place][0], threadIdx.x);
-    next_do.store(lds[place][1], threadIdx.x);
+    next_q.store(tile_at(place, 0), threadIdx.x);
+    next_do.store(tile_at(place, 1), threadIdx.x);
     if (threadIdx.x < kTile) {
-      lses[place][threadIdx.x] = next_lse;
-      deltas[place][threadIdx.x] = next_delta;
+      *stats_at(place, 0, threadIdx.x) = next_lse;
+      *stats_at(place, 1, threadIdx.x) = next_delta;
     }
   };
 
+  const typename Own::Lane own_places(lane);
+  constexpr int kAhead = kKeep ? D / 32 : 2;  // of dout's fragments, read before the probabilities are done
   float16v dk[D / 32], dv[D / 32];
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) dk[i] = dv[i] = zeros();
@@ -204,42 +230,60 @@ __global__ __launch_bounds__(kThreads, BF16 && D < 128 ? 2 : 1) void attention_d
   __syncthreads();
   int in_head = from, place = 0;
   for (int turn = 0; turn < turns; ++turn) {
-    if (turn + 1 < turns) load();
-    const uint8_t *queries = lds[place][0], *douts = lds[place][1];
-    {
-      float16v s = zeros(), dp = zeros();
+    if (kKeep && turn + 1 < turns) load();
+    const uint8_t *queries = tile_at(place, 0), *douts = tile_at(place, 1);
+    schedule_here();
+    float16v s = zeros(), dp = zeros();
 #pragma unroll
-      for (int step = 0; step < D / 16; ++step) {
-        multiply(s, T::along(queries, 0, step, lane), k[step]);
-        multiply(dp, T::along(douts, 0, step, lane), v[step]);
-      }
+    for (int step = 0; step < D / 16; ++step) {
+      multiply(s, T::along(queries, places, 0, step), k[step]);
+      const Frag<BF16> vs = kKeep ? v[kKeep ? step : 0] : Own::along(values, own_places, wave * 32, step);
+      multiply(dp, T::along(douts, places, 0, step), vs);
+    }
+    if (BF16) interleave<4, D / 16 * (kKeep ? 2 : 3), D / 8, kKeep ? 1 : 2>();
+    schedule_here();
+    if (!kKeep && turn + 1 < turns) load();  // (what the loads pass through is free only now)
+    Frag<BF16> across[D / 16];
+    if (BF16) {
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const float4v lse = *(const float4v*)&lses[place][8 * g + 4 * h];
+      for (int i = 0; i < kAhead; ++i) across[i] = T::across(douts, places, 16 * (i % 2), i / 2);
+    }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[4 * g + i] = exp2_fast(__builtin_fmaf(s[4 * g + i], a.c, -lse[i]));
-      }
-      // the tile's first query does not see the wave's last key
-      const int hidden = wave_key + 31 - (in_head * kTile + a.keys - a.queries);
-      if (a.causal && hidden > 0) {
-        const int at = (lane & 31) - 31 + hidden - 4 * h;  // rows below it do not see the lane's key
+    for (int g = 0; g < 4; ++g) {
+      const float4v lse = *(const float4v*)stats_at(place, 0, 8 * g + 4 * h);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = 8 * (r / 4) + r % 4 < at ? 0.0f : s[r];
-      }
+      for (int i = 0; i < 4; ++i) s[4 * g + i] = exp2_fast(__builtin_fmaf(s[4 * g + i], a.c, -lse[i]));
+    }
+    // the tile's first query does not see the wave's last key
+    const int hidden = wave_key + 31 - (in_head * kTile + a.keys - a.queries);
+    if (a.causal && hidden > 0) {
+      const int at = (lane & 31) - 31 + hidden - 4 * h;  // rows below it do not see the lane's key
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const float4v delta = *(const float4v*)&deltas[place][8 * g + 4 * h];
+      for (int r = 0; r < 16; ++r) s[r] = 8 * (r / 4) + r % 4 < at ? 0.0f : s[r];
+    }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) dp[4 * g + i] = s[4 * g + i] * (dp[4 * g + i] - delta[i]);
-      }
-      const Frag<BF16> p0 = as_frag<BF16, 0>(s), p1 = as_frag<BF16, 1>(s);
-      const Frag<BF16> d0 = as_frag<BF16, 0>(dp), d1 = as_frag<BF16, 1>(dp);
+    for (int g = 0; g < 4; ++g) {
+      const float4v delta = *(const float4v*)stats_at(place, 1, 8 * g + 4 * h);
 #pragma unroll
-      for (int part = 0; part < D / 32; ++part) {
-        multiply(dv[part], T::across(douts, 0, part, lane), p0);
-        multiply(dv[part], T::across(douts, 16, part, lane), p1);
-        multiply(dk[part], T::across(queries, 0, part, lane), d0);
-        multiply(dk[part], T::across(queries, 16, part, lane), d1);
+      for (int i = 0; i < 4; ++i) dp[4 * g + i] = s[4 * g + i] * (dp[4 * g + i] - delta[i]);
+    }
+    const Frag<BF16> p0 = as_frag<BF16, 0>(s), p1 = as_frag<BF16, 1>(s);
+    const Frag<BF16> d0 = as_frag<BF16, 0>(dp), d1 = as_frag<BF16, 1>(dp);
+    if (BF16) {
+      schedule_here();
+#pragma unroll
+      for (int i = kAhead; i < D / 16; ++i) across[i] = T::across(douts, places, 16 * (i % 2), i / 2);
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) multiply(dv[i / 2], across[i], i % 2 ? p1 : p0);
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) multiply(dk[i / 2], T::across(queries, places, 16 * (i % 2), i / 2), i % 2 ? d1 : d0);
+      interleave<2 * (D / 16 - kAhead), 2 * (2 * (D / 16) - kAhead), D / 8, 2>();
+      schedule_here();
+    } else {
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) {
+        multiply(dv[i / 2], T::across(douts, places, 16 * (i % 2), i / 2), i % 2 ? p1 : p0);
+        multiply(dk[i / 2], T::across(queries, places, 16 * (i % 2), i / 2), i % 2 ? d1 : d0);
       }
     }
     if (turn + 1 < turns) store(place ^ 1);

@@ -50,6 +50,9 @@ SHAPES = [
     (7, 64, 64, 2, 1, 64), (2, 128, 128, 4, 4, 64), (1, 129, 127, 2, 2, 72), (7, 100, 130, 6, 2, 80), (1, 257, 96, 4, 2, 88),
     (2, 3, 300, 8, 1, 96), (1, 200, 200, 4, 4, 104), (7, 1, 515, 8, 2, 128), (1, 300, 515, 2, 2, 128), (2, 515, 300, 4, 1, 128),
     (1, 700, 700, 2, 1, 120), (3, 17, 1, 4, 4, 56), (1, 2, 2049, 32, 4, 64), (300, 4, 4, 2, 2, 16),
+    # keys in parts, of few rows and of more
+    (2, 1, 2500, 4, 1, 128), (1, 1, 9001, 3, 3, 40), (1, 5, 1100, 6, 1, 96), (2, 130, 1500, 2, 1, 64),
+    (1, 40, 3001, 1, 1, 128), (2, 33, 777, 3, 3, 32),
 ]
 
 
