@@ -624,21 +624,27 @@ typedef struct microadam_attention {
 int microadam_attention_workspace(const microadam_attention* attention, int32_t grad, uint64_t* bytes);
 
 /*
- * out, and for the backward pass lse[batch][heads][queries] (NULL: not
- * wanted): log2 of the sum of 2^(z log2 e), +infinity where no key is seen.
+ * out, and in `saved` (NULL: not wanted) what the backward pass takes besides:
+ * each query's log2 sum 2^(z log2 e), and of a bfloat16 out what its rounding
+ * left over.  microadam_attention_saved says how many bytes that is, by the
+ * sizes and dtype alone; 256-byte aligned.
  */
+int microadam_attention_saved(const microadam_attention* attention, uint64_t* bytes);
+
 int microadam_attention_forward(const microadam_attention* attention, const microadam_heads* out,
-                                float* lse, void* workspace, uint64_t workspace_bytes, void* stream);
+                                void* saved, uint64_t saved_bytes, void* workspace,
+                                uint64_t workspace_bytes, void* stream);
 
 /*
  * dq, dk and dv for dout, from the operands of the forward call and the out and
- * lse that it wrote.  The gradients of shared heads are summed in registers,
- * in binary32, in one order: the same call gives the same bits.
+ * `saved` that it wrote.  The gradients of shared heads are summed in
+ * registers, in binary32, in one order: the same call gives the same bits.
  */
 int microadam_attention_grad(const microadam_attention* attention, const microadam_heads* out,
-                             const float* lse, const microadam_heads* dout, const microadam_heads* dq,
-                             const microadam_heads* dk, const microadam_heads* dv, void* workspace,
-                             uint64_t workspace_bytes, void* stream);
+                             const void* saved, uint64_t saved_bytes, const microadam_heads* dout,
+                             const microadam_heads* dq, const microadam_heads* dk,
+                             const microadam_heads* dv, void* workspace, uint64_t workspace_bytes,
+                             void* stream);
 
 const char* microadam_error_string(int code);
 

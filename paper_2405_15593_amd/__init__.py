@@ -182,7 +182,8 @@ EXPORTS = (
     "microadam_token_logprobs", "microadam_token_logprobs_grad",
     "microadam_clip_workspace", "microadam_grad_norm", "microadam_clip_grads",
     "microadam_layer_norm", "microadam_layer_norm_workspace", "microadam_layer_norm_grad",
-    "microadam_attention_workspace", "microadam_attention_forward", "microadam_attention_grad",
+    "microadam_attention_workspace", "microadam_attention_saved", "microadam_attention_forward",
+    "microadam_attention_grad",
 )
 
 
@@ -235,8 +236,9 @@ def load(path: str = LIBRARY):
     lib.microadam_layer_norm_workspace.argtypes = [P(microadam_rows), P(u64)]
     lib.microadam_layer_norm_grad.argtypes = [P(microadam_rows), vp, vp, vp, i64, vp, i64, vp, vp, vp, u64, vp]
     lib.microadam_attention_workspace.argtypes = [P(microadam_attention), i32, P(u64)]
-    lib.microadam_attention_forward.argtypes = [P(microadam_attention), P(microadam_heads), vp, vp, u64, vp]
-    lib.microadam_attention_grad.argtypes = [P(microadam_attention), P(microadam_heads), vp, P(microadam_heads),
+    lib.microadam_attention_saved.argtypes = [P(microadam_attention), P(u64)]
+    lib.microadam_attention_forward.argtypes = [P(microadam_attention), P(microadam_heads), vp, u64, vp, u64, vp]
+    lib.microadam_attention_grad.argtypes = [P(microadam_attention), P(microadam_heads), vp, u64, P(microadam_heads),
                                              P(microadam_heads), P(microadam_heads), P(microadam_heads), vp, u64, vp]
     lib.microadam_error_string.argtypes = [ctypes.c_int]
     lib.microadam_error_string.restype = ctypes.c_char_p
@@ -249,8 +251,8 @@ def load(path: str = LIBRARY):
               "microadam_orthogonalize", "microadam_muon_step", "microadam_token_logprobs",
               "microadam_token_logprobs_grad", "microadam_clip_workspace", "microadam_grad_norm",
               "microadam_clip_grads", "microadam_layer_norm", "microadam_layer_norm_workspace",
-              "microadam_layer_norm_grad", "microadam_attention_workspace", "microadam_attention_forward",
-              "microadam_attention_grad"):
+              "microadam_layer_norm_grad", "microadam_attention_workspace", "microadam_attention_saved",
+              "microadam_attention_forward", "microadam_attention_grad"):
         getattr(lib, f).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -470,18 +472,24 @@ def microadam_attention_workspace(attention: microadam_attention, grad: bool) ->
     return out.value
 
 
-def microadam_attention_forward(attention: microadam_attention, out: microadam_heads, lse_ptr: int,
-                                workspace_ptr: int, workspace_bytes: int, stream: int = 0) -> None:
-    _check(load().microadam_attention_forward(ctypes.byref(attention), ctypes.byref(out), lse_ptr, workspace_ptr,
-                                              workspace_bytes, stream), "microadam_attention_forward")
+def microadam_attention_saved(attention: microadam_attention) -> int:
+    out = ctypes.c_uint64(0)
+    _check(load().microadam_attention_saved(ctypes.byref(attention), ctypes.byref(out)), "microadam_attention_saved")
+    return out.value
 
 
-def microadam_attention_grad(attention: microadam_attention, out: microadam_heads, lse_ptr: int,
+def microadam_attention_forward(attention: microadam_attention, out: microadam_heads, saved_ptr: int,
+                                saved_bytes: int, workspace_ptr: int, workspace_bytes: int, stream: int = 0) -> None:
+    _check(load().microadam_attention_forward(ctypes.byref(attention), ctypes.byref(out), saved_ptr, saved_bytes,
+                                              workspace_ptr, workspace_bytes, stream), "microadam_attention_forward")
+
+
+def microadam_attention_grad(attention: microadam_attention, out: microadam_heads, saved_ptr: int, saved_bytes: int,
                              dout: microadam_heads, dq: microadam_heads, dk: microadam_heads, dv: microadam_heads,
                              workspace_ptr: int, workspace_bytes: int, stream: int = 0) -> None:
-    _check(load().microadam_attention_grad(ctypes.byref(attention), ctypes.byref(out), lse_ptr, ctypes.byref(dout),
-                                           ctypes.byref(dq), ctypes.byref(dk), ctypes.byref(dv), workspace_ptr,
-                                           workspace_bytes, stream), "microadam_attention_grad")
+    _check(load().microadam_attention_grad(ctypes.byref(attention), ctypes.byref(out), saved_ptr, saved_bytes,
+                                           ctypes.byref(dout), ctypes.byref(dq), ctypes.byref(dk), ctypes.byref(dv),
+                                           workspace_ptr, workspace_bytes, stream), "microadam_attention_grad")
 
 
 def microadam_error_string(code: int) -> str:

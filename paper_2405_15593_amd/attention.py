@@ -19,7 +19,7 @@ from typing import Optional
 import torch
 
 from . import (MICROADAM_BF16, MICROADAM_F32, microadam_attention, microadam_attention_forward,
-               microadam_attention_grad, microadam_attention_workspace, microadam_heads)
+               microadam_attention_grad, microadam_attention_saved, microadam_attention_workspace, microadam_heads)
 from ._autograd import refuse_tangents
 
 _HERE = contextlib.nullcontext()
@@ -67,46 +67,49 @@ def _struct(q, k, v, key_lengths, causal, scale):
                                b, sq, k.shape[1], h, k.shape[2], d, scale, _DTYPES[q.dtype], 1 if causal else 0)
 
 
-def _workspace(given, grad, device):
-    need = microadam_attention_workspace(given, grad)
+def _bytes(need, device):
+    """(the tensor that holds them, address) of so many bytes at a multiple of
+    256, where torch's allocator puts a tensor of its own."""
     if not need:
-        return None, None, 0
-    store = torch.empty(need + 256, dtype=torch.uint8, device=device)
-    return store, store.data_ptr() + (-store.data_ptr()) % 256, need
+        return None, None
+    store = torch.empty(need, dtype=torch.uint8, device=device)
+    return store, store.data_ptr()
 
 
 def _forward(q, k, v, key_lengths, causal, scale, keep):
     out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    b, sq, h, _ = q.shape
-    lse = torch.empty((b, h, sq), dtype=torch.float32, device=q.device) if keep else None
     given = _struct(q, k, v, key_lengths, causal, scale)
     with _on(q.device):
-        store, address, size = _workspace(given, False, q.device)
-        microadam_attention_forward(given, _heads(out), None if lse is None else lse.data_ptr(), address, size,
+        need, kept = microadam_attention_workspace(given, False), microadam_attention_saved(given) if keep else 0
+        store, address = _bytes(need, q.device)
+        saved, at = _bytes(kept, q.device)
+        microadam_attention_forward(given, _heads(out), at, kept, address, need,
                                     torch.cuda.current_stream(q.device.index).cuda_stream)
-    return out, lse
+    return out, saved
 
 
 class _Attention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, key_lengths, causal, scale):
-        out, lse = _forward(*(_rows(t) for t in (q, k, v)), key_lengths, causal, scale, True)
-        ctx.save_for_backward(q, k, v, key_lengths, out, lse)
+        out, saved = _forward(*(_rows(t) for t in (q, k, v)), key_lengths, causal, scale, True)
+        ctx.save_for_backward(q, k, v, key_lengths, out, saved)
         ctx.settings = (causal, scale)
         return out
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dout):
-        q, k, v, key_lengths, out, lse = ctx.saved_tensors
+        q, k, v, key_lengths, out, saved = ctx.saved_tensors
         causal, scale = ctx.settings
         q, k, v, dout = (_rows(t) for t in (q, k, v, dout))
         dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
         given = _struct(q, k, v, key_lengths, causal, scale)
         with _on(q.device):
-            store, address, size = _workspace(given, True, q.device)
-            microadam_attention_grad(given, _heads(out), lse.data_ptr(), _heads(dout), _heads(dq), _heads(dk),
-                                     _heads(dv), address, size,
+            need = microadam_attention_workspace(given, True)
+            store, address = _bytes(need, q.device)
+            microadam_attention_grad(given, _heads(out), None if saved is None else saved.data_ptr(),
+                                     0 if saved is None else saved.numel(), _heads(dout), _heads(dq), _heads(dk),
+                                     _heads(dv), address, need,
                                      torch.cuda.current_stream(q.device.index).cuda_stream)
         return dq, dk, dv, None, None, None
 

@@ -122,6 +122,16 @@ uint64_t up(uint64_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 
 uint64_t stats_bytes(const AttentionArgs& a) { return (uint64_t)a.batch * a.heads * a.queries * sizeof(float); }
 
+// The rows' log sums, and for bfloat16 what the rounding of out left over.
+uint64_t saved_bytes(const AttentionArgs& a) {
+  return up(stats_bytes(a)) + (a.bf16 ? up((uint64_t)a.batch * a.heads * a.queries * a.dim * 2) : 0);
+}
+
+void set_saved(AttentionArgs& a, const void* saved) {
+  a.lse = (float*)const_cast<void*>(saved);
+  a.rest = saved && a.bf16 ? (uint16_t*)((uint8_t*)const_cast<void*>(saved) + up(stats_bytes(a))) : nullptr;
+}
+
 uint64_t part_rows(const AttentionArgs& a) { return (uint64_t)a.batch * a.kv_heads * a.parts * a.rows; }
 
 uint64_t workspace_of(const AttentionArgs& a, bool grad) {
@@ -135,6 +145,12 @@ int check_workspace(const AttentionArgs& a, bool grad, const void* workspace, ui
   if (need && !workspace) return report(MICROADAM_ERR_INVALID_ARG, "workspace is NULL");
   if (need && (uintptr_t)workspace % kAlign)
     return report(MICROADAM_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+  return MICROADAM_OK;
+}
+
+int check_saved(const AttentionArgs& a, const void* saved, uint64_t size) {
+  if (size < saved_bytes(a)) return report(MICROADAM_ERR_STATE_SIZE, "saved is smaller than microadam_attention_saved's");
+  if ((uintptr_t)saved % kAlign) return report(MICROADAM_ERR_INVALID_ARG, "saved must be 256-byte aligned");
   return MICROADAM_OK;
 }
 
@@ -164,8 +180,18 @@ int microadam_attention_workspace(const microadam_attention* attention, int32_t 
   return MICROADAM_OK;
 }
 
-int microadam_attention_forward(const microadam_attention* attention, const microadam_heads* out, float* lse,
-                                void* workspace, uint64_t workspace_bytes, void* stream) {
+int microadam_attention_saved(const microadam_attention* attention, uint64_t* bytes) {
+  AttentionArgs a;
+  const int rc = check(attention, a);
+  if (rc) return rc;
+  if (!bytes) return report(MICROADAM_ERR_INVALID_ARG, "bytes is NULL");
+  *bytes = saved_bytes(a);
+  clear_report();
+  return MICROADAM_OK;
+}
+
+int microadam_attention_forward(const microadam_attention* attention, const microadam_heads* out, void* saved,
+                                uint64_t saved_size, void* workspace, uint64_t workspace_bytes, void* stream) {
   AttentionArgs a;
   int rc = check(attention, a);
   if (rc) return rc;
@@ -173,12 +199,12 @@ int microadam_attention_forward(const microadam_attention* attention, const micr
   Range read[4], written[3];
   if ((rc = inputs(attention, a, read))) return rc;
   if ((rc = operand(out, t.batch, t.queries, t.heads, t.dim, t.dtype, true, a.out, written[0]))) return rc;
-  if ((uintptr_t)lse % 4) return report(MICROADAM_ERR_INVALID_ARG, "lse is not aligned");
+  if (saved && (rc = check_saved(a, saved, saved_size))) return rc;
   if ((rc = check_workspace(a, false, workspace, workspace_bytes))) return rc;
-  written[1] = run(lse, (int64_t)stats_bytes(a));
+  written[1] = run(saved, (int64_t)saved_bytes(a));
   written[2] = run(workspace_of(a, false) ? workspace : nullptr, (int64_t)workspace_of(a, false));
   if ((rc = check_apart(written, 3, read, 4))) return rc;
-  a.lse = lse;
+  set_saved(a, saved);
   if (a.parts) {
     a.part_stats = (float*)workspace;
     a.part_out = (float*)((uint8_t*)workspace + up(part_rows(a) * 2 * sizeof(float)));
@@ -191,9 +217,10 @@ int microadam_attention_forward(const microadam_attention* attention, const micr
   return MICROADAM_OK;
 }
 
-int microadam_attention_grad(const microadam_attention* attention, const microadam_heads* out, const float* lse,
-                             const microadam_heads* dout, const microadam_heads* dq, const microadam_heads* dk,
-                             const microadam_heads* dv, void* workspace, uint64_t workspace_bytes, void* stream) {
+int microadam_attention_grad(const microadam_attention* attention, const microadam_heads* out, const void* saved,
+                             uint64_t saved_size, const microadam_heads* dout, const microadam_heads* dq,
+                             const microadam_heads* dk, const microadam_heads* dv, void* workspace,
+                             uint64_t workspace_bytes, void* stream) {
   AttentionArgs a;
   int rc = check(attention, a);
   if (rc) return rc;
@@ -206,13 +233,13 @@ int microadam_attention_grad(const microadam_attention* attention, const microad
       (rc = operand(dk, t.batch, t.keys, t.kv_heads, t.dim, t.dtype, true, a.dk, written[1])) ||
       (rc = operand(dv, t.batch, t.keys, t.kv_heads, t.dim, t.dtype, true, a.dv, written[2])))
     return rc;
-  if (a.batch > 0 && a.rows > 0 && !lse) return report(MICROADAM_ERR_INVALID_ARG, "lse is NULL");
-  if ((uintptr_t)lse % 4) return report(MICROADAM_ERR_INVALID_ARG, "lse is not aligned");
+  if (saved_bytes(a) && !saved) return report(MICROADAM_ERR_INVALID_ARG, "saved is NULL");
+  if ((rc = check_saved(a, saved, saved_size))) return rc;
   if ((rc = check_workspace(a, true, workspace, workspace_bytes))) return rc;
-  read[6] = run(lse, (int64_t)stats_bytes(a));
+  read[6] = run(saved, (int64_t)saved_bytes(a));
   written[3] = run(stats_bytes(a) ? workspace : nullptr, (int64_t)workspace_of(a, true));
   if ((rc = check_apart(written, 4, read, 7))) return rc;
-  a.lse = const_cast<float*>(lse);
+  set_saved(a, saved);
   a.delta = (float*)workspace;
   if (a.batch > 0) {
     const hipError_t e = launch_attention_grad(a, (hipStream_t)stream);

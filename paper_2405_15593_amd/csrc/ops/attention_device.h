@@ -22,8 +22,9 @@ struct AttentionArgs {
   int32_t causal, bf16;
   float scale;
   float c;       // scale * log2(e)
-  float* lse;    // [batch][heads][queries], in units of ln 2; +inf: no key
-  float* delta;  // backward: sum of dout out, alike
+  float* lse;      // [batch][heads][queries], in units of ln 2; +inf: no key; NULL forward: not wanted
+  uint16_t* rest;  // with lse and bfloat16, [batch][heads][queries][dim]: out before its rounding less out
+  float* delta;    // backward: sum of dout out, as lse
   // forward, with the keys split over workgroups: per part and row (maximum,
   // sum) and the unnormalised output
   float* part_out;    // [batch][kv_heads][parts][rows][dim]

@@ -244,6 +244,25 @@ __device__ inline void store_column(void* p, int64_t at, int left, const float16
   }
 }
 
+// What bfloat16's rounding of the same elements left over, to `at` on.
+__device__ inline void store_rest(uint16_t* p, int64_t at, int left, const float16v& d, float factor, int lane) {
+  const int h = lane >> 5;
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    const int e = 8 * g + 4 * h;
+    if (e >= left) continue;
+    float r[4];
+#pragma unroll
+    for (int i = 0; i < 4; i += 2) {
+      const float a = d[4 * g + i] * factor, b = d[4 * g + i + 1] * factor;
+      const uint32_t q = pack_bf16(a, b);
+      r[i] = a - __uint_as_float(q << 16);
+      r[i + 1] = b - __uint_as_float(q & 0xffff0000u);
+    }
+    *(uint2v*)(p + at + e) = uint2v{pack_bf16(r[0], r[1]), pack_bf16(r[2], r[3])};
+  }
+}
+
 // The value of the lane 32 away joined with one's own (a lane and that one hold
 // the halves of a column).
 __device__ inline float max_halves(float x) {

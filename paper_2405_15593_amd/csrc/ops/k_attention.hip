@@ -124,9 +124,13 @@ __device__ inline void finish(const AttentionArgs& a, int head_of, int batch, in
   const int64_t o_at = batch * a.out.batch + at.head * a.out.head + at.query * a.out.pos;
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) store_column<BF16>(a.out.at, o_at + 32 * i, a.dim - 32 * i, out[i], over, lane);
-  if (a.lse && lane < 32)
-    a.lse[((int64_t)batch * a.heads + at.head) * a.queries + at.query] =
-        l == 0.0f ? infinity() : m + __builtin_amdgcn_logf(l);
+  if (!a.lse) return;
+  const int64_t stat = ((int64_t)batch * a.heads + at.head) * a.queries + at.query;
+  if (lane < 32) a.lse[stat] = l == 0.0f ? infinity() : m + __builtin_amdgcn_logf(l);
+  if (BF16) {
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) store_rest(a.rest, stat * a.dim + 32 * i, a.dim - 32 * i, out[i], over, lane);
+  }
 }
 
 // The tiles [first, last) of a part of `tiles`.
@@ -372,14 +376,19 @@ __global__ __launch_bounds__(kThreads) void attention_join_kernel(const Attentio
     }
   }
   const float over = sum == 0.0f ? 0.0f : 1.0f / sum;
+  const int64_t stat = ((int64_t)batch * a.heads + at.head) * a.queries + at.query;
   if (d < a.dim) {
     const int64_t to = batch * a.out.batch + at.head * a.out.head + at.query * a.out.pos + d;
-    Elements<BF16>::store1(a.out.at, to, o[0] * over);
-    Elements<BF16>::store1(a.out.at, to + 1, o[1] * over);
+    o *= over;
+    Elements<BF16>::store1(a.out.at, to, o[0]);
+    Elements<BF16>::store1(a.out.at, to + 1, o[1]);
+    if (BF16 && a.lse) {
+      const uint32_t q = pack_bf16(o[0], o[1]);
+      *(uint32_t*)(a.rest + stat * a.dim + d) =
+          pack_bf16(o[0] - __uint_as_float(q << 16), o[1] - __uint_as_float(q & 0xffff0000u));
+    }
   }
-  if (a.lse && lane == 0)
-    a.lse[((int64_t)batch * a.heads + at.head) * a.queries + at.query] =
-        sum == 0.0f ? infinity() : top + __builtin_amdgcn_logf(sum);
+  if (a.lse && lane == 0) a.lse[stat] = sum == 0.0f ? infinity() : top + __builtin_amdgcn_logf(sum);
 }
 
 template <bool BF16, int D>

@@ -39,6 +39,9 @@ __global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attention_dq_kernel(co
   const int64_t q_at = batch * a.q.batch + at.head * a.q.head + at.query * a.q.pos;
   const int64_t do_at = batch * a.dout.batch + at.head * a.dout.head + at.query * a.dout.pos;
   const int64_t o_at = batch * a.out.batch + at.head * a.out.head + at.query * a.out.pos;
+  const int64_t stat = ((int64_t)batch * a.heads + at.head) * a.queries + at.query;
+  // (delta from out as it was before its rounding: of few keys ds is a small
+  // difference to it; with out alone dk of three keys was off by 3.8e-3)
   float delta = 0.0f;
 #pragma unroll
   for (int s = 0; s < D / 16; ++s) {
@@ -49,9 +52,13 @@ __global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attention_dq_kernel(co
     const Frag<BF16> o = load_frag<BF16>(a.out.at, o_at + d, there);
 #pragma unroll
     for (int j = 0; j < 8; ++j) delta = __builtin_fmaf((float)dout[s].v[j], (float)o.v[j], delta);
+    if (BF16) {
+      const Frag<BF16> rest = load_frag<BF16>(a.rest, stat * a.dim + d, there);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) delta = __builtin_fmaf((float)dout[s].v[j], (float)rest.v[j], delta);
+    }
   }
   delta = add_halves(delta);
-  const int64_t stat = ((int64_t)batch * a.heads + at.head) * a.queries + at.query;
   const float lse = live ? a.lse[stat] : infinity();
   if (live && lane < 32) a.delta[stat] = delta;
 

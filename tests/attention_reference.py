@@ -8,7 +8,7 @@ the roundings of the exponent's argument (3 u of its size, in units of ln 2),
 and the sum's chain of at most `keys` terms with its factors adds (keys + 16) u.
 p and ds are rounded to the dtype before their products (h each), the products
 summed in chains of at most `keys` (or rows) terms.  delta = sum dout out takes
-out as it was rounded.  Results are rounded once (h).
+out with what its rounding left over, which is rounded itself (h of h).  Results are rounded once (h).
 
 Below binary32's normal range 2^-126 there are no relative errors: the
 exponential gives zero there, and the matrix cores take smaller operands as
@@ -58,7 +58,7 @@ def reference(q, k, v, dout, causal, lengths, scale, dtype):
     dp = dout @ vv.transpose(2, 3)
     delta = (dout * out).sum(3, keepdim=True)
     ds = p * (dp - delta)
-    edelta = (dout.abs() * (eout + h * (out.abs() + eout) + d * U * out.abs())).sum(3, keepdim=True)
+    edelta = (dout.abs() * (eout + h * h * (out.abs() + eout) * 1.01 + 2 * d * U * out.abs())).sum(3, keepdim=True)
     eds = ep * (dp - delta).abs() + (p + ep) * (edelta + (d + 2) * U * (dout.abs() @ vv.abs().transpose(2, 3)) +
                                                 2 * U * (dp - delta).abs())
     eds = eds + h * (ds.abs() + eds) + TINY

@@ -13,7 +13,7 @@ F32, BF16 = ma.MICROADAM_F32, ma.MICROADAM_BF16
 INVALID, UNSUPPORTED, SIZE = (ma.MICROADAM_ERR_INVALID_ARG, ma.MICROADAM_ERR_UNSUPPORTED,
                               ma.MICROADAM_ERR_STATE_SIZE)
 # addresses that no refusal follows, 16 mebibytes apart
-Q, K, V, N, OUT, LSE, DOUT, DQ, DK, DV, WS = ((i + 1) << 24 for i in range(11))
+Q, K, V, N, OUT, SAVED, DOUT, DQ, DK, DV, WS = ((i + 1) << 24 for i in range(11))
 B, SQ, SK, H, HK, D = 2, 5, 7, 4, 2, 16
 
 
@@ -38,12 +38,12 @@ def given(**kw):
     return ma.microadam_attention(*a.values())
 
 
-def forward(a, out=None, lse=LSE, ws=WS, size=1 << 24):
-    ma.microadam_attention_forward(a, out or heads(OUT, SQ, H), lse, ws, size)
+def forward(a, out=None, saved=SAVED, kept=1 << 24, ws=WS, size=1 << 24):
+    ma.microadam_attention_forward(a, out or heads(OUT, SQ, H), saved, kept, ws, size)
 
 
-def backward(a, out=None, lse=LSE, dout=None, dq=None, dk=None, dv=None, ws=WS, size=1 << 24):
-    ma.microadam_attention_grad(a, out or heads(OUT, SQ, H), lse, dout or heads(DOUT, SQ, H), dq or heads(DQ, SQ, H),
+def backward(a, out=None, saved=SAVED, kept=1 << 24, dout=None, dq=None, dk=None, dv=None, ws=WS, size=1 << 24):
+    ma.microadam_attention_grad(a, out or heads(OUT, SQ, H), saved, kept, dout or heads(DOUT, SQ, H), dq or heads(DQ, SQ, H),
                                 dk or heads(DK, SK, HK), dv or heads(DV, SK, HK), ws, size)
 
 
@@ -87,7 +87,7 @@ def test_inputs(name, positions, count, at, kw, code):
 def test_inputs_with_shared_elements_are_allowed():
     """Where nothing is written, strides may be zero: up to the next refusal."""
     a = given(k=heads(K, SK, HK, batch_stride=0, head_stride=0))
-    refused(INVALID, forward, a, lse=LSE + 2)
+    refused(INVALID, forward, a, saved=SAVED + 128)
 
 
 @pytest.mark.parametrize("f,name,positions,count", [
@@ -101,10 +101,12 @@ def test_outputs(f, name, positions, count, kw):
 
 def test_outputs_apart():
     a = given()
-    refused(INVALID, forward, a, lse=OUT + 64)
-    refused(INVALID, forward, a, lse=OUT + 2)
-    refused(INVALID, backward, a, lse=None)
-    refused(INVALID, backward, a, lse=LSE + 1)
+    refused(INVALID, forward, a, saved=OUT)
+    refused(INVALID, forward, a, saved=Q + 512)
+    refused(INVALID, forward, a, saved=SAVED + 4)
+    refused(INVALID, backward, a, saved=None)
+    refused(INVALID, backward, a, saved=SAVED + 4)
+    refused(INVALID, backward, a, dq=heads(SAVED + 64, SQ, H))
     refused(INVALID, backward, a, dk=heads(DV + 4, SK, HK))
     refused(INVALID, backward, a, dq=heads(DOUT, SQ, H))
     refused(INVALID, backward, a, dq=heads(OUT, SQ, H))
@@ -120,17 +122,25 @@ def test_workspace():
     refused(INVALID, backward, given(), ws=WS + 64)
     refused(INVALID, backward, given(), ws=Q)
     assert ma.microadam_attention_workspace(given(batch=0), True) == 0
+    assert ma.microadam_attention_saved(given()) == 256
+    kept = ma.microadam_attention_saved(given(dtype=BF16))
+    assert kept == 256 + (B * H * SQ * D * 2 + 255) // 256 * 256
+    for f in (forward, backward):
+        refused(SIZE, f, given(), kept=255)
+        refused(SIZE, f, given(dtype=BF16), kept=kept - 1)
+    refused(INVALID, ma.microadam_attention_saved, given(causal=3))
     with pytest.raises(ma.MicroAdamError):
         ma._check(ma.load().microadam_attention_workspace(given(), 0, None), "microadam_attention_workspace")
-    assert ma.load().microadam_attention_forward(None, None, None, None, 0, None) == INVALID
-    assert ma.load().microadam_attention_forward(given(), None, None, None, 0, None) == INVALID
+    assert ma.load().microadam_attention_saved(given(), None) == INVALID
+    assert ma.load().microadam_attention_forward(None, None, None, 0, None, 0, None) == INVALID
+    assert ma.load().microadam_attention_forward(given(), None, None, 0, None, 0, None) == INVALID
 
 
 def test_nothing_to_do():
     none = heads(None, SQ, H)
     for kw in (dict(batch=0), dict(queries=0)):
-        forward(given(q=none, k=none, v=none, **kw), out=none, lse=None, ws=None, size=0)
-    backward(given(q=none, k=none, v=none, batch=0), none, None, none, none, none, none, None, 0)
+        forward(given(q=none, k=none, v=none, **kw), out=none, saved=None, kept=0, ws=None, size=0)
+    backward(given(q=none, k=none, v=none, batch=0), none, None, 0, none, none, none, none, None, 0)
 
 
 def test_python():
