@@ -109,12 +109,26 @@ struct GroupSum {
   }
 };
 
-// G threads to a row, P pieces of it each, R rows of a workgroup at a time.
+// A row's pieces in the registers: G threads to a row, P pieces each.
+template <bool BF16, int P, int G>
+struct Row {
+  typedef Elements<BF16> E;
+  uint4v q[P];
+  __device__ void load(const void* p, int64_t from, int t, int cols) {
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const int at = (i * G + t) * E::kPer;
+      q[i] = load_piece<BF16>(p, from + at, cols - at);
+    }
+  }
+  __device__ float get(int i, int j) const { return E::get(q[i], j); }
+};
+
+// ... R rows of a workgroup at a time.
 template <bool BF16, int P, int G, int R>
 struct Shape {
-  typedef Elements<BF16> E;
-  static constexpr int kPer = E::kPer;
-  static constexpr int kRows = R;
+  static constexpr int kRows = R, kGroup = G, kPer = Elements<BF16>::kPer;
+  static constexpr int kCols = P * G * kPer;  // at most
 };
 
 template <bool BF16, int P, int G, int R>
@@ -125,6 +139,13 @@ __global__ __launch_bounds__(G* R) void layer_norm_kernel(const LayerNormArgs a)
   GroupSum<G>& group = sums[threadIdx.x / G];
   const int t = threadIdx.x % G, cols = a.cols;
   const float over = 1.0f / (float)cols;
+  // every group takes as many turns as the others: they meet at barriers
+  constexpr bool kAhead = G == 256 || G == 1024;  // the next row's pieces are loaded while a row is summed
+  const int64_t step = (int64_t)gridDim.x * R;
+  int64_t row = (int64_t)blockIdx.x * R + threadIdx.x / G;
+  Row<BF16, P, G> next;
+  auto load = [&](int64_t r) { next.load(a.x, r < a.rows ? r * a.x_ld : 0, t, r < a.rows ? cols : 0); };
+  if (kAhead) load(row);
   float w[P][per], b[P][per];
 #pragma unroll
   for (int i = 0; i < P; ++i) {
@@ -132,23 +153,16 @@ __global__ __launch_bounds__(G* R) void layer_norm_kernel(const LayerNormArgs a)
     load_side<per>(a.weight, a.weight_bf16, at, left, 1.0f, w[i]);
     load_side<per>(a.bias, a.weight_bf16, at, left, 0.0f, b[i]);
   }
-  // every group takes as many turns as the others: they meet at barriers
-  const int64_t step = (int64_t)gridDim.x * R;
-  for (int64_t first = (int64_t)blockIdx.x * R; first < a.rows; first += step) {
-    const int64_t row = first + threadIdx.x / G;
+  for (int64_t first = (int64_t)blockIdx.x * R; first < a.rows; first += step, row += step) {
+    if (!kAhead) load(row);
+    const Row<BF16, P, G> x = next;
     const bool live = row < a.rows;
-    const int64_t from = live ? row * a.x_ld : 0;
-    uint4v q[P];
+    if (kAhead && first + step < a.rows) load(row + step);
     float sum = 0.0f;
-#pragma unroll
-    for (int i = 0; i < P; ++i) {
-      const int at = (i * G + t) * per;
-      q[i] = load_piece<BF16>(a.x, from + at, live ? cols - at : 0);
-    }
 #pragma unroll
     for (int i = 0; i < P; ++i)
 #pragma unroll
-      for (int j = 0; j < per; ++j) sum += E::get(q[i], j);
+      for (int j = 0; j < per; ++j) sum += x.get(i, j);
     const float about = group.sum(sum, 0.0f, 0)[0] * over;
     float d1 = 0.0f, d2 = 0.0f;
 #pragma unroll
@@ -156,7 +170,7 @@ __global__ __launch_bounds__(G* R) void layer_norm_kernel(const LayerNormArgs a)
       const int left = cols - (i * G + t) * per;
 #pragma unroll
       for (int j = 0; j < per; ++j) {
-        const float d = j < left ? E::get(q[i], j) - about : 0.0f;
+        const float d = j < left ? x.get(i, j) - about : 0.0f;
         d1 += d;
         d2 = __builtin_fmaf(d, d, d2);
       }
@@ -175,23 +189,38 @@ __global__ __launch_bounds__(G* R) void layer_norm_kernel(const LayerNormArgs a)
       if (at >= cols) break;
       float v[per];
 #pragma unroll
-      for (int j = 0; j < per; ++j)
-        v[j] = __builtin_fmaf(((E::get(q[i], j) - about) - off) * rstd, w[i][j], b[i][j]);
+      for (int j = 0; j < per; ++j) v[j] = __builtin_fmaf(((x.get(i, j) - about) - off) * rstd, w[i][j], b[i][j]);
       store_piece<BF16>(a.y, row * a.y_ld + at, cols - at, v);
     }
   }
 }
 
+// The partial sums of a workgroup lie as its threads hold them, dw then db: sum j
+// of piece i of thread t at (i per + j) G + t, so that they are written and read
+// in whole lines.
 template <bool BF16, int P, int G, int R>
 __global__ __launch_bounds__(G* R) void layer_norm_grad_kernel(const LayerNormArgs a) {
   typedef Elements<BF16> E;
-  constexpr int per = E::kPer;
-  // (the groups' sums of dw and db, one group at a time)
-  __shared__ float joined[R > 1 ? 2 * G * P * per : 1];
+  constexpr int per = E::kPer, kSums = P * G * per;
+  // (half of the groups' sums of dw and db)
+  __shared__ float joined[R > 1 ? R / 2 * 2 * kSums : 1];
   __shared__ GroupSum<G> sums[R];
   const int which = threadIdx.x / G, t = threadIdx.x % G, cols = a.cols;
   GroupSum<G>& group = sums[which];
   const float over = 1.0f / (float)cols;
+  constexpr bool kAhead = P == 1;  // (two pieces': 129 instead of 89 us)
+  const int64_t step = (int64_t)gridDim.x * R;
+  int64_t row = (int64_t)blockIdx.x * R + which;
+  Row<BF16, P, G> next_x, next_dy;
+  float next_mean = 0.0f, next_rstd = 0.0f;
+  auto load = [&](int64_t r) {
+    const bool there = r < a.rows;
+    next_x.load(a.x, there ? r * a.x_ld : 0, t, there ? cols : 0);
+    next_dy.load(a.dy, there ? r * a.dy_ld : 0, t, there ? cols : 0);
+    next_mean = there ? a.mean[r] : 0.0f;
+    next_rstd = there ? a.rstd[r] : 0.0f;
+  };
+  if (kAhead) load(row);
   float w[P][per], dw[P][per], db[P][per];
 #pragma unroll
   for (int i = 0; i < P; ++i) {
@@ -201,24 +230,18 @@ __global__ __launch_bounds__(G* R) void layer_norm_grad_kernel(const LayerNormAr
     for (int j = 0; j < per; ++j) dw[i][j] = db[i][j] = 0.0f;
   }
   int turn = 0;
-  for (int64_t first = (int64_t)blockIdx.x * R; first < a.rows; first += (int64_t)gridDim.x * R) {
-    const int64_t row = first + which;
+  for (int64_t first = (int64_t)blockIdx.x * R; first < a.rows; first += step, row += step) {
     const bool live = row < a.rows;
-    const int64_t x0 = live ? row * a.x_ld : 0, dy0 = live ? row * a.dy_ld : 0;
-    uint4v x[P], dy[P];
-#pragma unroll
-    for (int i = 0; i < P; ++i) {
-      const int at = (i * G + t) * per, left = live ? cols - at : 0;
-      x[i] = load_piece<BF16>(a.x, x0 + at, left);
-      dy[i] = load_piece<BF16>(a.dy, dy0 + at, left);
-    }
-    const float mean = live ? a.mean[row] : 0.0f, rstd = live ? a.rstd[row] : 0.0f;
+    if (!kAhead) load(row);
+    const Row<BF16, P, G> x = next_x, dy = next_dy;
+    const float mean = next_mean, rstd = next_rstd;
+    if (kAhead && first + step < a.rows) load(row + step);
     float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
     for (int i = 0; i < P; ++i)
 #pragma unroll
       for (int j = 0; j < per; ++j) {
-        const float d = E::get(dy[i], j), h = (E::get(x[i], j) - mean) * rstd, g = d * w[i][j];
+        const float d = dy.get(i, j), h = (x.get(i, j) - mean) * rstd, g = d * w[i][j];
         dw[i][j] = __builtin_fmaf(d, h, dw[i][j]);
         db[i][j] += d;
         s1 += g;
@@ -234,75 +257,77 @@ __global__ __launch_bounds__(G* R) void layer_norm_grad_kernel(const LayerNormAr
       float v[per];
 #pragma unroll
       for (int j = 0; j < per; ++j) {
-        const float h = (E::get(x[i], j) - mean) * rstd, g = E::get(dy[i], j) * w[i][j];
+        const float h = (x.get(i, j) - mean) * rstd, g = dy.get(i, j) * w[i][j];
         v[j] = (g - m1 - h * m2) * rstd;
       }
       store_piece<BF16>(a.dx, row * a.dx_ld + at, cols - at, v);
     }
   }
   if (!a.dweight && !a.dbias) return;
-  for (int r = 1; r < R; ++r) {
+#pragma unroll
+  for (int half = R / 2; half > 0; half /= 2) {
     __syncthreads();
-    if (which == r) {
+    if (which >= half && which < 2 * half) {
+      float* to = joined + (which - half) * 2 * kSums + t;
 #pragma unroll
-      for (int i = 0; i < P; ++i)
-#pragma unroll
-        for (int j = 0; j < per; ++j) {
-          joined[(i * per + j) * G + t] = dw[i][j];
-          joined[(P * per + i * per + j) * G + t] = db[i][j];
-        }
+      for (int i = 0; i < P * per; ++i) {
+        to[i * G] = dw[i / per][i % per];
+        to[kSums + i * G] = db[i / per][i % per];
+      }
     }
     __syncthreads();
-    if (which == 0) {
+    if (which < half) {
+      const float* from = joined + which * 2 * kSums + t;
 #pragma unroll
-      for (int i = 0; i < P; ++i)
-#pragma unroll
-        for (int j = 0; j < per; ++j) {
-          dw[i][j] += joined[(i * per + j) * G + t];
-          db[i][j] += joined[(P * per + i * per + j) * G + t];
-        }
+      for (int i = 0; i < P * per; ++i) {
+        dw[i / per][i % per] += from[i * G];
+        db[i / per][i % per] += from[kSums + i * G];
+      }
     }
   }
   if (which != 0) return;
-  float* to = a.partial + (int64_t)blockIdx.x * 2 * cols;
+  if (a.parts == 1) {  // one workgroup: these are the sums
 #pragma unroll
-  for (int i = 0; i < P; ++i) {
-    const int at = (i * G + t) * per;
+    for (int i = 0; i < P * per; ++i) {
+      const int c = (i / per * G + t) * per + i % per;
+      if (c >= cols) continue;
+      if (a.dweight) store_side(a.dweight, a.weight_bf16, c, dw[i / per][i % per]);
+      if (a.dbias) store_side(a.dbias, a.weight_bf16, c, db[i / per][i % per]);
+    }
+    return;
+  }
+  float* to = a.partial + (int64_t)blockIdx.x * 2 * kSums + t;
 #pragma unroll
-    for (int j = 0; j < per; ++j)
-      if (at + j < cols) {
-        if (a.parts == 1) {  // one workgroup: these are the sums
-          if (a.dweight) store_side(a.dweight, a.weight_bf16, at + j, dw[i][j]);
-          if (a.dbias) store_side(a.dbias, a.weight_bf16, at + j, db[i][j]);
-        } else {
-          to[at + j] = dw[i][j];
-          to[cols + at + j] = db[i][j];
-        }
-      }
+  for (int i = 0; i < P * per; ++i) {
+    to[i * G] = dw[i / per][i % per];
+    to[kSums + i * G] = db[i / per][i % per];
   }
 }
 
-// The partial sums of 64 columns, sixteen runs of them side by side.
-constexpr int kJoinCols = 64, kJoinRuns = 16;
+// The partial sums of 64 places, sixteen runs of them side by side.
+constexpr int kJoinPlaces = 64, kJoinRuns = 16;
 
-__global__ __launch_bounds__(kJoinCols* kJoinRuns) void join_sides_kernel(const LayerNormArgs a) {
-  __shared__ float part[kJoinRuns][kJoinCols];
-  const int c = blockIdx.x * kJoinCols + (threadIdx.x & 63), run = threadIdx.x >> 6;
+__global__ __launch_bounds__(kJoinPlaces* kJoinRuns) void join_sides_kernel(const LayerNormArgs a) {
+  __shared__ float part[kJoinRuns][kJoinPlaces];
+  const int n = blockIdx.x * kJoinPlaces + (threadIdx.x & 63), run = threadIdx.x >> 6;
   void* out = blockIdx.y ? a.dbias : a.dweight;
   if (!out) return;
-  const float* from = a.partial + (blockIdx.y ? a.cols : 0);
+  const float* from = a.partial + (blockIdx.y ? a.sums : 0) + n;
   float sum = 0.0f;
-  if (c < a.cols) {
+  if (n < a.sums) {
 #pragma unroll 8
-    for (int p = run; p < a.parts; p += kJoinRuns) sum += from[(int64_t)p * 2 * a.cols + c];
+    for (int p = run; p < a.parts; p += kJoinRuns) sum += from[(int64_t)p * 2 * a.sums];
   }
   part[run][threadIdx.x & 63] = sum;
   __syncthreads();
-  if (run != 0 || c >= a.cols) return;
+  if (run != 0 || n >= a.sums) return;
   sum = part[0][threadIdx.x];
 #pragma unroll
   for (int i = 1; i < kJoinRuns; ++i) sum += part[i][threadIdx.x];
-  store_side(out, a.weight_bf16, c, sum);
+  const int t = n & ((1 << a.group_bits) - 1), k = n >> a.group_bits;
+  const int j = k & ((1 << a.per_bits) - 1), i = k >> a.per_bits;
+  const int c = (((i << a.group_bits) + t) << a.per_bits) + j;
+  if (c < a.cols) store_side(out, a.weight_bf16, c, sum);
 }
 
 // ------------------------------------------------- rows beyond the registers
@@ -429,23 +454,52 @@ __global__ __launch_bounds__(kSideThreads) void long_sides_kernel(const LayerNor
     }
 }
 
-// Calls f with the shape of a row's group: the smallest that holds it.  False
-// where none does.
+// Calls f with the shape of a row's group, the smallest that holds it; false where
+// none does.  Of the sizes of group, pieces and workgroup that were tried, and
+// with the next row's loads ahead or not, these took the least time or nearly.
+//
+// Forward, 2^26 bfloat16 elements (two pieces a thread, 16 waves to a CU; 32 of one
+// piece: 65536 x 512 25 instead of 31 us):
+//   cols      1024  2048  4096  8192  16384
+//   us        45    44    46    47    53
+//   others    45-53 46-58 47-69 49-84 54-63    (one piece; four; more workgroups)
 template <bool BF16, class F>
-bool with_shape(int64_t cols, F f) {
+bool with_forward_shape(int64_t cols, F f) {
   constexpr int e = Elements<BF16>::kPer;
-  if (cols <= 64 * 1 * e) return f(Shape<BF16, 1, 64, 4>()), true;
-  if (cols <= 64 * 2 * e) return f(Shape<BF16, 2, 64, 4>()), true;
-  if (cols <= 256 * 1 * e) return f(Shape<BF16, 1, 256, 1>()), true;
-  if (cols <= 256 * 2 * e) return f(Shape<BF16, 2, 256, 1>()), true;
-  if (cols <= 512 * 2 * e) return f(Shape<BF16, 2, 512, 1>()), true;
-  if (cols <= 1024 * 2 * e) return f(Shape<BF16, 2, 1024, 1>()), true;
+  if (cols <= 64 * e) return f(Shape<BF16, 1, 64, 4>()), true;
+  if (cols <= 128 * e) return f(Shape<BF16, 2, 64, 4>()), true;
+  if (cols <= 256 * e) return f(Shape<BF16, 2, 128, 1>()), true;
+  if (cols <= 512 * e) return f(Shape<BF16, 2, 256, 1>()), true;
+  if (cols <= 1024 * e) return f(Shape<BF16, 2, 512, 1>()), true;
+  if (cols <= 2048 * e) return f(Shape<BF16, 2, 1024, 1>()), true;
+  if constexpr (!BF16) {  // (as many elements as bfloat16's two pieces)
+    if (cols <= 4096 * e) return f(Shape<BF16, 4, 1024, 1>()), true;
+  }
+  return false;
+}
+
+// Backward, with the join (one piece a thread, one workgroup of 16 waves to a CU,
+// whose sums of dw and db are the fewest; longer rows two pieces, none ahead):
+//   us        75    75    76    79    89
+//   others    75-86 76-95 77-92 79-90 93-129   (two pieces; smaller workgroups)
+template <bool BF16, class F>
+bool with_backward_shape(int64_t cols, F f) {
+  constexpr int e = Elements<BF16>::kPer;
+  if (cols <= 64 * e) return f(Shape<BF16, 1, 64, 16>()), true;
+  if (cols <= 128 * e) return f(Shape<BF16, 1, 128, 8>()), true;
+  if (cols <= 256 * e) return f(Shape<BF16, 1, 256, 4>()), true;
+  if (cols <= 512 * e) return f(Shape<BF16, 1, 512, 2>()), true;
+  if (cols <= 1024 * e) return f(Shape<BF16, 1, 1024, 1>()), true;
+  if (cols <= 2048 * e) return f(Shape<BF16, 2, 1024, 1>()), true;
+  if constexpr (!BF16) {  // (as many elements as bfloat16's two pieces)
+    if (cols <= 4096 * e) return f(Shape<BF16, 4, 1024, 1>()), true;
+  }
   return false;
 }
 
 template <bool BF16, int P, int G, int R>
 void forward(const LayerNormArgs& a, hipStream_t s, Shape<BF16, P, G, R>) {
-  const int64_t turns = (a.rows + R - 1) / R, most = 2048 * 256 / (G * R);
+  const int64_t turns = (a.rows + R - 1) / R, most = 256 * (P == 1 ? 2048 : 1024) / (G * R);
   layer_norm_kernel<BF16, P, G, R><<<dim3((unsigned)(turns < most ? turns : most)), dim3(G * R), 0, s>>>(a);
 }
 
@@ -456,13 +510,13 @@ void backward(const LayerNormArgs& a, hipStream_t s, Shape<BF16, P, G, R>) {
 
 template <bool BF16>
 void launch_forward(const LayerNormArgs& a, hipStream_t s) {
-  if (with_shape<BF16>(a.cols, [&](auto shape) { forward(a, s, shape); })) return;
+  if (with_forward_shape<BF16>(a.cols, [&](auto shape) { forward(a, s, shape); })) return;
   long_norm_kernel<BF16><<<dim3((unsigned)(a.rows < 1024 ? a.rows : 1024)), dim3(kLongThreads), 0, s>>>(a);
 }
 
 template <bool BF16>
 void launch_backward(const LayerNormArgs& a, hipStream_t s) {
-  if (with_shape<BF16>(a.cols, [&](auto shape) { backward(a, s, shape); })) return;
+  if (with_backward_shape<BF16>(a.cols, [&](auto shape) { backward(a, s, shape); })) return;
   constexpr int wide = kSideThreads * Elements<BF16>::kPer;
   if (a.dweight || a.dbias)
     long_sides_kernel<BF16><<<dim3((a.cols + wide - 1) / wide, a.parts), dim3(kSideThreads), 0, s>>>(a);
@@ -470,17 +524,31 @@ void launch_backward(const LayerNormArgs& a, hipStream_t s) {
     long_norm_grad_kernel<BF16><<<dim3((unsigned)(a.rows < 1024 ? a.rows : 1024)), dim3(kLongThreads), 0, s>>>(a);
 }
 
+int bits_of(int n) {
+  int b = 0;
+  while (1 << b < n) ++b;
+  return b;
+}
+
 }  // namespace
 
-int layer_norm_parts(int64_t rows, int64_t cols, bool bf16) {
-  int64_t parts = 0;
+LayerNormSums layer_norm_sums(int64_t rows, int64_t cols, bool bf16) {
+  LayerNormSums n;
   auto of = [&](auto shape) {
-    constexpr int r = decltype(shape)::kRows;
-    parts = (rows + r - 1) / r;
+    typedef decltype(shape) S;
+    // two turns of a workgroup at least: what it leaves costs as much as a row
+    const int64_t parts = (rows + 2 * S::kRows - 1) / (2 * S::kRows);
+    n.parts = (int)(parts < 1 ? 1 : parts < kNormMostParts ? parts : kNormMostParts);
+    n.sums = S::kCols;
+    n.group_bits = bits_of(S::kGroup);
+    n.per_bits = bits_of(S::kPer);
   };
-  const bool held = bf16 ? with_shape<true>(cols, of) : with_shape<false>(cols, of);
-  if (!held) return (int)(rows < 2 ? 2 : rows < 64 ? rows : 64);  // (two: the join kernel writes the result)
-  return (int)(parts < 1 ? 1 : parts < kNormMostParts ? parts : kNormMostParts);
+  if (bf16 ? with_backward_shape<true>(cols, of) : with_backward_shape<false>(cols, of)) return n;
+  n.parts = (int)(rows < 2 ? 2 : rows < 64 ? rows : 64);  // (two: the join kernel writes the result)
+  n.sums = (int)cols;
+  n.group_bits = 30;
+  n.per_bits = 0;
+  return n;
 }
 
 hipError_t launch_layer_norm(const LayerNormArgs& a, hipStream_t s) {
@@ -497,7 +565,7 @@ hipError_t launch_layer_norm_grad(const LayerNormArgs& a, hipStream_t s) {
   else
     launch_backward<false>(a, s);
   if ((a.dweight || a.dbias) && a.parts > 1)
-    join_sides_kernel<<<dim3((a.cols + kJoinCols - 1) / kJoinCols, 2), dim3(kJoinCols * kJoinRuns), 0, s>>>(a);
+    join_sides_kernel<<<dim3((a.sums + kJoinPlaces - 1) / kJoinPlaces, 2), dim3(kJoinPlaces * kJoinRuns), 0, s>>>(a);
   return hipGetLastError();
 }
 

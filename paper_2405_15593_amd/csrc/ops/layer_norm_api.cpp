@@ -83,8 +83,8 @@ int check_apart(const Range* written, int n_written, const Range* read, int n_re
 }
 
 uint64_t workspace_of(const microadam_rows* r) {
-  const int parts = layer_norm_parts(r->rows, r->cols, r->dtype == MICROADAM_BF16);
-  return parts > 1 ? (uint64_t)parts * 2 * (uint64_t)r->cols * sizeof(float) : 0;
+  const LayerNormSums n = layer_norm_sums(r->rows, r->cols, r->dtype == MICROADAM_BF16);
+  return n.parts > 1 ? (uint64_t)n.parts * 2 * (uint64_t)n.sums * sizeof(float) : 0;
 }
 
 }  // namespace
@@ -162,7 +162,11 @@ int microadam_layer_norm_grad(const microadam_rows* rows, const float* mean, con
   a.dweight = dweight;
   a.dbias = dbias;
   a.partial = (float*)workspace;
-  a.parts = layer_norm_parts(rows->rows, rows->cols, a.bf16);
+  const LayerNormSums n = layer_norm_sums(rows->rows, rows->cols, a.bf16);
+  a.parts = n.parts;
+  a.sums = n.sums;
+  a.group_bits = n.group_bits;
+  a.per_bits = n.per_bits;
   // (no rows: the sums are zeros)
   if (sides || (dx && a.rows > 0)) {
     const hipError_t e = launch_layer_norm_grad(a, (hipStream_t)stream);

@@ -6,7 +6,7 @@
 
 namespace microadam {
 
-constexpr int kNormMostParts = 512;  // partial sums of the weight's and bias's gradients, at most
+constexpr int kNormMostParts = 256;  // partial sums of the weight's and bias's gradients, at most
 
 struct LayerNormArgs {
   const void* x;
@@ -28,12 +28,16 @@ struct LayerNormArgs {
   int64_t dx_ld;
   void* dweight;  // NULL: not wanted
   void* dbias;
-  float* partial;  // [parts][2][cols]
-  int32_t parts;
+  float* partial;  // [parts][2][sums]
+  int32_t parts, sums, group_bits, per_bits;
 };
 
-// How many partial sums the backward pass of this size writes.
-int layer_norm_parts(int64_t rows, int64_t cols, bool bf16);
+// The partial sums of dw and db that the backward pass of this size writes: how
+// many, of how many places each, and where a column's is (k_layer_norm.hip).
+struct LayerNormSums {
+  int32_t parts, sums, group_bits, per_bits;
+};
+LayerNormSums layer_norm_sums(int64_t rows, int64_t cols, bool bf16);
 
 hipError_t launch_layer_norm(const LayerNormArgs& a, hipStream_t s);
 hipError_t launch_layer_norm_grad(const LayerNormArgs& a, hipStream_t s);

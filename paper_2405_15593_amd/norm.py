@@ -73,29 +73,28 @@ def _forward(x, weight, bias, eps, keep):
     given, rows, ld = _matrix(x)
     w, b = (t if t is None else t.contiguous() for t in (weight, bias))
     y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    mean = rstd = None
-    if keep:
-        mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=x.device).unbind(0)
+    stats = torch.empty(2 * rows, dtype=torch.float32, device=x.device) if keep else None   # means, then rstds
+    mean = None if stats is None else stats.data_ptr()
     with _on(x.device):
         microadam_layer_norm(microadam_rows(given.data_ptr(), _address(w), _address(b), rows, x.shape[-1], ld, eps, *codes),
-                             y.data_ptr(), x.shape[-1], _address(mean), _address(rstd),
+                             y.data_ptr(), x.shape[-1], mean, mean and mean + 4 * rows,
                              torch.cuda.current_stream(x.device.index).cuda_stream)
-    return y, mean, rstd
+    return y, stats
 
 
 class _LayerNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias, eps):
-        y, mean, rstd = _forward(x, weight, bias, eps, True)
+        y, stats = _forward(x, weight, bias, eps, True)
         # (the bias itself is not needed, its dtype is)
-        ctx.save_for_backward(x, weight, mean, rstd)
+        ctx.save_for_backward(x, weight, stats)
         ctx.settings = (eps, None if bias is None else bias.dtype)
         return y
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
-        x, weight, mean, rstd = ctx.saved_tensors
+        x, weight, stats = ctx.saved_tensors
         eps, bias_dtype = ctx.settings
         want_x, want_w, want_b, _ = ctx.needs_input_grad
         side_dtype = weight.dtype if weight is not None else bias_dtype or x.dtype
@@ -111,7 +110,8 @@ class _LayerNorm(torch.autograd.Function):
         with _on(dev):
             need = microadam_layer_norm_workspace(r) if want_w or want_b else 0
             workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
-            microadam_layer_norm_grad(r, mean.data_ptr(), rstd.data_ptr(), dy.data_ptr(), dy_ld, _address(dx), cols,
+            mean = stats.data_ptr()
+            microadam_layer_norm_grad(r, mean, mean + 4 * rows, dy.data_ptr(), dy_ld, _address(dx), cols,
                                       _address(dw), _address(db), _address(workspace), need,
                                       torch.cuda.current_stream(dev.index).cuda_stream)
         return dx, dw, db, None
