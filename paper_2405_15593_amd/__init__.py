@@ -433,7 +433,7 @@ def microadam_clip_workspace() -> int:
 
 def microadam_grad_norm(grads, numels, dtypes, n: int, norm_ptr: int, workspace_ptr: int, workspace_bytes: int,
                         stream: int = 0) -> None:
-    """`grads`, `numels`, `dtypes`: ctypes arrays of c_void_p, c_int64, c_int32."""
+    """`grads`, `numels`, `dtypes`: ctypes arrays of c_void_p, c_int64, c_int32, or their addresses."""
     _check(load().microadam_grad_norm(grads, numels, dtypes, n, norm_ptr, workspace_ptr, workspace_bytes, stream),
            "microadam_grad_norm")
 

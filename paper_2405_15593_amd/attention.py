@@ -13,6 +13,7 @@ Tensors are float32 or bfloat16 on a ROCm device, the dim a multiple of 8 up to
 from __future__ import annotations
 
 import contextlib
+import functools
 import math
 from typing import Optional
 
@@ -20,7 +21,7 @@ import torch
 
 from . import (MICROADAM_BF16, MICROADAM_F32, microadam_attention, microadam_attention_forward,
                microadam_attention_grad, microadam_attention_saved, microadam_attention_workspace, microadam_heads)
-from ._autograd import refuse_tangents
+from ._autograd import once_differentiable, refuse_tangents, stream_of
 
 _HERE = contextlib.nullcontext()
 _DTYPES = {torch.float32: MICROADAM_F32, torch.bfloat16: MICROADAM_BF16}
@@ -67,6 +68,20 @@ def _struct(q, k, v, key_lengths, causal, scale):
                                b, sq, k.shape[1], h, k.shape[2], d, scale, _DTYPES[q.dtype], 1 if causal else 0)
 
 
+@functools.lru_cache(maxsize=256)
+def _sizes(b, sq, sk, h, hk, d, code):
+    """(workspace forward, workspace of the gradients, saved) bytes."""
+    none = microadam_heads(None, 0, 0, 0)
+    given = microadam_attention(none, none, none, None, b, sq, sk, h, hk, d, 1.0, code, 0)
+    return (microadam_attention_workspace(given, False), microadam_attention_workspace(given, True),
+            microadam_attention_saved(given))
+
+
+def _sizes_of(q, k):
+    b, sq, h, d = q.shape
+    return _sizes(b, sq, k.shape[1], h, k.shape[2], d, _DTYPES[q.dtype])
+
+
 def _bytes(need, device):
     """(the tensor that holds them, address) of so many bytes at a multiple of
     256, where torch's allocator puts a tensor of its own."""
@@ -77,41 +92,48 @@ def _bytes(need, device):
 
 
 def _forward(q, k, v, key_lengths, causal, scale, keep):
-    out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    """(out, what the backward pass takes besides or None)."""
+    dev = q.device
+    out = torch.empty_like(q, memory_format=torch.contiguous_format)
     given = _struct(q, k, v, key_lengths, causal, scale)
-    with _on(q.device):
-        need, kept = microadam_attention_workspace(given, False), microadam_attention_saved(given) if keep else 0
-        store, address = _bytes(need, q.device)
-        saved, at = _bytes(kept, q.device)
-        microadam_attention_forward(given, _heads(out), at, kept, address, need,
-                                    torch.cuda.current_stream(q.device.index).cuda_stream)
+    need, _, kept = _sizes_of(q, k)
+    if not keep:
+        kept = 0
+    with _on(dev):
+        store, address = _bytes(need, dev)
+        saved, at = _bytes(kept, dev)
+        microadam_attention_forward(given, _heads(out), at, kept, address, need, stream_of(dev.index))
     return out, saved
+
+
+def _backward(ctx, dout):
+    """(autograd calls this on a thread of its own: what can be known before is
+    in ctx.settings)"""
+    q, k, v, key_lengths, out, saved = ctx.saved_tensors
+    causal, scale, need, kept = ctx.settings
+    q, k, v, dout = _rows(q), _rows(k), _rows(v), _rows(dout)
+    dq = torch.empty_like(q, memory_format=torch.contiguous_format)
+    dk = torch.empty_like(k, memory_format=torch.contiguous_format)
+    dv = torch.empty_like(v, memory_format=torch.contiguous_format)
+    given = _struct(q, k, v, key_lengths, causal, scale)
+    dev = q.device
+    with _on(dev):
+        store, address = _bytes(need, dev)
+        microadam_attention_grad(given, _heads(out), None if saved is None else saved.data_ptr(), kept, _heads(dout),
+                                 _heads(dq), _heads(dk), _heads(dv), address, need, stream_of(dev.index))
+    return dq, dk, dv, None, None, None
 
 
 class _Attention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, key_lengths, causal, scale):
-        out, saved = _forward(*(_rows(t) for t in (q, k, v)), key_lengths, causal, scale, True)
+        out, saved = _forward(_rows(q), _rows(k), _rows(v), key_lengths, causal, scale, True)
         ctx.save_for_backward(q, k, v, key_lengths, out, saved)
-        ctx.settings = (causal, scale)
+        _, need, kept = _sizes_of(q, k)
+        ctx.settings = (causal, scale, need, kept)
         return out
 
-    @staticmethod
-    @torch.autograd.function.once_differentiable
-    def backward(ctx, dout):
-        q, k, v, key_lengths, out, saved = ctx.saved_tensors
-        causal, scale = ctx.settings
-        q, k, v, dout = (_rows(t) for t in (q, k, v, dout))
-        dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
-        given = _struct(q, k, v, key_lengths, causal, scale)
-        with _on(q.device):
-            need = microadam_attention_workspace(given, True)
-            store, address = _bytes(need, q.device)
-            microadam_attention_grad(given, _heads(out), None if saved is None else saved.data_ptr(),
-                                     0 if saved is None else saved.numel(), _heads(dout), _heads(dq), _heads(dk),
-                                     _heads(dv), address, need,
-                                     torch.cuda.current_stream(q.device.index).cuda_stream)
-        return dq, dk, dv, None, None, None
+    backward = once_differentiable(_backward)
 
 
 def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, causal: bool = False,
@@ -131,4 +153,4 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, causal: bool
         key_lengths = key_lengths.contiguous()
     if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad):
         return _Attention.apply(q, k, v, key_lengths, causal, float(scale))
-    return _forward(*(_rows(t) for t in (q, k, v)), key_lengths, causal, float(scale), False)[0]
+    return _forward(_rows(q), _rows(k), _rows(v), key_lengths, causal, float(scale), False)[0]

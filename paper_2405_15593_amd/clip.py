@@ -12,14 +12,15 @@ current stream.
 from __future__ import annotations
 
 import contextlib
-import ctypes
+from array import array
+from operator import attrgetter
 from typing import Iterable, Optional
 
 import torch
 from torch.autograd.graph import increment_version
 
 from . import MICROADAM_BF16, MICROADAM_F32, microadam_clip_grads, microadam_clip_workspace, microadam_grad_norm
-from ._autograd import refuse_tangents
+from ._autograd import refuse_tangents, stream_of
 
 _HERE = contextlib.nullcontext()
 _DTYPES = {torch.float32: MICROADAM_F32, torch.bfloat16: MICROADAM_BF16}
@@ -46,27 +47,25 @@ def _dense(t: torch.Tensor) -> bool:
     return True
 
 
+# (per tensor of a list of hundreds, whose host time is the call's: mapped, not looped over)
+_data_ptr, _numel, _get_device, _is_contiguous = (torch.Tensor.data_ptr, torch.Tensor.numel, torch.Tensor.get_device,
+                                                  torch.Tensor.is_contiguous)
+_dtype, _requires_grad = attrgetter("dtype"), attrgetter("requires_grad")
+
+
 def _listed(what: str, grads: list):
-    """(addresses, numels, dtype codes) as arrays."""
-    device = grads[0].device
-    if device.type != "cuda":
-        raise ValueError(f"{what}: tensors on a ROCm device")
-    codes = []
-    differentiable = torch.is_grad_enabled()
-    for g in grads:
-        code = _DTYPES.get(g.dtype)
-        if code is None:
-            raise TypeError(f"{what}: float32 or bfloat16, not {g.dtype}")
-        codes.append(code)
-        if g.device != device:
-            raise ValueError(f"{what}: one device")
-        if differentiable and g.requires_grad:
-            raise NotImplementedError(f"{what}: no derivative; a gradient requires grad")
-        if not g.is_contiguous() and not _dense(g):
-            raise ValueError(f"{what}: a gradient with gaps or overlaps in memory")
-    n = len(grads)
-    return ((ctypes.c_void_p * n)(*[g.data_ptr() for g in grads]), (ctypes.c_int64 * n)(*[g.numel() for g in grads]),
-            (ctypes.c_int32 * n)(*codes), n)
+    """The addresses, numels and dtype codes as arrays."""
+    if set(map(_get_device, grads)) != {grads[0].device.index} or not grads[0].is_cuda:
+        raise ValueError(f"{what}: tensors on one ROCm device")
+    try:
+        codes = array("i", map(_DTYPES.__getitem__, map(_dtype, grads)))
+    except KeyError as e:
+        raise TypeError(f"{what}: float32 or bfloat16, not {e.args[0]}") from None
+    if torch.is_grad_enabled() and any(map(_requires_grad, grads)):
+        raise NotImplementedError(f"{what}: no derivative; a gradient requires grad")
+    if not all(map(_is_contiguous, grads)) and not all(map(_dense, grads)):
+        raise ValueError(f"{what}: a gradient with gaps or overlaps in memory")
+    return array("Q", map(_data_ptr, grads)), array("q", map(_numel, grads)), codes
 
 
 def _workspace(device, workspace):
@@ -86,13 +85,14 @@ def grad_norm(grads: Iterable[torch.Tensor], *, workspace: Optional[torch.Tensor
     if not grads:
         raise ValueError("grads: at least one tensor")
     refuse_tangents("grad_norm", grads)
-    given = _listed("grads", grads)
+    arrays = _listed("grads", grads)
+    given = [a.buffer_info()[0] for a in arrays]
     device = grads[0].device
     with _on(device):
         norm = torch.empty((), dtype=torch.float32, device=device)
         address, size, keep = _workspace(device, workspace)
-        microadam_grad_norm(*given, norm.data_ptr(), address, size,
-                            torch.cuda.current_stream(device.index).cuda_stream)
+        microadam_grad_norm(*given, len(grads), norm.data_ptr(), address, size,
+                            stream_of(device.index))
     return norm
 
 
@@ -106,13 +106,14 @@ def clip_grads(grads: Iterable[torch.Tensor], max_norm: float, *, eps: float = 1
     if not grads:
         raise ValueError("grads: at least one tensor")
     refuse_tangents("clip_grads", grads)
-    given = _listed("grads", grads)
+    arrays = _listed("grads", grads)
+    given = [a.buffer_info()[0] for a in arrays]
     device = grads[0].device
     with _on(device):
         norm = torch.empty((), dtype=torch.float32, device=device)
         address, size, keep = _workspace(device, workspace)
-        microadam_clip_grads(*given, max_norm, eps, norm.data_ptr(), address, size,
-                             torch.cuda.current_stream(device.index).cuda_stream)
+        microadam_clip_grads(*given, len(grads), max_norm, eps, norm.data_ptr(), address, size,
+                             stream_of(device.index))
     increment_version(grads)
     return norm
 

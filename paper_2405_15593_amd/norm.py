@@ -10,13 +10,14 @@ copied first.  Work is queued on torch's current stream.
 from __future__ import annotations
 
 import contextlib
+import functools
 from typing import Optional
 
 import torch
 
 from . import (MICROADAM_BF16, MICROADAM_F32, microadam_layer_norm, microadam_layer_norm_grad,
                microadam_layer_norm_workspace, microadam_rows)
-from ._autograd import refuse_tangents
+from ._autograd import once_differentiable, refuse_tangents, stream_of
 
 _HERE = contextlib.nullcontext()
 _DTYPES = {torch.float32: MICROADAM_F32, torch.bfloat16: MICROADAM_BF16}
@@ -64,57 +65,69 @@ def _check(x, weight, bias):
     return code, code if side is None else _DTYPES[side]
 
 
+@functools.lru_cache(maxsize=256)
+def _workspace_bytes(rows, cols, code):
+    return microadam_layer_norm_workspace(microadam_rows(None, None, None, rows, cols, cols, 0.0, code, code))
+
+
 def _address(t):
     return None if t is None else t.data_ptr()
 
 
 def _forward(x, weight, bias, eps, keep):
+    """(y, the statistics or None, rows, dtype codes)."""
     codes = _check(x, weight, bias)
     given, rows, ld = _matrix(x)
-    w, b = (t if t is None else t.contiguous() for t in (weight, bias))
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    stats = torch.empty(2 * rows, dtype=torch.float32, device=x.device) if keep else None   # means, then rstds
+    w, b = (t if t is None or t.is_contiguous() else t.contiguous() for t in (weight, bias))
+    cols, dev = x.shape[-1], x.device
+    y = torch.empty_like(x, memory_format=torch.contiguous_format)
+    stats = torch.empty(2 * rows, dtype=torch.float32, device=dev) if keep else None   # means, then rstds
     mean = None if stats is None else stats.data_ptr()
-    with _on(x.device):
-        microadam_layer_norm(microadam_rows(given.data_ptr(), _address(w), _address(b), rows, x.shape[-1], ld, eps, *codes),
-                             y.data_ptr(), x.shape[-1], mean, mean and mean + 4 * rows,
-                             torch.cuda.current_stream(x.device.index).cuda_stream)
-    return y, stats
+    with _on(dev):
+        r = microadam_rows(given.data_ptr(), _address(w), _address(b), rows, cols, ld, eps, *codes)
+        microadam_layer_norm(r, y.data_ptr(), cols, mean, mean and mean + 4 * rows, stream_of(dev.index))
+    return y, stats, rows, codes
+
+
+def _backward(ctx, dy):
+    """(autograd calls this on a thread of its own: what can be known before is
+    in ctx.settings, and the usual layouts take the short way)"""
+    x, weight, stats = ctx.saved_tensors
+    want_x, want_w, want_b, _ = ctx.needs_input_grad
+    rows, cols, eps, codes, side, need = ctx.settings
+    plain, ld = x.is_contiguous(), cols
+    if not plain:
+        x, _, ld = _matrix(x)
+    if not dy.is_contiguous():
+        dy, _, dy_ld = _matrix(dy)
+    else:
+        dy_ld = cols
+    w = weight if weight is None or weight.is_contiguous() else weight.contiguous()
+    dx = (torch.empty_like(x) if plain else x.new_empty(x.shape)) if want_x else None
+    dw = stats.new_empty(cols, dtype=side) if want_w else None
+    db = stats.new_empty(cols, dtype=side) if want_b else None
+    workspace = stats.new_empty(need) if need else None
+    r = microadam_rows(x.data_ptr(), None if w is None else w.data_ptr(), None, rows, cols, ld, eps, *codes)
+    mean, dev = stats.data_ptr(), x.device
+    with _on(dev):
+        microadam_layer_norm_grad(r, mean, mean + 4 * rows, dy.data_ptr(), dy_ld, None if dx is None else dx.data_ptr(),
+                                  cols, None if dw is None else dw.data_ptr(), None if db is None else db.data_ptr(),
+                                  None if workspace is None else workspace.data_ptr(), 4 * need, stream_of(dev.index))
+    return dx, dw, db, None
 
 
 class _LayerNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias, eps):
-        y, stats = _forward(x, weight, bias, eps, True)
-        # (the bias itself is not needed, its dtype is)
+        y, stats, rows, codes = _forward(x, weight, bias, eps, True)
         ctx.save_for_backward(x, weight, stats)
-        ctx.settings = (eps, None if bias is None else bias.dtype)
+        cols = x.shape[-1]
+        side = weight.dtype if weight is not None else bias.dtype if bias is not None else x.dtype
+        need = _workspace_bytes(rows, cols, codes[0]) if ctx.needs_input_grad[1] or ctx.needs_input_grad[2] else 0
+        ctx.settings = (rows, cols, eps, codes, side, need // 4)
         return y
 
-    @staticmethod
-    @torch.autograd.function.once_differentiable
-    def backward(ctx, dy):
-        x, weight, stats = ctx.saved_tensors
-        eps, bias_dtype = ctx.settings
-        want_x, want_w, want_b, _ = ctx.needs_input_grad
-        side_dtype = weight.dtype if weight is not None else bias_dtype or x.dtype
-        cols, dev = x.shape[-1], x.device
-        given, rows, ld = _matrix(x)
-        dy, _, dy_ld = _matrix(dy)
-        w = weight if weight is None else weight.contiguous()
-        dx = torch.empty(x.shape, dtype=x.dtype, device=dev) if want_x else None
-        dw = torch.empty(cols, dtype=side_dtype, device=dev) if want_w else None
-        db = torch.empty(cols, dtype=side_dtype, device=dev) if want_b else None
-        r = microadam_rows(given.data_ptr(), _address(w), None, rows, cols, ld, eps, _DTYPES[x.dtype],
-                           _DTYPES[side_dtype])
-        with _on(dev):
-            need = microadam_layer_norm_workspace(r) if want_w or want_b else 0
-            workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
-            mean = stats.data_ptr()
-            microadam_layer_norm_grad(r, mean, mean + 4 * rows, dy.data_ptr(), dy_ld, _address(dx), cols,
-                                      _address(dw), _address(db), _address(workspace), need,
-                                      torch.cuda.current_stream(dev.index).cuda_stream)
-        return dx, dw, db, None
+    backward = once_differentiable(_backward)
 
 
 def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, *,
