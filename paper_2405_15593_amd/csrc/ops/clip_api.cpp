@@ -19,6 +19,10 @@ using namespace microadam;
 namespace {
 
 constexpr uint64_t kWorkspace = (uint64_t)kClipSlots * sizeof(double);
+// The last-level cache's 256 MiB: beyond it reads past the caches take 549 instead
+// of 652 us for 3.8 GB, and the scaling 1440 instead of 1510; a list of 53 MB is
+// scaled in 21 instead of 18 us.
+constexpr int64_t kCached = (int64_t)256 << 20;
 constexpr int64_t kMaxNumel = (int64_t)1 << 40;
 static_assert(sizeof(ClipArgs) <= 4096, "kernel arguments");
 
@@ -100,11 +104,13 @@ int queue(const void* const* grads, const int64_t* numels, const int32_t* dtypes
   a.max_norm = max_norm;
   a.eps = eps;
   // one number of slots for all launches of the call
-  int64_t most = 1;
+  int64_t most = 1, chunks = 0;
   for (int32_t i = 0; i < n;) {
     i = fill(a, grads, numels, dtypes, n, i);
+    chunks += a.first[a.n];
     most = std::max(most, (int64_t)a.first[a.n]);
   }
+  a.past = chunks > kCached / kClipChunk ? 1 : 0;
   a.slots = (int32_t)std::min<int64_t>(kClipSlots, most);
   hipError_t e;
   std::vector<int32_t> starts;

@@ -21,6 +21,7 @@ struct ClipArgs {
   int32_t n;
   double* partial;  // kClipSlots
   int32_t slots;    // in use
+  int32_t past;     // the whole list is more than the caches hold
   int32_t add;      // to what an earlier launch of the call left there
   double max_norm, eps;
   float* norm;  // NULL: not this launch's to write

@@ -17,6 +17,7 @@ namespace microadam {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kScaleGroups = 4096;  // workgroups of the scaling pass, at most
 constexpr int kPieces = (int)(kClipChunk / 16 / kThreads);  // a thread's, of a chunk
 
 __device__ inline double wave_sum(double x) {
@@ -73,14 +74,27 @@ __device__ inline void each_inside(uint64_t p, uint64_t at, uint64_t end, F f) {
   }
 }
 
-template <bool BF16>
+// A list that no cache holds is read and written past them.
+template <bool PAST>
+__device__ inline uint4v load_piece(const uint4v* p) {
+  return PAST ? __builtin_nontemporal_load(p) : *p;
+}
+template <bool PAST>
+__device__ inline void store_piece(uint4v* p, const uint4v& q) {
+  if (PAST)
+    __builtin_nontemporal_store(q, p);
+  else
+    *p = q;
+}
+
+template <bool BF16, bool PAST>
 __device__ inline double chunk_squares(uint64_t from, uint64_t at, uint64_t end) {
   typedef Elements<BF16> E;
   double sum = 0.0;
   if (from >= at && from + kClipChunk <= end) {
     uint4v q[kPieces];
 #pragma unroll
-    for (int i = 0; i < kPieces; ++i) q[i] = ((const uint4v*)from)[i * kThreads + threadIdx.x];
+    for (int i = 0; i < kPieces; ++i) q[i] = load_piece<PAST>((const uint4v*)from + i * kThreads + threadIdx.x);
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) sum += squares<BF16>(q[i]);
     return sum;
@@ -99,6 +113,7 @@ __device__ inline double chunk_squares(uint64_t from, uint64_t at, uint64_t end)
   return sum;
 }
 
+template <bool PAST>
 __global__ __launch_bounds__(kThreads) void square_sums_kernel(const ClipArgs a) {
   double sum = 0.0;
   const int chunks = a.first[a.n];
@@ -107,7 +122,7 @@ __global__ __launch_bounds__(kThreads) void square_sums_kernel(const ClipArgs a)
     const bool bf16 = a.at[t] & 1;
     const uint64_t at = a.at[t] & ~(uint64_t)1, end = a.end[t];
     const uint64_t from = (at & ~(uint64_t)15) + (uint64_t)(c - a.first[t]) * kClipChunk;
-    sum += bf16 ? chunk_squares<true>(from, at, end) : chunk_squares<false>(from, at, end);
+    sum += bf16 ? chunk_squares<true, PAST>(from, at, end) : chunk_squares<false, PAST>(from, at, end);
   }
   sum = block_sum(sum);
   if (threadIdx.x == 0) a.partial[blockIdx.x] = a.add ? a.partial[blockIdx.x] + sum : sum;
@@ -137,16 +152,17 @@ __device__ inline uint4v scale_piece(const uint4v& q, double c) {
   return E::put(v);
 }
 
-template <bool BF16>
+template <bool BF16, bool PAST>
 __device__ inline void scale_chunk(uint64_t from, uint64_t at, uint64_t end, double c) {
   typedef Elements<BF16> E;
   if (from >= at && from + kClipChunk <= end) {
     uint4v* p = (uint4v*)from;
     uint4v q[kPieces];
 #pragma unroll
-    for (int i = 0; i < kPieces; ++i) q[i] = p[i * kThreads + threadIdx.x];
+    for (int i = 0; i < kPieces; ++i) q[i] = load_piece<PAST>(p + i * kThreads + threadIdx.x);
 #pragma unroll
-    for (int i = 0; i < kPieces; ++i) p[i * kThreads + threadIdx.x] = scale_piece<BF16>(q[i], c);
+    for (int i = 0; i < kPieces; ++i)
+      store_piece<PAST>(p + i * kThreads + threadIdx.x, scale_piece<BF16>(q[i], c));
     return;
   }
   for (int i = threadIdx.x; i < (int)(kClipChunk / 16); i += kThreads) {
@@ -159,6 +175,7 @@ __device__ inline void scale_chunk(uint64_t from, uint64_t at, uint64_t end, dou
   }
 }
 
+template <bool PAST>
 __global__ __launch_bounds__(kThreads) void scale_grads_kernel(const ClipArgs a) {
   const double norm = norm_of(a);
   if (a.norm && blockIdx.x == 0 && threadIdx.x == 0) *a.norm = (float)norm;
@@ -170,16 +187,19 @@ __global__ __launch_bounds__(kThreads) void scale_grads_kernel(const ClipArgs a)
     const uint64_t at = a.at[t] & ~(uint64_t)1, end = a.end[t];
     const uint64_t from = (at & ~(uint64_t)15) + (uint64_t)(k - a.first[t]) * kClipChunk;
     if (bf16)
-      scale_chunk<true>(from, at, end, c);
+      scale_chunk<true, PAST>(from, at, end, c);
     else
-      scale_chunk<false>(from, at, end, c);
+      scale_chunk<false, PAST>(from, at, end, c);
   }
 }
 
 }  // namespace
 
 hipError_t launch_square_sums(const ClipArgs& a, hipStream_t s) {
-  square_sums_kernel<<<dim3(a.slots), dim3(kThreads), 0, s>>>(a);
+  if (a.past)
+    square_sums_kernel<true><<<dim3(a.slots), dim3(kThreads), 0, s>>>(a);
+  else
+    square_sums_kernel<false><<<dim3(a.slots), dim3(kThreads), 0, s>>>(a);
   return hipGetLastError();
 }
 
@@ -189,8 +209,11 @@ hipError_t launch_grad_norm(const ClipArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_scale_grads(const ClipArgs& a, hipStream_t s) {
-  const int chunks = a.first[a.n], grid = chunks < 1 ? 1 : chunks < kClipSlots ? chunks : kClipSlots;
-  scale_grads_kernel<<<dim3(grid), dim3(kThreads), 0, s>>>(a);
+  const int chunks = a.first[a.n], grid = chunks < 1 ? 1 : chunks < kScaleGroups ? chunks : kScaleGroups;
+  if (a.past)
+    scale_grads_kernel<true><<<dim3(grid), dim3(kThreads), 0, s>>>(a);
+  else
+    scale_grads_kernel<false><<<dim3(grid), dim3(kThreads), 0, s>>>(a);
   return hipGetLastError();
 }
 

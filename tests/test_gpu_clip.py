@@ -77,6 +77,24 @@ def test_lists(name, start, dtype):
     assert torch.equal(flat[:start], whole[:start]) and torch.equal(flat[-5:], whole[-5:])
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+def test_more_than_the_caches_hold(dtype):
+    """A list of 300 MB, in binary64 on the device."""
+    print(f"[clip] 300 MB {dtype}", flush=True)
+    n = 300_000_000 // dtype.itemsize
+    flat, grads = bucket([(n // 3,), (7,), (n - n // 3 - 7,)], dtype, start=1)
+    before = flat.clone()
+    want = math.sqrt(sum(float(p.double().square().sum()) for p in before[1:-5].split(1 << 26)))
+    limit = 0.3 * want
+    check_norm(grad_norm(grads), want)
+    check_norm(clip_grads(grads, limit), want)
+    factor = limit / (want + 1e-6)
+    for a, b in zip(flat[1:-5].split(1 << 26), before[1:-5].split(1 << 26)):
+        exact = b.double() * factor
+        assert bool(((a.double() - exact).abs() <= exact.abs() * HALF[dtype] * SLACK + 2.0 ** -134).all())
+    assert torch.equal(flat[:1], before[:1]) and torch.equal(flat[-5:], before[-5:])
+
+
 def test_mixed_types_and_orders():
     """Both dtypes in one list, transposed gradients, gradients in any order of
     addresses."""
