@@ -34,6 +34,18 @@ struct AttentionArgs {
 
 constexpr int kMostParts = 256;
 
+// Whether 128 rows (or keys) to a workgroup are too few workgroups for 256 CUs, so
+// that its four waves had better share 32 of them and take every fourth tile of
+// the others.  One workgroup to a CU, two for binary32, whose matrix instructions
+// leave no time over.  Forward / backward in us, shared or not:
+//   bfloat16  1 x 2048 x 8 heads of 128, causal  128 workgroups  26 / 81   47 / 159
+//             2 x  512 x 32           "          256             23 / 94   20 / 56
+//   binary32  4 x 1024 x 8 heads of 64, causal   256             54 / 193  86 / 267
+//             32 x 512 x 4            "          512             64 / 257  60 / 196
+inline bool few_groups(const AttentionArgs& a, int positions) {
+  return (int64_t)((positions + 127) / 128) * a.kv_heads * a.batch < (a.bf16 ? 256 : 512);
+}
+
 // How many parts a forward call's keys are split into; 0: not at all.
 int32_t attention_parts(const AttentionArgs& a);
 

@@ -26,6 +26,7 @@ __device__ inline void scores(float16v (&s)[KEYS / 32], const uint8_t* tile, con
                               const Frag<BF16> (&q)[D / 16]) {
   constexpr int n = KEYS / 32;
   schedule_here();
+  __builtin_amdgcn_s_setprio(1);
 #pragma unroll
   for (int i = 0; i < n; ++i) s[i] = zeros();
 #pragma unroll
@@ -34,6 +35,7 @@ __device__ inline void scores(float16v (&s)[KEYS / 32], const uint8_t* tile, con
     for (int i = 0; i < n; ++i) multiply(s[i], Tile<BF16, D, KEYS>::along(tile, at, 32 * i, step), q[step]);
   if (BF16) interleave<4, D / 16 * n, D / 16 * n>();
   schedule_here();
+  __builtin_amdgcn_s_setprio(0);
 }
 
 template <int N>
@@ -149,12 +151,7 @@ __global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attention_kernel(const
   __shared__ __align__(16) uint8_t lds[2][2][T::kBytes];  // [turn][keys, values]
   const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
   const int tiles = (a.rows + kRows - 1) / kRows;
-  int block = blockIdx.x, part = 0;
-  if (a.parts) {
-    part = block % a.parts;
-    block /= a.parts;
-  }
-  const Work work = work_of(block, a.kv_heads * a.batch);
+  const Work work = work_of(blockIdx.x, a.kv_heads * a.batch);
   const int tile = tiles - 1 - work.order, head_of = work.head;  // (the last rows see the most keys)
   const typename T::Lane places(lane);
   const int kv_head = head_of % a.kv_heads, batch = head_of / a.kv_heads;
@@ -173,7 +170,7 @@ __global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attention_kernel(const
     q[s] = load_frag<BF16>(a.q.at, q_at + d, live && d < a.dim);
   }
 
-  const Part own = part_of(a, part, (last_key(a, tile * kRows, kRows, length) + keys - 1) / keys);
+  const int turns = (last_key(a, tile * kRows, kRows, length) + keys - 1) / keys;
 
   Staged<BF16, D, keys, kThreads> next_k, next_v;
   constexpr int size = T::kSize;
@@ -195,14 +192,14 @@ __global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attention_kernel(const
   float16v out[D / 32];
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) out[i] = zeros();
-  if (own.first < own.last) {
-    load(own.first);
-    store(own.first);
+  if (turns > 0) {
+    load(0);
+    store(0);
   }
   wait_all();
   __syncthreads();
-  for (int turn = own.first; turn < own.last; ++turn) {
-    if (turn + 1 < own.last) load(turn + 1);
+  for (int turn = 0; turn < turns; ++turn) {
+    if (turn + 1 < turns) load(turn + 1);
     const int first = turn * keys;
     if (first < most) {
       float16v s[keys / 32];
@@ -210,16 +207,16 @@ __global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attention_kernel(const
       if (first + keys > least) mask(s, first, limit, lane, -infinity());
       add_tile<BF16, D, keys>(s, lds[turn & 1][1], places, a.c, m, l, out);
     }
-    if (turn + 1 < own.last) store(turn + 1);
+    if (turn + 1 < turns) store(turn + 1);
     __syncthreads();
   }
 
   l = add_halves(l);
-  if (live) finish<BF16, D>(a, head_of, batch, row, at, part, m, l, out, lane);
+  if (live) finish<BF16, D>(a, head_of, batch, row, at, 0, m, l, out, lane);
 }
 
-// Up to 32 rows of a key head, a token's or a few: the four waves take the same
-// rows and every fourth tile of the part's keys, each on its own way through its
+// Where there are few rows for the CUs, a token's or some hundred: the four waves
+// of a workgroup take the same 32 rows and every fourth tile of the part's keys, each on its own way through its
 // own place in LDS, and are joined at the end.
 constexpr int kFewRows = 32, kFewKeys = 32;
 
@@ -231,14 +228,17 @@ __global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attention_few_kernel(c
   __shared__ __align__(16) uint8_t lds[kWaves][2][T::kBytes];
   static_assert((kWaves - 1) * kSums * 64 * sizeof(float) <= sizeof(lds), "the waves' sums");
   const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
-  int head_of = blockIdx.x, part = 0;
+  int block = blockIdx.x, part = 0;
   if (a.parts) {
-    part = head_of % a.parts;
-    head_of /= a.parts;
+    part = block % a.parts;
+    block /= a.parts;
   }
+  const int tiles = (a.rows + kFewRows - 1) / kFewRows;
+  const Work work = work_of(block, a.kv_heads * a.batch);
+  const int tile = tiles - 1 - work.order, head_of = work.head;  // (the last rows see the most keys)
   const int kv_head = head_of % a.kv_heads, batch = head_of / a.kv_heads;
   const int length = keys_of(a, batch);
-  const Part own = part_of(a, part, (last_key(a, 0, kFewRows, length) + kFewKeys - 1) / kFewKeys);
+  const Part own = part_of(a, part, (last_key(a, tile * kFewRows, kFewRows, length) + kFewKeys - 1) / kFewKeys);
 
   Staged<BF16, D, kFewKeys, 64> next_k, next_v;
   constexpr int size = T::kSize;
@@ -254,7 +254,7 @@ __global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attention_few_kernel(c
   };
   if (turn < own.last) load(turn);
 
-  const int row = lane & 31;
+  const int row = tile * kFewRows + (lane & 31);
   const bool live = row < a.rows;
   const RowAt at = row_at(a, kv_head, live ? row : 0);
   const int limit = live ? limit_of(a, at.query, length) : 0;
@@ -391,15 +391,17 @@ __global__ __launch_bounds__(kThreads) void attention_join_kernel(const Attentio
   if (a.lse && lane == 0) a.lse[stat] = sum == 0.0f ? infinity() : top + __builtin_amdgcn_logf(sum);
 }
 
+bool few_rows(const AttentionArgs& a) { return a.rows <= kFewRows || few_groups(a, a.rows); }
+
 template <bool BF16, int D>
 void launch_rows(const AttentionArgs& a, hipStream_t s) {
   const int heads = a.kv_heads * a.batch, parts = a.parts ? a.parts : 1;
-  if (a.rows <= kFewRows) {
-    attention_few_kernel<BF16, D><<<dim3((unsigned)(heads * parts)), dim3(kThreads), 0, s>>>(a);
-  } else {
-    const int tiles = (a.rows + kRows - 1) / kRows;
-    attention_kernel<BF16, D><<<dim3((unsigned)(tiles * heads * parts)), dim3(kThreads), 0, s>>>(a);
-  }
+  const bool few = few_rows(a);
+  const int tiles = few ? (a.rows + kFewRows - 1) / kFewRows : (a.rows + kRows - 1) / kRows;
+  if (few)
+    attention_few_kernel<BF16, D><<<dim3((unsigned)(tiles * heads * parts)), dim3(kThreads), 0, s>>>(a);
+  else
+    attention_kernel<BF16, D><<<dim3((unsigned)(tiles * heads)), dim3(kThreads), 0, s>>>(a);
   if (a.parts) {
     const int64_t waves = kThreads / 64, blocks = ((int64_t)heads * a.rows + waves - 1) / waves;
     attention_join_kernel<BF16><<<dim3((unsigned)blocks), dim3(kThreads), 0, s>>>(a);
@@ -424,11 +426,10 @@ void launch_dim(const AttentionArgs& a, hipStream_t s) {
 // as many parts as give two to a CU, of at least so many tiles that a part's
 // work is worth the join (4 to 5 us with its launch).
 int32_t attention_parts(const AttentionArgs& a) {
-  const bool few = a.rows <= kFewRows;
-  const int64_t heads = (int64_t)a.kv_heads * a.batch, groups = few ? heads : heads * ((a.rows + kRows - 1) / kRows);
+  if (!few_rows(a)) return 0;
+  const int64_t groups = (int64_t)((a.rows + kFewRows - 1) / kFewRows) * a.kv_heads * a.batch;
   if (groups < 1 || groups >= 256) return 0;
-  const int64_t tile = few ? kFewKeys : a.bf16 ? kKeys<true> : kKeys<false>;
-  const int64_t most = (a.keys + tile - 1) / tile / (few ? 8 : 4);
+  const int64_t most = (a.keys + kFewKeys - 1) / kFewKeys / 8;
   int64_t parts = (512 + groups - 1) / groups;
   parts = parts < most ? parts : most;
   parts = parts < kMostParts ? parts : kMostParts;

@@ -15,22 +15,51 @@ namespace microadam {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / 64;
 constexpr int kRows = 128;      // of a workgroup, rows or keys
 constexpr int kTile = 32;       // keys or rows of a tile
 
-template <bool BF16, int D>
-__global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attention_dq_kernel(const AttentionArgs a) {
+// SPLIT: where there are few rows (keys) for the CUs, a workgroup has 32 of them
+// for all four waves, which take every fourth tile, each on its own way through
+// its own place in LDS, and are joined at the end.
+
+// The sums of the waves' same results, in wave 0: `sums` is free and has room for
+// three waves' results.
+template <int N>
+__device__ inline void join_waves(float16v (&x)[N], float* sums, int wave, int lane) {
+  __syncthreads();
+  if (wave > 0) {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sums[(((wave - 1) * N + i) * 16 + r) * 64 + lane] = x[i][r];
+  }
+  __syncthreads();
+  if (wave > 0) return;
+#pragma unroll
+  for (int w = 0; w < kWaves - 1; ++w)
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[i][r] += sums[((w * N + i) * 16 + r) * 64 + lane];
+}
+
+template <bool BF16, int D, bool SPLIT>
+__global__ __launch_bounds__(kThreads, BF16 && !SPLIT ? 2 : 1) void attention_dq_kernel(const AttentionArgs a) {
   typedef Tile<BF16, D, kTile> T;
-  __shared__ __align__(16) uint8_t lds[2][2][T::kBytes];  // [turn][keys, values]
+  constexpr int own_rows = SPLIT ? 32 : kRows;
+  __shared__ __align__(16) uint8_t lds[SPLIT ? kWaves : 2][2][T::kBytes];  // [wave or turn][keys, values]
+  static_assert(!SPLIT || sizeof(lds) >= (kWaves - 1) * D / 32 * 16 * 64 * sizeof(float), "the waves' sums");
   const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
-  const int tiles = (a.rows + kRows - 1) / kRows;
+  const int stager = SPLIT ? lane : (int)threadIdx.x;
+  const int tiles = (a.rows + own_rows - 1) / own_rows;
   const Work work = work_of(blockIdx.x, a.kv_heads * a.batch);
   const int tile = tiles - 1 - work.order, head_of = work.head;  // (the last rows see the most keys)
   const typename T::Lane places(lane);
   const int kv_head = head_of % a.kv_heads, batch = head_of / a.kv_heads;
   const int length = keys_of(a, batch);
 
-  const int row = tile * kRows + wave * 32 + (lane & 31);
+  const int row = tile * own_rows + (SPLIT ? 0 : wave * 32) + (lane & 31);
   const bool live = row < a.rows;
   const RowAt at = row_at(a, kv_head, live ? row : 0);
   const int limit = live ? limit_of(a, at.query, length) : 0;
@@ -60,41 +89,39 @@ __global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attention_dq_kernel(co
   }
   delta = add_halves(delta);
   const float lse = live ? a.lse[stat] : infinity();
-  if (live && lane < 32) a.delta[stat] = delta;
+  if (live && lane < 32 && (!SPLIT || wave == 0)) a.delta[stat] = delta;
 
-  const int turns = (last_key(a, tile * kRows, kRows, length) + kTile - 1) / kTile;
+  const int turns = (last_key(a, tile * own_rows, own_rows, length) + kTile - 1) / kTile;
 
-  Staged<BF16, D, kTile, kThreads> next_k, next_v;
+  Staged<BF16, D, kTile, SPLIT ? 64 : kThreads> next_k, next_v;
   constexpr int size = T::kSize;
   const int64_t k_pos = a.k.pos * size, v_pos = a.v.pos * size;
   const uint8_t* k_at = (const uint8_t*)a.k.at + (batch * a.k.batch + kv_head * a.k.head) * size;
   const uint8_t* v_at = (const uint8_t*)a.v.at + (batch * a.v.batch + kv_head * a.v.head) * size;
-  next_k.start(a.dim, (int)k_pos, threadIdx.x);
-  next_v.start(a.dim, (int)v_pos, threadIdx.x);
+  next_k.start(a.dim, (int)k_pos, stager);
+  next_v.start(a.dim, (int)v_pos, stager);
   auto load = [&](int turn) {
     next_k.load(k_at, k_pos, a.dim, turn * kTile, length);
     next_v.load(v_at, v_pos, a.dim, turn * kTile, length);
   };
-  auto store = [&](int turn) {
-    next_k.store(lds[turn & 1][0], threadIdx.x);
-    next_v.store(lds[turn & 1][1], threadIdx.x);
+  auto store = [&](int place) {
+    next_k.store(lds[place][0], stager);
+    next_v.store(lds[place][1], stager);
   };
 
   float16v dq[D / 32];
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) dq[i] = zeros();
-  if (turns > 0) {
-    load(0);
-    store(0);
-  }
-  wait_all();
-  __syncthreads();
-  for (int turn = 0; turn < turns; ++turn) {
-    if (turn + 1 < turns) load(turn + 1);
+  // What the next tile's loads pass through is free only after the scores where a
+  // wave loads a whole tile of 128 binary32 elements a row.
+  constexpr bool kLate = SPLIT && !BF16 && D == 128;
+  auto add = [&](int turn, int place, auto more) {
+    if (!kLate) more();
     const int first = turn * kTile;
-    const uint8_t *keys = lds[turn & 1][0], *values = lds[turn & 1][1];
+    const uint8_t *keys = lds[place][0], *values = lds[place][1];
     if (first < most) {
       schedule_here();
+      __builtin_amdgcn_s_setprio(1);
       float16v s = zeros(), dp = zeros();
 #pragma unroll
       for (int step = 0; step < D / 16; ++step) {
@@ -103,6 +130,8 @@ __global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attention_dq_kernel(co
       }
       if (BF16) interleave<4, D / 8, D / 8>();
       schedule_here();
+      __builtin_amdgcn_s_setprio(0);
+      if (kLate) more();
       constexpr int ahead = D < 128 ? D / 16 : D / 32;  // (fragments that there are registers for)
       Frag<BF16> across[D / 16];
 #pragma unroll
@@ -125,9 +154,37 @@ __global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attention_dq_kernel(co
         multiply(dq[part], across[2 * part], d0);
         multiply(dq[part], across[2 * part + 1], d1);
       }
+    } else if (kLate) {
+      more();
     }
-    if (turn + 1 < turns) store(turn + 1);
+  };
+  if constexpr (SPLIT) {
+    if (wave < turns) load(wave);
+    wait_all();
+    for (int turn = wave; turn < turns; turn += kWaves) {
+      store(wave);
+      wave_order();
+      add(turn, wave, [&]() {
+        if (turn + kWaves < turns) load(turn + kWaves);
+      });
+      wave_order();
+    }
+    join_waves(dq, (float*)&lds[0][0][0], wave, lane);
+    if (wave > 0) return;
+  } else {
+    if (turns > 0) {
+      load(0);
+      store(0);
+    }
+    wait_all();
     __syncthreads();
+    for (int turn = 0; turn < turns; ++turn) {
+      add(turn, turn & 1, [&]() {
+        if (turn + 1 < turns) load(turn + 1);
+      });
+      if (turn + 1 < turns) store((turn + 1) & 1);
+      __syncthreads();
+    }
   }
   if (!live) return;
   const int64_t dq_at = batch * a.dq.batch + at.head * a.dq.head + at.query * a.dq.pos;
@@ -135,17 +192,20 @@ __global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attention_dq_kernel(co
   for (int i = 0; i < D / 32; ++i) store_column<BF16>(a.dq.at, dq_at + 32 * i, a.dim - 32 * i, dq[i], a.scale, lane);
 }
 
-template <bool BF16, int D>
-__global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attention_dkv_kernel(const AttentionArgs a) {
+template <bool BF16, int D, bool SPLIT>
+__global__ __launch_bounds__(kThreads, BF16 && !SPLIT ? 2 : 1) void attention_dkv_kernel(const AttentionArgs a) {
   typedef Tile<BF16, D, kTile> T;
+  constexpr int own_keys = SPLIT ? 32 : kRows;
+  constexpr int kPlaces = SPLIT ? kWaves : 2;
   // Two sums of 128 x 32, k and v are 192 registers with bfloat16's 128 elements:
   // two waves to a SIMD only with v in LDS.  Two workgroups fill a CU's 160 KiB to
   // the byte, so the rows' log sums and deltas lie in v's padding.
-  constexpr bool kKeep = !(BF16 && D == 128);
+  constexpr bool kKeep = SPLIT || !(BF16 && D == 128);
   typedef Tile<BF16, D, kRows> Own;
-  constexpr int kStats = 2 * 2 * kTile * 4, kTiles = 2 * 2 * T::kBytes;
+  constexpr int kStats = kPlaces * 2 * kTile * 4, kTiles = kPlaces * 2 * T::kBytes;
   static_assert(kKeep || (Own::kPad == 4 && kStats <= 8 * 64), "padding");
   __shared__ __align__(16) uint8_t lds[kTiles + (kKeep ? kStats : Own::kBytes)];
+  static_assert(!SPLIT || sizeof(lds) >= (kWaves - 1) * D / 32 * 16 * 64 * sizeof(float), "the waves' sums");
   auto tile_at = [&](int place, int which) { return lds + (place * 2 + which) * T::kBytes; };  // queries, dout
   uint8_t* const values = lds + kTiles;
   auto stats_at = [&](int place, int which, int i) {  // log sums, deltas; four from a multiple of four on
@@ -159,7 +219,8 @@ __global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attention_dkv_kernel(c
   const int kv_head = head_of % a.kv_heads, batch = head_of / a.kv_heads;
   const int length = keys_of(a, batch);
 
-  const int key0 = tile * kRows, wave_key = key0 + wave * 32, key = wave_key + (lane & 31);
+  const int stager = SPLIT ? lane : (int)threadIdx.x;
+  const int key0 = tile * own_keys, wave_key = key0 + (SPLIT ? 0 : wave * 32), key = wave_key + (lane & 31);
   const bool live = key < length;
   Frag<BF16> k[D / 16], v[kKeep ? D / 16 : 1];
   const int64_t k_at = batch * a.k.batch + kv_head * a.k.head + key * a.k.pos;
@@ -188,39 +249,31 @@ __global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attention_dkv_kernel(c
   const int of_head = (a.queries + kTile - 1) / kTile - from;
   const int turns = key0 < length && of_head > 0 ? of_head * a.group : 0;
 
-  Staged<BF16, D, kTile, kThreads> next_q, next_do;
+  Staged<BF16, D, kTile, SPLIT ? 64 : kThreads> next_q, next_do;
   float next_lse = 0.0f, next_delta = 0.0f;
   constexpr int size = T::kSize;
   const int64_t q_pos = a.q.pos * size, do_pos = a.dout.pos * size;
-  next_q.start(a.dim, (int)q_pos, threadIdx.x);
-  next_do.start(a.dim, (int)do_pos, threadIdx.x);
-  const uint8_t *q_at = (const uint8_t*)a.q.at + (batch * a.q.batch + (int64_t)kv_head * a.group * a.q.head) * size,
-                *do_at = (const uint8_t*)a.dout.at +
-                         (batch * a.dout.batch + (int64_t)kv_head * a.group * a.dout.head) * size;
-  int64_t stat = ((int64_t)batch * a.heads + kv_head * a.group) * a.queries;
-  int next_tile = from;  // of the head, of what is loaded next
-  auto load = [&]() {
-    const int first = next_tile * kTile;
-    next_q.load(q_at, q_pos, a.dim, first, a.queries);
-    next_do.load(do_at, do_pos, a.dim, first, a.queries);
-    if (threadIdx.x < kTile) {
-      const int query = first + threadIdx.x;
+  next_q.start(a.dim, (int)q_pos, stager);
+  next_do.start(a.dim, (int)do_pos, stager);
+  auto load = [&](int turn) {
+    const int of = uniform(turn / of_head), head = kv_head * a.group + of;
+    const int first = (from + turn - of * of_head) * kTile;
+    next_q.load((const uint8_t*)a.q.at + (batch * a.q.batch + head * a.q.head) * size, q_pos, a.dim, first, a.queries);
+    next_do.load((const uint8_t*)a.dout.at + (batch * a.dout.batch + head * a.dout.head) * size, do_pos, a.dim, first,
+                 a.queries);
+    if (stager < kTile) {
+      const int64_t stat = ((int64_t)batch * a.heads + head) * a.queries;
+      const int query = first + stager;
       next_lse = query < a.queries ? a.lse[stat + query] : infinity();
       next_delta = query < a.queries ? a.delta[stat + query] : 0.0f;
     }
-    if (++next_tile == from + of_head) {
-      next_tile = from;
-      q_at += a.q.head * size;
-      do_at += a.dout.head * size;
-      stat += a.queries;
-    }
   };
   auto store = [&](int place) {
-    next_q.store(tile_at(place, 0), threadIdx.x);
-    next_do.store(tile_at(place, 1), threadIdx.x);
-    if (threadIdx.x < kTile) {
-      *stats_at(place, 0, threadIdx.x) = next_lse;
-      *stats_at(place, 1, threadIdx.x) = next_delta;
+    next_q.store(tile_at(place, 0), stager);
+    next_do.store(tile_at(place, 1), stager);
+    if (stager < kTile) {
+      *stats_at(place, 0, stager) = next_lse;
+      *stats_at(place, 1, stager) = next_delta;
     }
   };
 
@@ -229,17 +282,14 @@ __global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attention_dkv_kernel(c
   float16v dk[D / 32], dv[D / 32];
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) dk[i] = dv[i] = zeros();
-  if (turns > 0) {
-    load();
-    store(0);
-  }
-  wait_all();
-  __syncthreads();
-  int in_head = from, place = 0;
-  for (int turn = 0; turn < turns; ++turn) {
-    if (kKeep && turn + 1 < turns) load();
+  // (`more` loads the next tile: after the scores where what the loads pass through
+  // is free only then)
+  constexpr bool kLate = !kKeep || (SPLIT && !BF16 && D == 128);
+  auto add = [&](int turn, int place, auto more) {
+    if (!kLate) more();
     const uint8_t *queries = tile_at(place, 0), *douts = tile_at(place, 1);
     schedule_here();
+    __builtin_amdgcn_s_setprio(1);
     float16v s = zeros(), dp = zeros();
 #pragma unroll
     for (int step = 0; step < D / 16; ++step) {
@@ -249,7 +299,8 @@ __global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attention_dkv_kernel(c
     }
     if (BF16) interleave<4, D / 16 * (kKeep ? 2 : 3), D / 8, kKeep ? 1 : 2>();
     schedule_here();
-    if (!kKeep && turn + 1 < turns) load();  // (what the loads pass through is free only now)
+    __builtin_amdgcn_s_setprio(0);
+    if (kLate) more();
     Frag<BF16> across[D / 16];
     if (BF16) {
 #pragma unroll
@@ -262,6 +313,7 @@ __global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attention_dkv_kernel(c
       for (int i = 0; i < 4; ++i) s[4 * g + i] = exp2_fast(__builtin_fmaf(s[4 * g + i], a.c, -lse[i]));
     }
     // the tile's first query does not see the wave's last key
+    const int in_head = from + turn - uniform(turn / of_head) * of_head;
     const int hidden = wave_key + 31 - (in_head * kTile + a.keys - a.queries);
     if (a.causal && hidden > 0) {
       const int at = (lane & 31) - 31 + hidden - 4 * h;  // rows below it do not see the lane's key
@@ -293,10 +345,35 @@ __global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attention_dkv_kernel(c
         multiply(dk[i / 2], T::across(queries, places, 16 * (i % 2), i / 2), i % 2 ? d1 : d0);
       }
     }
-    if (turn + 1 < turns) store(place ^ 1);
+  };
+  if constexpr (SPLIT) {
+    if (wave < turns) load(wave);
+    wait_all();
+    for (int turn = wave; turn < turns; turn += kWaves) {
+      store(wave);
+      wave_order();
+      add(turn, wave, [&]() {
+        if (turn + kWaves < turns) load(turn + kWaves);
+      });
+      wave_order();
+    }
+    join_waves(dk, (float*)lds, wave, lane);
+    join_waves(dv, (float*)lds, wave, lane);
+    if (wave > 0) return;
+  } else {
+    if (turns > 0) {
+      load(0);
+      store(0);
+    }
+    wait_all();
     __syncthreads();
-    if (++in_head == from + of_head) in_head = from;
-    place ^= 1;
+    for (int turn = 0; turn < turns; ++turn) {
+      add(turn, turn & 1, [&]() {
+        if (turn + 1 < turns) load(turn + 1);
+      });
+      if (turn + 1 < turns) store((turn + 1) & 1);
+      __syncthreads();
+    }
   }
   if (key >= a.keys) return;
   // (a key behind the length has scores of its zeros: no gradient)
@@ -312,9 +389,20 @@ __global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attention_dkv_kernel(c
 
 template <bool BF16, int D>
 void launch_both(const AttentionArgs& a, hipStream_t s) {
-  const int heads = a.kv_heads * a.batch, rows = (a.rows + kRows - 1) / kRows, keys = (a.keys + kRows - 1) / kRows;
-  if (rows) attention_dq_kernel<BF16, D><<<dim3((unsigned)(rows * heads)), dim3(kThreads), 0, s>>>(a);
-  if (keys) attention_dkv_kernel<BF16, D><<<dim3((unsigned)(keys * heads)), dim3(kThreads), 0, s>>>(a);
+  const int heads = a.kv_heads * a.batch;
+  const auto groups = [&](int n, int of) { return (unsigned)((int64_t)((n + of - 1) / of) * heads); };
+  if (a.rows) {
+    if (few_groups(a, a.rows))
+      attention_dq_kernel<BF16, D, true><<<dim3(groups(a.rows, 32)), dim3(kThreads), 0, s>>>(a);
+    else
+      attention_dq_kernel<BF16, D, false><<<dim3(groups(a.rows, kRows)), dim3(kThreads), 0, s>>>(a);
+  }
+  if (a.keys) {
+    if (few_groups(a, a.keys))
+      attention_dkv_kernel<BF16, D, true><<<dim3(groups(a.keys, 32)), dim3(kThreads), 0, s>>>(a);
+    else
+      attention_dkv_kernel<BF16, D, false><<<dim3(groups(a.keys, kRows)), dim3(kThreads), 0, s>>>(a);
+  }
 }
 
 template <bool BF16>

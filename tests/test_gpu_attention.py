@@ -53,6 +53,9 @@ SHAPES = [
     # keys in parts, of few rows and of more
     (2, 1, 2500, 4, 1, 128), (1, 1, 9001, 3, 3, 40), (1, 5, 1100, 6, 1, 96), (2, 130, 1500, 2, 1, 64),
     (1, 40, 3001, 1, 1, 128), (2, 33, 777, 3, 3, 32),
+    # rows and keys enough for workgroups of 128
+    (8, 130, 130, 32, 32, 128), (16, 70, 150, 32, 16, 72), (16, 150, 100, 32, 32, 64), (32, 129, 190, 16, 16, 24),
+    (9, 257, 257, 32, 32, 40), (10, 40, 260, 64, 32, 120),
 ]
 
 
