@@ -145,7 +145,7 @@ __device__ inline Part part_of(const AttentionArgs& a, int part, int tiles) {
 }
 
 template <bool BF16, int D>
-__global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attention_kernel(const AttentionArgs a) {
+__global__ __launch_bounds__(kThreads, BF16 || D <= 64 ? 2 : 1) void attention_kernel(const AttentionArgs a) {
   constexpr int keys = kKeys<BF16>;
   typedef Tile<BF16, D, keys> T;
   __shared__ __align__(16) uint8_t lds[2][2][T::kBytes];  // [turn][keys, values]
@@ -221,7 +221,7 @@ __global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attention_kernel(const
 constexpr int kFewRows = 32, kFewKeys = 32;
 
 template <bool BF16, int D>
-__global__ __launch_bounds__(kThreads, BF16 ? 2 : 1) void attention_few_kernel(const AttentionArgs a) {
+__global__ __launch_bounds__(kThreads, BF16 || D <= 64 ? 2 : 1) void attention_few_kernel(const AttentionArgs a) {
   typedef Tile<BF16, D, kFewKeys> T;
   constexpr int kWaves = kThreads / 64;
   constexpr int kSums = D / 32 * 16 + 2;  // floats that a lane hands over

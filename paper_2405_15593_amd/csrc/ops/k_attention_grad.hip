@@ -45,7 +45,7 @@ __device__ inline void join_waves(float16v (&x)[N], float* sums, int wave, int l
 }
 
 template <bool BF16, int D, bool SPLIT>
-__global__ __launch_bounds__(kThreads, BF16 && !SPLIT ? 2 : 1) void attention_dq_kernel(const AttentionArgs a) {
+__global__ __launch_bounds__(kThreads, (BF16 && !SPLIT) || D <= 64 ? 2 : 1) void attention_dq_kernel(const AttentionArgs a) {
   typedef Tile<BF16, D, kTile> T;
   constexpr int own_rows = SPLIT ? 32 : kRows;
   __shared__ __align__(16) uint8_t lds[SPLIT ? kWaves : 2][2][T::kBytes];  // [wave or turn][keys, values]
@@ -112,9 +112,9 @@ __global__ __launch_bounds__(kThreads, BF16 && !SPLIT ? 2 : 1) void attention_dq
   float16v dq[D / 32];
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) dq[i] = zeros();
-  // What the next tile's loads pass through is free only after the scores where a
-  // wave loads a whole tile of 128 binary32 elements a row.
-  constexpr bool kLate = SPLIT && !BF16 && D == 128;
+  // (`more` loads the next tile: after the scores where what the loads pass through
+  // is free only then)
+  constexpr bool kLate = SPLIT && !BF16;
   auto add = [&](int turn, int place, auto more) {
     if (!kLate) more();
     const int first = turn * kTile;
@@ -193,24 +193,27 @@ __global__ __launch_bounds__(kThreads, BF16 && !SPLIT ? 2 : 1) void attention_dq
 }
 
 template <bool BF16, int D, bool SPLIT>
-__global__ __launch_bounds__(kThreads, BF16 && !SPLIT ? 2 : 1) void attention_dkv_kernel(const AttentionArgs a) {
+__global__ __launch_bounds__(kThreads, (BF16 && !SPLIT) || D <= 64 ? 2 : 1) void attention_dkv_kernel(const AttentionArgs a) {
   typedef Tile<BF16, D, kTile> T;
   constexpr int own_keys = SPLIT ? 32 : kRows;
   constexpr int kPlaces = SPLIT ? kWaves : 2;
   // Two sums of 128 x 32, k and v are 192 registers with bfloat16's 128 elements:
-  // two waves to a SIMD only with v in LDS.  Two workgroups fill a CU's 160 KiB to
-  // the byte, so the rows' log sums and deltas lie in v's padding.
+  // two waves to a SIMD only with v in LDS.  Two workgroups then fill a CU's 160
+  // KiB to the byte, so the rows' log sums and deltas lie in the tiles' padding.
   constexpr bool kKeep = SPLIT || !(BF16 && D == 128);
   typedef Tile<BF16, D, kRows> Own;
-  constexpr int kStats = kPlaces * 2 * kTile * 4, kTiles = kPlaces * 2 * T::kBytes;
-  static_assert(kKeep || (Own::kPad == 4 && kStats <= 8 * 64), "padding");
-  __shared__ __align__(16) uint8_t lds[kTiles + (kKeep ? kStats : Own::kBytes)];
+  constexpr bool kPadded = T::kPad == 4;
+  constexpr int kTiles = kPlaces * 2 * T::kBytes;
+  __shared__ __align__(16) uint8_t lds[kTiles + (kPadded ? 0 : kPlaces * 2 * kTile * 4) + (kKeep ? 0 : Own::kBytes)];
+  uint8_t* const values = lds + kTiles;  // (128 elements a row are padded)
+  static_assert(kKeep || kPadded, "values");
   static_assert(!SPLIT || sizeof(lds) >= (kWaves - 1) * D / 32 * 16 * 64 * sizeof(float), "the waves' sums");
   auto tile_at = [&](int place, int which) { return lds + (place * 2 + which) * T::kBytes; };  // queries, dout
-  uint8_t* const values = lds + kTiles;
-  auto stats_at = [&](int place, int which, int i) {  // log sums, deltas; four from a multiple of four on
-    const int n = (place * 2 + which) * kTile + i;
-    return (float*)(kKeep ? values + n * 4 : values + (n >> 4) * Own::kStride + Own::kChunks * 16 + (n & 15) * 4);
+  // log sums, deltas; four from a multiple of four on
+  auto stats_at = [&](int place, int which, int i) {
+    const int n = which * kTile + i;
+    return (float*)(kPadded ? tile_at(place, 0) + (n >> 4) * T::kStride + T::kChunks * 16 + (n & 15) * 4
+                            : lds + kTiles + (place * 2 * kTile + n) * 4);
   };
   const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), h = lane >> 5;
   const Work work = work_of(blockIdx.x, a.kv_heads * a.batch);
@@ -282,9 +285,7 @@ __global__ __launch_bounds__(kThreads, BF16 && !SPLIT ? 2 : 1) void attention_dk
   float16v dk[D / 32], dv[D / 32];
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) dk[i] = dv[i] = zeros();
-  // (`more` loads the next tile: after the scores where what the loads pass through
-  // is free only then)
-  constexpr bool kLate = !kKeep || (SPLIT && !BF16 && D == 128);
+  constexpr bool kLate = !kKeep || (SPLIT && !BF16);
   auto add = [&](int turn, int place, auto more) {
     if (!kLate) more();
     const uint8_t *queries = tile_at(place, 0), *douts = tile_at(place, 1);
