@@ -1,7 +1,10 @@
 """MicroAdam inside a training loop: a small randomly initialised decoder-only
 transformer on synthetic tokens, trained with ``MicroAdamW``, with ``Muon`` for
 the blocks' matrices beside ``MicroAdamW`` for the other parameters (the loss
-from ``token_logprobs``), and, for comparison, with torch's dense AdamW.
+from ``token_logprobs``), and, for comparison, with torch's dense AdamW.  With
+``own`` the package's kernels also take the model's layer norms
+(``layer_norm``), its attention (``attention``) and the loss, and with
+``max_norm`` the gradients are clipped before the step (``clip_grad_norm``).
 
 The tokens follow a fixed random first-order Markov chain (seeded), so the
 loss has a floor well below log(V) that a working optimizer approaches.  The
@@ -9,7 +12,7 @@ run reports each optimizer's loss curve, optimizer state bytes and the time of
 its optimizer step inside the loop.  Everything is float32 (the attention and
 its backward stay in float32).
 
-    python -m paper_2405_15593_amd.insitu [--steps 200] [--layers 4] [--dim 256]
+    python -m paper_2405_15593_amd.insitu [--steps 200] [--layers 4] [--dim 256] [--own] [--max-norm 1.0]
 """
 from __future__ import annotations
 
@@ -22,11 +25,19 @@ import torch
 import torch.nn as nn
 import torch.nn.functional as F
 
+from .attention import attention
+from .clip import clip_grad_norm
+from .norm import layer_norm
+
+
+def own_norm(norm: nn.LayerNorm, x):
+    return layer_norm(x, norm.weight, norm.bias, eps=norm.eps)
+
 
 class Block(nn.Module):
-    def __init__(self, dim: int, heads: int):
+    def __init__(self, dim: int, heads: int, own: bool = False):
         super().__init__()
-        self.heads = heads
+        self.heads, self.own = heads, own
         self.norm1 = nn.LayerNorm(dim)
         self.qkv = nn.Linear(dim, 3 * dim)
         self.proj = nn.Linear(dim, dim)
@@ -36,6 +47,11 @@ class Block(nn.Module):
 
     def forward(self, x):
         b, s, d = x.shape
+        if self.own:
+            # queries, keys and values stay where the projection leaves them
+            q, k, v = self.qkv(own_norm(self.norm1, x)).view(b, s, 3, self.heads, d // self.heads).unbind(2)
+            x = x + self.proj(attention(q, k, v, causal=True).view(b, s, d))
+            return x + self.fc2(F.gelu(self.fc1(own_norm(self.norm2, x))))
         q, k, v = self.qkv(self.norm1(x)).split(d, dim=-1)
         shape = (b, s, self.heads, d // self.heads)
         q, k, v = (y.reshape(shape).transpose(1, 2).contiguous() for y in (q, k, v))
@@ -45,11 +61,12 @@ class Block(nn.Module):
 
 
 class TinyLM(nn.Module):
-    def __init__(self, vocab: int, dim: int, layers: int, heads: int, seq: int):
+    def __init__(self, vocab: int, dim: int, layers: int, heads: int, seq: int, own: bool = False):
         super().__init__()
+        self.own = own
         self.tok = nn.Embedding(vocab, dim)
         self.pos = nn.Embedding(seq, dim)
-        self.blocks = nn.ModuleList(Block(dim, heads) for _ in range(layers))
+        self.blocks = nn.ModuleList(Block(dim, heads, own) for _ in range(layers))
         self.norm = nn.LayerNorm(dim)
         self.head = nn.Linear(dim, vocab, bias=False)
 
@@ -57,7 +74,7 @@ class TinyLM(nn.Module):
         x = self.tok(ids) + self.pos(torch.arange(ids.shape[1], device=ids.device))
         for blk in self.blocks:
             x = blk(x)
-        return self.head(self.norm(x))
+        return self.head(own_norm(self.norm, x) if self.own else self.norm(x))
 
 
 class MarkovTokens:
@@ -85,12 +102,12 @@ class MarkovTokens:
 
 
 def train(opt_name: str, steps: int, vocab=1024, dim=256, layers=4, heads=4, seq=128, batch=32,
-          lr=1e-3, seed=0, device="cuda", log_every=10):
+          lr=1e-3, seed=0, device="cuda", log_every=10, own=False, max_norm=None):
     from .logprobs import token_logprobs
     from .muon import Muon
     from .optim import MicroAdamW
     torch.manual_seed(seed)
-    model = TinyLM(vocab, dim, layers, heads, seq).to(device)
+    model = TinyLM(vocab, dim, layers, heads, seq, own).to(device)
     params = [p for p in model.parameters()]
     n_params = sum(p.numel() for p in params)
     if opt_name == "microadam":
@@ -107,13 +124,15 @@ def train(opt_name: str, steps: int, vocab=1024, dim=256, layers=4, heads=4, seq
     t0 = time.perf_counter()
     for step in range(steps):
         x, y = data.next()
-        if opt_name == "muon":
+        if opt_name == "muon" or own:
             loss = -token_logprobs(model(x), y).logp.mean()
         else:
             loss = F.cross_entropy(model(x).reshape(-1, vocab), y.reshape(-1))
         for opt in opts:
             opt.zero_grad(set_to_none=True)
         loss.backward()
+        if max_norm is not None:
+            norm = clip_grad_norm(params, max_norm)
         ev[0].record()
         for opt in opts:
             opt.step()
@@ -123,6 +142,7 @@ def train(opt_name: str, steps: int, vocab=1024, dim=256, layers=4, heads=4, seq
             losses.append((step, float(loss.detach())))
             opt_ms.append(ev[0].elapsed_time(ev[1]))
     torch.cuda.synchronize()
+    norms = {} if max_norm is None or not steps else {"grad_norm": float(norm)}
     wall = time.perf_counter() - t0
     if opt_name != "adamw":
         state = sum(opt.state_bytes() for opt in opts)
@@ -132,7 +152,7 @@ def train(opt_name: str, steps: int, vocab=1024, dim=256, layers=4, heads=4, seq
     return {"optimizer": opt_name, "params": n_params, "steps": steps, "losses": losses,
             "final_loss": losses[-1][1], "opt_step_ms": sum(opt_ms[1:]) / max(1, len(opt_ms) - 1),
             "wall_s": wall, "state_bytes": state, "state_bytes_per_param": state / n_params,
-            "loss_floor": data.entropy, "log_vocab": math.log(vocab)}
+            "loss_floor": data.entropy, "log_vocab": math.log(vocab), **norms}
 
 
 def main():
@@ -141,8 +161,11 @@ def main():
     ap.add_argument("--layers", type=int, default=4)
     ap.add_argument("--dim", type=int, default=256)
     ap.add_argument("--lr", type=float, default=1e-3)
+    ap.add_argument("--own", action="store_true", help="layer norm, attention and loss by the package's kernels")
+    ap.add_argument("--max-norm", type=float, default=None, help="clip the gradients' norm")
     args = ap.parse_args()
-    out = {name: train(name, args.steps, layers=args.layers, dim=args.dim, lr=args.lr)
+    out = {name: train(name, args.steps, layers=args.layers, dim=args.dim, lr=args.lr, own=args.own,
+                       max_norm=args.max_norm)
            for name in ("microadam", "muon", "adamw")}
     print(json.dumps(out))
 
