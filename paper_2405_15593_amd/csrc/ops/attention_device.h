@@ -46,6 +46,12 @@ inline bool few_groups(const AttentionArgs& a, int positions) {
   return (int64_t)((positions + 127) / 128) * a.kv_heads * a.batch < (a.bf16 ? 256 : 512);
 }
 
+// Whether the rows go to the kernel without matrix products.
+constexpr int kTokenRows = 8;
+inline bool token_rows(const AttentionArgs& a) { return !a.bf16 && a.rows <= kTokenRows; }
+
+void launch_attention_token(const AttentionArgs& a, hipStream_t s);
+
 // How many parts a forward call's keys are split into; 0: not at all.
 int32_t attention_parts(const AttentionArgs& a);
 

@@ -9,6 +9,8 @@
 // and out^T += v^T p^T, so that a row's maximum, sum and factor are its lane's
 // own.  Four waves share the tiles of keys and values in LDS, which the next
 // tile's loads pass in registers.
+#include <algorithm>
+
 #include "attention_tile.h"
 
 namespace microadam {
@@ -321,16 +323,17 @@ __global__ __launch_bounds__(kThreads, BF16 || D <= 64 ? 2 : 1) void attention_f
   finish<BF16, D>(a, head_of, batch, row, at, part, top, l, out, lane);
 }
 
-// The parts of a row's keys joined, a wave a row: lane i has the sums of parts
-// i, i + 64, .., then two elements of the row.
-template <bool BF16>
+// The parts of a row's keys joined by WAVES waves: lane i has the sums of parts i,
+// i + 64, .., then two elements of the row; the waves share the parts.
+template <bool BF16, int WAVES>
 __global__ __launch_bounds__(kThreads) void attention_join_kernel(const AttentionArgs a) {
-  constexpr int kEach = kMostParts / 64;
-  const int lane = threadIdx.x & 63;
-  const int64_t n = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
-  if (n >= (int64_t)a.batch * a.kv_heads * a.rows) return;
-  const int64_t head_of = n / a.rows;
-  const int row = (int)(n - head_of * a.rows);
+  constexpr int kEach = kMostParts / 64, kRowsHere = kThreads / 64 / WAVES;
+  __shared__ float2v others[kThreads / 64][64];
+  const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), which = wave % WAVES;
+  const int64_t rows = (int64_t)a.batch * a.kv_heads * a.rows, n = (int64_t)blockIdx.x * kRowsHere + wave / WAVES;
+  const bool live = n < rows;
+  const int64_t head_of = live ? n / a.rows : 0;
+  const int row = live ? (int)(n - head_of * a.rows) : 0;
   const int batch = (int)(head_of / a.kv_heads);
   const RowAt at = row_at(a, (int)(head_of % a.kv_heads), row);
   const int64_t first = head_of * a.parts * a.rows + row;
@@ -338,7 +341,7 @@ __global__ __launch_bounds__(kThreads) void attention_join_kernel(const Attentio
 #pragma unroll
   for (int i = 0; i < kEach; ++i) {
     const int part = 64 * i + lane;
-    const bool there = part < a.parts;
+    const bool there = live && part < a.parts;
     const float2v s = there ? *(const float2v*)(a.part_stats + 2 * (first + (int64_t)part * a.rows)) : float2v{0.0f, 0.0f};
     m[i] = there ? s[0] : -infinity();
     l[i] = s[1];
@@ -361,12 +364,12 @@ __global__ __launch_bounds__(kThreads) void attention_join_kernel(const Attentio
   for (int i = 0; i < kEach; ++i) {
     const int parts = a.parts - 64 * i < 64 ? a.parts - 64 * i : 64;
     const float* from_part = a.part_out + (first + (int64_t)64 * i * a.rows) * a.dim + d;
-    for (int p = 0; p < parts; p += 8) {
+    for (int p = 8 * which; p < parts; p += 8 * WAVES) {
       float2v x[8];
 #pragma unroll
       for (int u = 0; u < 8; ++u)
-        x[u] = p + u < parts && d < a.dim ? *(const float2v*)(from_part + (int64_t)(p + u) * a.rows * a.dim)
-                                          : float2v{0.0f, 0.0f};
+        x[u] = live && p + u < parts && d < a.dim ? *(const float2v*)(from_part + (int64_t)(p + u) * a.rows * a.dim)
+                                                  : float2v{0.0f, 0.0f};
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
         const float factor = __shfl(m[i], (p + u) & 63);
@@ -375,6 +378,14 @@ __global__ __launch_bounds__(kThreads) void attention_join_kernel(const Attentio
       }
     }
   }
+  if (WAVES > 1) {
+    others[wave][lane] = o;
+    __syncthreads();
+    if (which != 0) return;
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) o += others[wave + w][lane];
+  }
+  if (!live) return;
   const float over = sum == 0.0f ? 0.0f : 1.0f / sum;
   const int64_t stat = ((int64_t)batch * a.heads + at.head) * a.queries + at.query;
   if (d < a.dim) {
@@ -398,13 +409,19 @@ void launch_rows(const AttentionArgs& a, hipStream_t s) {
   const int heads = a.kv_heads * a.batch, parts = a.parts ? a.parts : 1;
   const bool few = few_rows(a);
   const int tiles = few ? (a.rows + kFewRows - 1) / kFewRows : (a.rows + kRows - 1) / kRows;
-  if (few)
+  if (!BF16 && token_rows(a))
+    launch_attention_token(a, s);
+  else if (few)
     attention_few_kernel<BF16, D><<<dim3((unsigned)(tiles * heads * parts)), dim3(kThreads), 0, s>>>(a);
   else
     attention_kernel<BF16, D><<<dim3((unsigned)(tiles * heads)), dim3(kThreads), 0, s>>>(a);
   if (a.parts) {
-    const int64_t waves = kThreads / 64, blocks = ((int64_t)heads * a.rows + waves - 1) / waves;
-    attention_join_kernel<BF16><<<dim3((unsigned)blocks), dim3(kThreads), 0, s>>>(a);
+    // (more than eight parts: four waves a row)
+    const int64_t rows = (int64_t)heads * a.rows, waves = kThreads / 64;
+    if (a.parts > 8)
+      attention_join_kernel<BF16, kThreads / 64><<<dim3((unsigned)rows), dim3(kThreads), 0, s>>>(a);
+    else
+      attention_join_kernel<BF16, 1><<<dim3((unsigned)((rows + waves - 1) / waves)), dim3(kThreads), 0, s>>>(a);
   }
 }
 
@@ -423,17 +440,14 @@ void launch_dim(const AttentionArgs& a, hipStream_t s) {
 }  // namespace
 
 // Keys are split where the rows alone are too few workgroups for 256 CUs: into
-// as many parts as give two to a CU, of at least so many tiles that a part's
-// work is worth the join (4 to 5 us with its launch).
+// as many parts as give two to a CU, of at least so many keys that a part's work
+// is worth the join (4 to 5 us with its launch).
 int32_t attention_parts(const AttentionArgs& a) {
-  if (!few_rows(a)) return 0;
-  const int64_t groups = (int64_t)((a.rows + kFewRows - 1) / kFewRows) * a.kv_heads * a.batch;
+  if (!token_rows(a) && !few_rows(a)) return 0;
+  const int64_t tiles = token_rows(a) ? 1 : (a.rows + kFewRows - 1) / kFewRows, groups = tiles * a.kv_heads * a.batch;
   if (groups < 1 || groups >= 256) return 0;
-  const int64_t most = (a.keys + kFewKeys - 1) / kFewKeys / 8;
-  int64_t parts = (512 + groups - 1) / groups;
-  parts = parts < most ? parts : most;
-  parts = parts < kMostParts ? parts : kMostParts;
-  return parts > 1 ? (int32_t)parts : 0;
+  const int64_t parts = std::min((512 + groups - 1) / groups, (int64_t)a.keys / (token_rows(a) ? 128 : 256));
+  return parts > 1 ? (int32_t)std::min<int64_t>(parts, kMostParts) : 0;
 }
 
 hipError_t launch_attention(const AttentionArgs& a, hipStream_t s) {

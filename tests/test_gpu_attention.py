@@ -53,6 +53,8 @@ SHAPES = [
     # keys in parts, of few rows and of more
     (2, 1, 2500, 4, 1, 128), (1, 1, 9001, 3, 3, 40), (1, 5, 1100, 6, 1, 96), (2, 130, 1500, 2, 1, 64),
     (1, 40, 3001, 1, 1, 128), (2, 33, 777, 3, 3, 32),
+    # a few rows as a stream over the keys (binary32)
+    (2, 2, 700, 8, 2, 64), (1, 7, 3, 2, 2, 16), (1, 4, 260, 2, 1, 128), (3, 1, 1300, 2, 1, 32), (2, 8, 2000, 1, 1, 104),
     # rows and keys enough for workgroups of 128
     (8, 130, 130, 32, 32, 128), (16, 70, 150, 32, 16, 72), (16, 150, 100, 32, 32, 64), (32, 129, 190, 16, 16, 24),
     (9, 257, 257, 32, 32, 40), (10, 40, 260, 64, 32, 120),
