@@ -142,8 +142,11 @@ __global__ __launch_bounds__(kThreads, (BF16 && !SPLIT) || D <= 64 ? 2 : 1) void
         s[r] = p * (dp[r] - delta);
       }
       if (first + kTile > least) {
+        // (a key that is a query's only one: p is 1 whatever the score, where dp -
+        // delta would leave the rounding of two sums)
+        const int end = limit > 1 ? limit : 0;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = first + 8 * (r / 4) + 4 * (lane >> 5) + r % 4 < limit ? s[r] : 0.0f;
+        for (int r = 0; r < 16; ++r) s[r] = first + 8 * (r / 4) + 4 * (lane >> 5) + r % 4 < end ? s[r] : 0.0f;
       }
       schedule_here();
       const Frag<BF16> d0 = as_frag<BF16, 0>(s), d1 = as_frag<BF16, 1>(s);
@@ -326,6 +329,12 @@ __global__ __launch_bounds__(kThreads, (BF16 && !SPLIT) || D <= 64 ? 2 : 1) void
       const float4v delta = *(const float4v*)stats_at(place, 1, 8 * g + 4 * h);
 #pragma unroll
       for (int i = 0; i < 4; ++i) dp[4 * g + i] = s[4 * g + i] * (dp[4 * g + i] - delta[i]);
+    }
+    // queries that see one key (as in dq): with one in all, or the first that sees any
+    const int alone = a.queries - a.keys - in_head * kTile;
+    if (length == 1 || (a.causal && wave_key == 0 && alone >= 0 && alone < kTile)) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) dp[r] = length == 1 || 8 * (r / 4) + 4 * h + r % 4 == alone ? 0.0f : dp[r];
     }
     const Frag<BF16> p0 = as_frag<BF16, 0>(s), p1 = as_frag<BF16, 1>(s);
     const Frag<BF16> d0 = as_frag<BF16, 0>(dp), d1 = as_frag<BF16, 1>(dp);

@@ -142,6 +142,33 @@ def test_nothing_past_the_length_is_read(sq, types):
             assert not got[0][i].any() and not got[1][i].any()
 
 
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("shape", [(3, 40, 1, 4, 2, 64), (32, 130, 1, 16, 16, 128), (2, 1, 1, 8, 8, 32)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_a_single_key_has_no_gradient(shape, types):
+    """Its probability is 1 whatever the score: dq and dk are zeros, no
+    differences of rounded sums."""
+    print(f"[attention] a single key {shape} {types}", flush=True)
+    q, k, v, dout = inputs(*shape, TYPES[types])
+    for causal in (False, True):
+        _, dq, dk, _ = run(q, k, v, dout, causal=causal)
+        assert not dq.any() and not dk.any()
+    check_all(q, k, v, dout)
+    # one key among more by its length, or as the first query's
+    q, k, v, dout = inputs(2, 70, 70, 4, 4, 64, TYPES[types])
+    one = torch.tensor([1, 1], dtype=torch.int32, device="cuda")
+    got = run(q, k, v, dout, causal=True, key_lengths=one)
+    assert not got[1].any() and not got[2].any() and bool(got[3].any())
+    for sk in (70, 50):
+        got = run(q, k[:, :sk], v[:, :sk], dout, causal=True)
+        assert not got[1][:, :71 - sk].any() and bool(got[1][:, 71 - sk:].any())
+    # that query alone: nothing for the first key either
+    only = torch.zeros_like(dout)
+    only[:, 0] = dout[:, 0]
+    got = run(q, k, v, only, causal=True)
+    assert not got[1].any() and not got[2].any() and bool(got[3].any())
+
+
 def test_not_finite():
     """NaN in a query is that query's alone."""
     print("[attention] not finite", flush=True)
