@@ -298,7 +298,9 @@ __device__ inline RowAt row_at(const AttentionArgs& a, int kv_head, int row) {
   return {kv_head * a.group + h, row - h * a.queries};
 }
 
+// (without queries nothing is read)
 __device__ inline int keys_of(const AttentionArgs& a, int batch) {
+  if (!a.queries) return 0;
   if (!a.lengths) return a.keys;
   const int n = a.lengths[batch];
   return n < 0 ? 0 : n < a.keys ? n : a.keys;

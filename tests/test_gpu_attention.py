@@ -191,6 +191,22 @@ def test_empty():
         assert not any(t.any() for t in got)
 
 
+def test_no_queries_read_nothing():
+    """dk and dv are zeros, and neither keys nor values need be there."""
+    print("[attention] no queries", flush=True)
+    for dtype, code in ((torch.float32, ma.MICROADAM_F32), (torch.bfloat16, ma.MICROADAM_BF16)):
+        for dim in (64, 128):
+            for keys in (5, 200 * 256):
+                none = ma.microadam_heads(None, 0, 0, 0)
+                given = ma.microadam_attention(none, none, none, None, 1, 0, keys, 2, 2, dim, 1.0, code, 0)
+                dk, dv = (torch.full((keys, 2, dim), math.nan, dtype=dtype, device="cuda") for _ in range(2))
+                at = [ma.microadam_heads(t.data_ptr(), 0, 2 * dim, dim) for t in (dk, dv)]
+                ma.microadam_attention_grad(given, none, None, 0, none, none, *at, None, 0,
+                                            torch.cuda.current_stream().cuda_stream)
+                torch.cuda.synchronize()
+                assert not dk.any() and not dv.any()
+
+
 def test_same_bits():
     """Of calls alike, and of a sequence alone and in a batch."""
     print("[attention] same bits", flush=True)
