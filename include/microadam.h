@@ -596,10 +596,12 @@ int microadam_layer_norm_grad(const microadam_rows* rows, const float* mean, con
  * before their products with bfloat16 operands (half a step, 2^-8 of each),
  * binary32 operands are multiplied in binary32.
  *
+ * batch times kv_heads times the tiles of 128 rows (or keys) stay below 2^24.
+ *
  * An operand is addressed by the elements from sequence to sequence, position
  * to position (dim to 2^23) and head to head (>= 0, at most 2^40; addresses are
- * aligned to the element type); the elements of dim are contiguous.  What is written has
- * no two elements in one place, and shares no byte with what is read.
+ * aligned to the element type); the elements of dim are contiguous.  What is
+ * written has no two elements in one place, and shares no byte with what is read.
  */
 typedef struct microadam_heads {
   void* data;

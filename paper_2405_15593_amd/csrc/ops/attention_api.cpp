@@ -18,8 +18,8 @@ namespace {
 
 constexpr int64_t kMaxSide = (int64_t)1 << 30;     // queries of a key head's query heads, keys
 constexpr int64_t kMaxStride = (int64_t)1 << 40;
-constexpr int64_t kMaxPosition = (int64_t)1 << 23;  // a tile's 64 rows are reached by 31 bits of bytes
-constexpr int64_t kMaxGroups = (int64_t)1 << 30;   // workgroups
+constexpr int64_t kMaxPosition = (int64_t)1 << 23;  // the rows that are loaded at once (64, of bfloat16 128) lie within 2^31 bytes
+constexpr int64_t kMaxGroups = (int64_t)1 << 24;   // workgroups of 256: a launch has fewer than 2^32 threads
 constexpr uint64_t kAlign = 256;
 
 int64_t size_of(int32_t dtype) { return dtype == MICROADAM_BF16 ? 2 : 4; }
@@ -38,9 +38,10 @@ int check(const microadam_attention* t, AttentionArgs& a) {
   if (t->batch > kMaxSide || t->queries > kMaxSide || t->keys > kMaxSide || t->heads > kMaxSide ||
       (t->heads / t->kv_heads) * t->queries > kMaxSide)
     return report(MICROADAM_ERR_UNSUPPORTED, "more than 2^30 sequences, keys, or queries that share a key head");
-  const int64_t tiles = (std::max((t->heads / t->kv_heads) * t->queries, t->keys) + 31) / 32;
-  if (t->batch > 0 && tiles > 0 && t->kv_heads > kMaxGroups / t->batch / tiles)
-    return report(MICROADAM_ERR_UNSUPPORTED, "batch times heads times positions too large");
+  // (tiles of 32 are taken only where those of 128 are fewer than 512)
+  const int64_t tiles = (std::max((t->heads / t->kv_heads) * t->queries, t->keys) + 127) / 128;
+  if (t->batch > 0 && tiles > 0 && t->kv_heads > (kMaxGroups - 1) / t->batch / tiles)
+    return report(MICROADAM_ERR_UNSUPPORTED, "sequences times key heads times tiles of 128 positions: 2^24 or more");
   const float c = (float)(t->scale * 1.4426950408889634);
   if (!(c > 0.0f) || !std::isfinite(c) || !((float)t->scale > 0.0f))
     return report(MICROADAM_ERR_INVALID_ARG, "scale must be > 0 and in the range of binary32");

@@ -143,6 +143,14 @@ def test_nothing_to_do():
     backward(given(q=none, k=none, v=none, batch=0), none, None, 0, none, none, none, none, None, 0)
 
 
+def test_workgroups():
+    """A launch has fewer than 2^24 of them: the last size that passes, and the next."""
+    for kw, most in ((dict(queries=1, keys=1), (1 << 23) - 1), (dict(queries=64, keys=1), (1 << 23) - 1),
+                     (dict(queries=65, keys=1), (1 << 22) - 1), (dict(queries=1, keys=129), (1 << 22) - 1)):
+        ma.microadam_attention_saved(given(batch=most, **kw))
+        refused(UNSUPPORTED, ma.microadam_attention_saved, given(batch=most + 1, **kw))
+
+
 def test_python():
     x = torch.ones(1, 2, 1, 8)
     with pytest.raises(ValueError):
