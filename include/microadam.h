@@ -537,8 +537,8 @@ int microadam_clip_grads(void* const* grads, const int64_t* numels, const int32_
  *     m = mean x,  r = 1 / sqrt(mean (x - m)^2 + eps),  h = (x - m) r,
  *     y = h w + b
  * in binary32 or more, y rounded once to x's dtype.  cols is at most 2^24, rows
- * at most 2^31; addresses are aligned to their element type, and rows may start
- * anywhere.  A row with NaN or an infinity gives NaN in its own y.
+ * at most 2^31, rows times ld at most 2^60; addresses are aligned to their
+ * element type, and rows may start anywhere.  A row with NaN or an infinity gives NaN in its own y.
  */
 typedef struct microadam_rows {
   const void* x;

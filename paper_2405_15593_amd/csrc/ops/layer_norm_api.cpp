@@ -16,6 +16,7 @@ namespace {
 constexpr int64_t kMaxCols = (int64_t)1 << 24;
 constexpr int64_t kMaxRows = (int64_t)1 << 31;
 constexpr int64_t kMaxLd = (int64_t)1 << 40;
+constexpr int64_t kMaxReach = (int64_t)1 << 60;
 
 int64_t size_of(int32_t dtype) { return dtype == MICROADAM_BF16 ? 2 : 4; }
 bool is_dtype(int32_t d) { return d == MICROADAM_F32 || d == MICROADAM_BF16; }
@@ -55,6 +56,8 @@ int check(const microadam_rows* r, LayerNormArgs& a) {
 int check_ld(int64_t ld, const microadam_rows* r) {
   if (ld < r->cols && r->rows > 1) return report(MICROADAM_ERR_INVALID_ARG, "a row stride is below cols");
   if (ld > kMaxLd) return report(MICROADAM_ERR_UNSUPPORTED, "a row stride is above 2^40");
+  if (r->rows > 1 && ld > kMaxReach / r->rows)
+    return report(MICROADAM_ERR_UNSUPPORTED, "a matrix reaches over more than 2^60 elements");
   return MICROADAM_OK;
 }
 

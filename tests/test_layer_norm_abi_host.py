@@ -55,6 +55,17 @@ def test_rows(kw, code):
     refused(code, backward, rows(**kw))
 
 
+def test_reach():
+    """A matrix ends within 2^60 elements: what lies where is known in 64 bits."""
+    far = dict(rows=1 << 30, cols=16)
+    for f in (forward, backward):
+        refused(UNSUPPORTED, f, rows(ld=(1 << 30) + 1, **far))
+    refused(UNSUPPORTED, forward, rows(**far), y_ld=1 << 40)
+    refused(UNSUPPORTED, backward, rows(**far), dy_ld=1 << 31)
+    refused(UNSUPPORTED, backward, rows(**far), dx_ld=1 << 31)
+    refused(INVALID, forward, rows(ld=1 << 30, **far))     # (the reach is allowed: y lies in x)
+
+
 @pytest.mark.parametrize("kw,code", [
     (dict(y=None), INVALID), (dict(y=Y + 2), INVALID), (dict(y_ld=15), INVALID), (dict(mean=None), INVALID),
     (dict(rstd=None), INVALID), (dict(mean=MEAN + 1), INVALID), (dict(y_ld=1 << 41), UNSUPPORTED),
