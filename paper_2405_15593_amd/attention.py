@@ -32,10 +32,14 @@ def _on(device):
     return _HERE if device.index == torch.cuda.current_device() else torch.cuda.device(device)
 
 
+_FAR = 1 << 23
+
+
 def _rows(t: torch.Tensor) -> torch.Tensor:
-    """t, or a copy where its rows are not contiguous or share elements."""
+    """t, or a copy where its rows are not contiguous, share elements or lie
+    further apart than the C ABI takes."""
     _, pos, _, one = t.stride()
-    return t if one == 1 and (pos >= t.shape[3] or t.shape[1] <= 1) else t.contiguous()
+    return t if one == 1 and (t.shape[3] <= pos <= _FAR or t.shape[1] <= 1) else t.contiguous()
 
 
 def _heads(t: torch.Tensor) -> microadam_heads:
@@ -143,9 +147,10 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, causal: bool
     consecutive query heads share a key head.  ``scale`` is 1 / sqrt(dim)
     unless given.  ``key_lengths`` (int32, one per sequence): how many of the
     first keys there are; what lies past them is not read.  ``causal``: the
-    last query sees the last of the keys, each one before it one key less.  A
-    query without a key gives zeros.  There is no derivative of the backward
-    pass, nor one in forward mode."""
+    last query sees the last of the keys, each one before it one key less; what
+    it hides is multiplied by zero, and expected to be finite.  A query without
+    a key gives zeros.  There is no derivative of the backward pass, nor one in
+    forward mode."""
     refuse_tangents("attention", (q, k, v))
     _check(q, k, v, key_lengths)
     scale = 1.0 / math.sqrt(q.shape[3]) if scale is None and q.shape[3] else scale if scale is not None else 1.0

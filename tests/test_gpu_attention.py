@@ -119,6 +119,12 @@ def test_layouts(types):
     k1, v1 = (t[:1].expand(2, 70, 4, 64) for t in (k, v))
     for g, w in zip(run(q, k1, v1, dout), run(q, k1.contiguous(), v1.contiguous(), dout)):
         assert torch.equal(g, w)
+    # positions further apart than the kernels reach
+    far = torch.zeros((1 << 23) + 8 + 64, device="cuda", dtype=dtype).as_strided((1, 2, 1, 64), (0, (1 << 23) + 8, 0, 1))
+    far.copy_(k[:1, :2, :1])
+    near = far.contiguous()
+    for g, w in zip(run(far, far, far, far), run(near, near, near, near)):
+        assert torch.equal(g, w)
     # gradients of what was expanded are summed by autograd
     leaf = k[:1].clone().requires_grad_()
     torch.autograd.grad(attention(q, leaf.expand(2, 70, 4, 64), v), leaf, dout)
