@@ -258,6 +258,24 @@ def load(path: str = LIBRARY):
     return lib
 
 
+_torch_side = None
+
+
+def operators():
+    """The tensor side of the operators that have one in C++; raises if it is
+    not built."""
+    global _torch_side
+    if _torch_side is None:
+        load()
+        import torch  # noqa: F401  (whose libraries it needs)
+        path = os.path.join(_PKG, "_operators.so")
+        if not os.path.exists(path):
+            raise RuntimeError(f"{path} is not built: run `python -c 'import __graft_entry__ as g; g.build()'`")
+        from . import _operators
+        _torch_side = _operators
+    return _torch_side
+
+
 def _check(rc: int, where: str) -> None:
     if rc != MICROADAM_OK:
         lib = load()

@@ -112,3 +112,10 @@ def test_python():
     for bad in (x, x.to(torch.float16), x.double()):
         with pytest.raises((ValueError, TypeError)):
             layer_norm(bad)
+
+
+def test_the_tensor_side_is_not_built(monkeypatch, tmp_path):
+    monkeypatch.setattr(ma, "_torch_side", None)
+    monkeypatch.setattr(ma, "_PKG", str(tmp_path))
+    with pytest.raises(RuntimeError, match="not built"):
+        layer_norm(torch.ones(2, 3))
