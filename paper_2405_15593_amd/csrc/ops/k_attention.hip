@@ -326,9 +326,9 @@ __global__ __launch_bounds__(kThreads, BF16 || D <= 64 ? 2 : 1) void attention_f
 // The parts of a row's keys joined by WAVES waves: lane i has the sums of parts i,
 // i + 64, .., then two elements of the row; the waves share the parts.
 template <bool BF16, int WAVES>
-__global__ __launch_bounds__(kThreads) void attention_join_kernel(const AttentionArgs a) {
-  constexpr int kEach = kMostParts / 64, kRowsHere = kThreads / 64 / WAVES;
-  __shared__ float2v others[kThreads / 64][64];
+__global__ __launch_bounds__(WAVES == 1 ? kThreads : 64 * WAVES) void attention_join_kernel(const AttentionArgs a) {
+  constexpr int kEach = kMostParts / 64, kRowsHere = WAVES == 1 ? kThreads / 64 : 1;
+  __shared__ float2v others[WAVES * kRowsHere][64];
   const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), which = wave % WAVES;
   const int64_t rows = (int64_t)a.batch * a.kv_heads * a.rows, n = (int64_t)blockIdx.x * kRowsHere + wave / WAVES;
   const bool live = n < rows;
@@ -416,10 +416,13 @@ void launch_rows(const AttentionArgs& a, hipStream_t s) {
   else
     attention_kernel<BF16, D><<<dim3((unsigned)(tiles * heads)), dim3(kThreads), 0, s>>>(a);
   if (a.parts) {
-    // (more than eight parts: four waves a row)
+    // (waves to a row; of 32, 128 and 256 parts sixteen instead of four: 13.5 -> 12.7,
+    // 14.0 -> 12.9 and 19.9 -> 16.9 us for both launches)
     const int64_t rows = (int64_t)heads * a.rows, waves = kThreads / 64;
-    if (a.parts > 8)
-      attention_join_kernel<BF16, kThreads / 64><<<dim3((unsigned)rows), dim3(kThreads), 0, s>>>(a);
+    if (a.parts > 16)
+      attention_join_kernel<BF16, 16><<<dim3((unsigned)rows), dim3(1024), 0, s>>>(a);
+    else if (a.parts > 8)
+      attention_join_kernel<BF16, 4><<<dim3((unsigned)rows), dim3(256), 0, s>>>(a);
     else
       attention_join_kernel<BF16, 1><<<dim3((unsigned)((rows + waves - 1) / waves)), dim3(kThreads), 0, s>>>(a);
   }
