@@ -80,6 +80,26 @@ def test_scales(scale, types):
     check_all(*inputs(1, 70, 130, 2, 1, 64, TYPES[types]), causal=True, scale=scale)
 
 
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("shape", [(9, 1, 3000, 4, 1, 64), (70, 1, 700, 2, 1, 32), (200, 1, 600, 1, 1, 16), (5, 60, 2000, 1, 1, 96)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_uneven_lengths(shape, types):
+    """Keys in parts: one long sequence among short ones, all alike, each another,
+    none at all."""
+    print(f"[attention] uneven {shape} {types}", flush=True)
+    b, sq, sk = shape[:3]
+    given = inputs(*shape, TYPES[types], seed=sum(shape))
+    g = torch.Generator().manual_seed(5)
+    for lengths in (torch.tensor([sk] + [3] * (b - 1)), torch.tensor([1] * (b - 1) + [sk]), torch.full((b,), sk // 2),
+                    torch.randint(0, sk + 1, (b,), generator=g), torch.zeros(b, dtype=torch.long),
+                    torch.tensor([0] * (b // 2) + [sk - 7] + [0] * (b - b // 2 - 1))):
+        lengths = lengths.to("cuda", torch.int32)
+        for causal in (False, True):
+            out = attention(*given[:3], causal=causal, key_lengths=lengths)
+            want, tolerance = reference(*given, causal, lengths, shape[5] ** -0.5, TYPES[types])
+            check((out,), want[:1], tolerance[:1], TYPES[types])
+
+
 def test_large_scores():
     """Scores of thousands, alike and apart: no overflow, no NaN."""
     print("[attention] large scores", flush=True)
