@@ -19,6 +19,7 @@ struct __attribute__((packed, aligned(2))) Piece2 {
 struct __attribute__((packed, aligned(4))) Piece4 {
   uint4v q;
 };
+typedef uint32_t piece2 __attribute__((ext_vector_type(4), aligned(2)));
 
 // Two binary32 values as two bfloat16, rounded to nearest even.
 __device__ inline uint32_t pack_bf16(float a, float b) {
@@ -51,6 +52,10 @@ struct Elements {
   __device__ static uint4v load(const void* p, int64_t i) {
     if (BF16) return ((const Piece2*)((const uint16_t*)p + i))->q;
     return ((const Piece4*)((const float*)p + i))->q;
+  }
+  // ... past the caches
+  __device__ static uint4v load_past(const void* p, int64_t i) {
+    return (uint4v)__builtin_nontemporal_load((const piece2*)((const uint8_t*)p + i * kSize));
   }
   __device__ static void store(void* p, int64_t i, const uint4v& q) {
     if (BF16)

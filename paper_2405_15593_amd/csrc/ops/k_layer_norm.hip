@@ -13,9 +13,10 @@
 // a fixed order.  Rows too long for registers are read once more per pass, and
 // their dw and db summed by columns.
 //
-// The bound is memory.  16384 x 4096 bfloat16: forward 46 to 50 us (5.4 to 5.8
-// TB/s), backward 75 to 81 and 4 to 5 for the join (4.7 to 5.1 TB/s).  Small
-// matrices take a row's own time: 4096 x 256 binary32 5, 6 and 3 us.
+// The bound is memory.  16384 x 4096 bfloat16: forward 45 to 50 us (5.4 to 6.0
+// TB/s), backward with the join of 4 to 5 us 69 to 80 (5.0 to 5.8 TB/s, by where the
+// matrices lie to each other).  Small matrices take a row's own time: 4096 x 256
+// binary32 5, 6 and 3 us.
 #include "elements.h"
 #include "layer_norm_device.h"
 
@@ -40,9 +41,10 @@ __device__ inline uint4v load_some(const void* p, int64_t at, int left) {
 }
 
 // Up to sixteen bytes of a row from element `at` on, zeros from `left` elements on.
-template <bool BF16>
+template <bool BF16, bool PAST = false>
 __device__ inline uint4v load_piece(const void* p, int64_t at, int left) {
-  if (left >= Elements<BF16>::kPer) return Elements<BF16>::load(p, at);
+  typedef Elements<BF16> E;
+  if (left >= E::kPer) return PAST ? E::load_past(p, at) : E::load(p, at);
   return load_some<BF16>(p, at, left);
 }
 
@@ -118,11 +120,12 @@ template <bool BF16, int P, int G>
 struct Row {
   typedef Elements<BF16> E;
   uint4v q[P];
+  template <bool PAST>
   __device__ void load(const void* p, int64_t from, int t, int cols) {
 #pragma unroll
     for (int i = 0; i < P; ++i) {
       const int at = (i * G + t) * E::kPer;
-      q[i] = load_piece<BF16>(p, from + at, cols - at);
+      q[i] = load_piece<BF16, PAST>(p, from + at, cols - at);
     }
   }
   __device__ float get(int i, int j) const { return E::get(q[i], j); }
@@ -135,7 +138,7 @@ struct Shape {
   static constexpr int kCols = P * G * kPer;  // at most
 };
 
-template <bool BF16, int P, int G, int R>
+template <bool BF16, int P, int G, int R, bool PAST>
 __global__ __launch_bounds__(G* R) void layer_norm_kernel(const LayerNormArgs a) {
   typedef Elements<BF16> E;
   constexpr int per = E::kPer;
@@ -148,7 +151,7 @@ __global__ __launch_bounds__(G* R) void layer_norm_kernel(const LayerNormArgs a)
   const int64_t step = (int64_t)gridDim.x * R;
   int64_t row = (int64_t)blockIdx.x * R + threadIdx.x / G;
   Row<BF16, P, G> next;
-  auto load = [&](int64_t r) { next.load(a.x, r < a.rows ? r * a.x_ld : 0, t, r < a.rows ? cols : 0); };
+  auto load = [&](int64_t r) { next.template load<PAST>(a.x, r < a.rows ? r * a.x_ld : 0, t, r < a.rows ? cols : 0); };
   if (kAhead) load(row);
   float w[P][per], b[P][per];
 #pragma unroll
@@ -202,7 +205,7 @@ __global__ __launch_bounds__(G* R) void layer_norm_kernel(const LayerNormArgs a)
 // The partial sums of a workgroup lie as its threads hold them, dw then db: sum j
 // of piece i of thread t at (i per + j) G + t, so that they are written and read
 // in whole lines.
-template <bool BF16, int P, int G, int R>
+template <bool BF16, int P, int G, int R, bool PAST>
 __global__ __launch_bounds__(G* R) void layer_norm_grad_kernel(const LayerNormArgs a) {
   typedef Elements<BF16> E;
   constexpr int per = E::kPer, kSums = P * G * per;
@@ -219,8 +222,8 @@ __global__ __launch_bounds__(G* R) void layer_norm_grad_kernel(const LayerNormAr
   float next_mean = 0.0f, next_rstd = 0.0f;
   auto load = [&](int64_t r) {
     const bool there = r < a.rows;
-    next_x.load(a.x, there ? r * a.x_ld : 0, t, there ? cols : 0);
-    next_dy.load(a.dy, there ? r * a.dy_ld : 0, t, there ? cols : 0);
+    next_x.template load<PAST>(a.x, there ? r * a.x_ld : 0, t, there ? cols : 0);
+    next_dy.template load<PAST>(a.dy, there ? r * a.dy_ld : 0, t, there ? cols : 0);
     next_mean = there ? a.mean[r] : 0.0f;
     next_rstd = there ? a.rstd[r] : 0.0f;
   };
@@ -501,15 +504,33 @@ bool with_backward_shape(int64_t cols, F f) {
   return false;
 }
 
+// Whether what a pass reads and writes, so many matrices, is more than the
+// last-level cache's 256 MiB: it is read past the caches then.  With / without, us:
+//   backward  24576 x  4096 bfloat16 (604 MB)  98 / 113   16384 x 2048 binary32 (403 MB) 67 / 76
+//             65536 x   512 bfloat16 (201 MB)  37.8 / 37.2
+//   forward   24576 x  4096 bfloat16 (403 MB)  66 / 77     4096 x 16000 binary32 (524 MB) 82 / 100
+//             16384 x  4096 bfloat16 (268 MB)  46.8 / 45.5
+// (Results that are written past them too: 1 to 5 us more.)
+bool past_caches(const LayerNormArgs& a, int matrices) {
+  return a.rows * a.cols * (a.bf16 ? 2 : 4) * matrices > (int64_t)256 << 20;
+}
+
 template <bool BF16, int P, int G, int R>
 void forward(const LayerNormArgs& a, hipStream_t s, Shape<BF16, P, G, R>) {
   const int64_t turns = (a.rows + R - 1) / R, most = 256 * (P == 1 ? 2048 : 1024) / (G * R);
-  layer_norm_kernel<BF16, P, G, R><<<dim3((unsigned)(turns < most ? turns : most)), dim3(G * R), 0, s>>>(a);
+  const dim3 grid((unsigned)(turns < most ? turns : most));
+  if (past_caches(a, 2))
+    layer_norm_kernel<BF16, P, G, R, true><<<grid, dim3(G * R), 0, s>>>(a);
+  else
+    layer_norm_kernel<BF16, P, G, R, false><<<grid, dim3(G * R), 0, s>>>(a);
 }
 
 template <bool BF16, int P, int G, int R>
 void backward(const LayerNormArgs& a, hipStream_t s, Shape<BF16, P, G, R>) {
-  layer_norm_grad_kernel<BF16, P, G, R><<<dim3(a.parts), dim3(G * R), 0, s>>>(a);
+  if (past_caches(a, 3))
+    layer_norm_grad_kernel<BF16, P, G, R, true><<<dim3(a.parts), dim3(G * R), 0, s>>>(a);
+  else
+    layer_norm_grad_kernel<BF16, P, G, R, false><<<dim3(a.parts), dim3(G * R), 0, s>>>(a);
 }
 
 template <bool BF16>
