@@ -13,10 +13,9 @@
 // a fixed order.  Rows too long for registers are read once more per pass, and
 // their dw and db summed by columns.
 //
-// The bound is memory.  16384 x 4096 bfloat16: forward 45 to 50 us (5.4 to 6.0
-// TB/s), backward with the join of 4 to 5 us 69 to 80 (5.0 to 5.8 TB/s, by where the
-// matrices lie to each other).  Small matrices take a row's own time: 4096 x 256
-// binary32 5, 6 and 3 us.
+// The bound is memory.  16384 x 4096 bfloat16, forward and backward in turn: 125 us
+// (5.4 TB/s), 49 of them forward, 4 to 5 the join.  Small matrices take a row's own
+// time: 4096 x 256 binary32 5, 6 and 3 us.
 #include "elements.h"
 #include "layer_norm_device.h"
 
@@ -504,15 +503,16 @@ bool with_backward_shape(int64_t cols, F f) {
   return false;
 }
 
-// Whether what a pass reads and writes, so many matrices, is more than the
-// last-level cache's 256 MiB: it is read past the caches then.  With / without, us:
-//   backward  24576 x  4096 bfloat16 (604 MB)  98 / 113   16384 x 2048 binary32 (403 MB) 67 / 76
-//             65536 x   512 bfloat16 (201 MB)  37.8 / 37.2
-//   forward   24576 x  4096 bfloat16 (403 MB)  66 / 77     4096 x 16000 binary32 (524 MB) 82 / 100
-//             16384 x  4096 bfloat16 (268 MB)  46.8 / 45.5
-// (Results that are written past them too: 1 to 5 us more.)
+// Whether what a pass reads and writes, so many matrices, fills the last-level
+// cache's 256 MiB: it is read past the caches then.  Forward and backward in turn,
+// and each with an operator that reads its result (a product; a sum), with / without, us:
+//   32768 x 4096 bfloat16  244 / 254   307 + 286 / 309 + 288
+//   16384 x 4096           125 / 132   152 + 138 / 155 + 146
+//    8192 x 4096            69 /  66    92 +  72 /  92 +  74   (neither is)
+//    2048 x 4096            27 /  26    45 +  26 /  45 +  26
+// (Results that are written past the caches: 117 for the second, but 160 + 148.)
 bool past_caches(const LayerNormArgs& a, int matrices) {
-  return a.rows * a.cols * (a.bf16 ? 2 : 4) * matrices > (int64_t)256 << 20;
+  return a.rows * a.cols * (a.bf16 ? 2 : 4) * matrices >= (int64_t)256 << 20;
 }
 
 template <bool BF16, int P, int G, int R>

@@ -91,6 +91,29 @@ def test_many_rows(rows, cols, types):
     check(run(*given), *reference(*given, 1e-5))
 
 
+@pytest.mark.parametrize("types,rows,cols", [("f32", 33001, 1031), ("bf16", 33001, 2049), ("bf16_f32", 8400, 16384)])
+def test_beyond_the_caches(types, rows, cols):
+    """Rows of a call over 256 MiB have the bits of a small call's; dw and db are
+    the sums over small calls' in binary64 (each within its own tolerance)."""
+    print(f"[norm] beyond the caches {rows} x {cols} {types}", flush=True)
+    x, w, b, dy = inputs(rows, cols, types)
+    y, dx, dw, db = run(x, w, b, dy)
+    for at in range(0, rows, rows // 3):
+        part = slice(at, at + 300)
+        small = run(x[part], w, b, dy[part])
+        assert torch.equal(y[part], small[0]) and torch.equal(dx[part], small[1])
+    mean = x.double().mean(1, keepdim=True)
+    rstd = 1.0 / torch.sqrt(x.double().var(1, correction=0, keepdim=True) + 1e-5)
+    chain = (rows / 512 + 64) * U
+    for at in range(0, cols, 256):
+        part = slice(at, at + 256)
+        h, d = (x[:, part].double() - mean) * rstd, dy[:, part].double()
+        eh = 64 * U * (1 + h.abs()) + U * mean.abs() * rstd
+        for g, want, t in ((dw[part], (d * h).sum(0), (d.abs() * eh).sum(0) + chain * (d * h).abs().sum(0)),
+                           (db[part], d.sum(0), chain * d.abs().sum(0))):
+            assert bool(((g.double() - want).abs() <= t + HALF[g.dtype] * (want.abs() + t)).all())
+
+
 @pytest.mark.parametrize("offset", [-300.0, 1e4])
 @pytest.mark.parametrize("cols", [200, 3000, 16500])
 def test_a_mean_far_from_zero(cols, offset):
