@@ -50,6 +50,20 @@ inline bool few_groups(const AttentionArgs& a, int positions) {
 constexpr int kTokenRows = 8;
 inline bool token_rows(const AttentionArgs& a) { return !a.bf16 && a.rows <= kTokenRows; }
 
+// Whether keys and values, which a few rows' call reads once, are read past the
+// caches: where they fill the last-level cache's 256 MiB alone (fewer may be there
+// still from the call before) and a load takes whole lines of 128 bytes.  One query
+// of 32 heads on 8, with / without, us:
+//   bfloat16  64 x 2048 keys of 128 (537 MB)  88 / 99    131072 (537 MB)  94 / 104
+//             8 x 4096, lengths (67 of 134 MB)  cold 23.0 / 24.8, else 24.6 / 20.8
+//             8 x 8192 of 80 (lines shared with other heads)  40 / 38
+//   binary32  32768 of 128 (268 MB)  51 / 56             4 x 16384, lengths  46 / 49
+inline bool past_caches(const AttentionArgs& a) {
+  const int size = a.bf16 ? 2 : 4;
+  return a.dim >= 64 && a.dim * size % 128 == 0 &&
+         (int64_t)a.batch * a.kv_heads * a.keys * a.dim * 2 * size >= (int64_t)256 << 20;
+}
+
 void launch_attention_token(const AttentionArgs& a, hipStream_t s);
 
 // How many parts a forward call's keys are split into; 0: not at all.

@@ -182,6 +182,8 @@ struct Tile {
   }
 };
 
+constexpr int kNonTemporal = 2;  // a buffer load's cache policy
+
 // A tile on its way from memory to LDS through THREADS threads' registers: rows
 // of one head, `pos` bytes apart.  The buffer's size ends with the last row that
 // there is, so that rows past it read as zeros without a branch.
@@ -202,13 +204,14 @@ struct Staged {
     }
   }
   // The rows [first, first + ROWS) of which those below `end` are there.
+  template <bool PAST = false>
   __device__ void load(const void* base, int64_t pos, int dim, int first, int end) {
     const int rows = end - first < ROWS ? end - first : ROWS;
     const int bytes = rows > 0 ? (rows - 1) * (int)pos + dim * T::kSize : 0;
     const auto buffer =
         __builtin_amdgcn_make_buffer_rsrc((void*)((const uint8_t*)base + first * pos), 0, bytes, 0x00020000);
 #pragma unroll
-    for (int i = 0; i < kCount; ++i) q[i] = __builtin_amdgcn_raw_buffer_load_b128(buffer, (int)from[i], 0, 0);
+    for (int i = 0; i < kCount; ++i) q[i] = __builtin_amdgcn_raw_buffer_load_b128(buffer, (int)from[i], 0, PAST ? kNonTemporal : 0);
   }
   __device__ void store(uint8_t* tile, int thread) const {
 #pragma unroll

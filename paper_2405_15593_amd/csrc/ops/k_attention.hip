@@ -230,7 +230,7 @@ __global__ __launch_bounds__(kThreads, BF16 || D <= 64 ? 2 : 1) void attention_k
 // each on its own way through its own place in LDS, and are joined at the end.
 constexpr int kFewRows = 32, kFewKeys = 32;
 
-template <bool BF16, int D>
+template <bool BF16, int D, bool PAST>
 __global__ __launch_bounds__(kThreads, BF16 || D <= 64 ? 2 : 1) void attention_few_kernel(const AttentionArgs a) {
   typedef Tile<BF16, D, kFewKeys> T;
   constexpr int kWaves = kThreads / 64;
@@ -259,8 +259,8 @@ __global__ __launch_bounds__(kThreads, BF16 || D <= 64 ? 2 : 1) void attention_f
   next_v.start(a.dim, (int)v_pos, lane);
   int turn = own.first + wave;
   auto load = [&](int t) {
-    next_k.load(k_at, k_pos, a.dim, t * kFewKeys, length);
-    next_v.load(v_at, v_pos, a.dim, t * kFewKeys, length);
+    next_k.template load<PAST>(k_at, k_pos, a.dim, t * kFewKeys, length);
+    next_v.template load<PAST>(v_at, v_pos, a.dim, t * kFewKeys, length);
   };
   if (turn < own.last) load(turn);
 
@@ -419,8 +419,10 @@ void launch_rows(const AttentionArgs& a, hipStream_t s) {
   const int tiles = few ? (a.rows + kFewRows - 1) / kFewRows : (a.rows + kRows - 1) / kRows;
   if (!BF16 && token_rows(a))
     launch_attention_token(a, s);
+  else if (few && tiles == 1 && past_caches(a))
+    attention_few_kernel<BF16, D, true><<<dim3((unsigned)(heads * parts)), dim3(kThreads), 0, s>>>(a);
   else if (few)
-    attention_few_kernel<BF16, D><<<dim3((unsigned)(tiles * heads * parts)), dim3(kThreads), 0, s>>>(a);
+    attention_few_kernel<BF16, D, false><<<dim3((unsigned)(tiles * heads * parts)), dim3(kThreads), 0, s>>>(a);
   else
     attention_kernel<BF16, D><<<dim3((unsigned)(tiles * heads)), dim3(kThreads), 0, s>>>(a);
   if (a.parts) {

@@ -6,11 +6,10 @@
 // 51; bfloat16, whose products are sixteen times as fast, 33 and 34).  Here G lanes
 // hold a key, eight elements each, and R rows of q: a score is a sum over G lanes
 // (in-row permutes), and out's part of the key is added where v lies.  Nothing
-// passes through LDS before the end.
-// Every group of G lanes keeps its own maximum, sum and output over every so
-// many keys; a workgroup's groups are joined in LDS, parts of the keys by
-// attention_join_kernel.  The bound is memory: those 268 MB take 48 to 56 us (4.8 to
-// 5.6 TB/s) and 4 to 5 for the join.
+// passes through LDS before the end.  Every group of G lanes keeps its own maximum,
+// sum and output over every so many keys; a workgroup's groups are joined in LDS,
+// parts of the keys by attention_join_kernel.  The bound is memory: those 268 MB
+// take 43 to 47 us (5.7 to 6.3 TB/s) and 4 to 5 for the join.
 #include "attention_tile.h"
 
 namespace microadam {
@@ -35,8 +34,9 @@ __device__ inline float sum_lanes(float x) {
   return x;
 }
 
-template <int G, int R>
+template <int G, int R, bool PAST>
 __global__ __launch_bounds__(kThreads, 2) void attention_token_kernel(const AttentionArgs a) {
+  constexpr int kPolicy = PAST ? kNonTemporal : 0;
   constexpr int kKeys = 64 / G;            // keys of a wave at once
   constexpr int kDeep = R == 8 ? 2 : 4;    // one behind the other (as registers allow)
   constexpr int kStep = kKeys * kDeep;
@@ -45,7 +45,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_token_kernel(const Atte
   __shared__ float sums[R][kGroups][G * 8];
   __shared__ float stats[R][kGroups][2];
   const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
-  const int in = lane % G, group = lane / G, d = in * 8;
+  const int in = lane % G, group = lane / G;
   int head_of = blockIdx.x, part = 0;
   if (a.parts) {
     part = head_of % a.parts;
@@ -69,13 +69,17 @@ __global__ __launch_bounds__(kThreads, 2) void attention_token_kernel(const Atte
   const int64_t k_pos = a.k.pos * size, v_pos = a.v.pos * size;
   const uint8_t* k_at = (const uint8_t*)a.k.at + (batch * a.k.batch + kv_head * a.k.head) * size;
   const uint8_t* v_at = (const uint8_t*)a.v.at + (batch * a.v.batch + kv_head * a.v.head) * size;
-  uint32_t k_from[kDeep], v_from[kDeep];
+  // (element 4 (i G + in) + j of a row is a lane's 4 i + j: each load takes whole lines)
+  auto element = [&](int i) { return 4 * (i * G + in); };
+  uint32_t k_from[kDeep][kLoads], v_from[kDeep][kLoads];
 #pragma unroll
-  for (int u = 0; u < kDeep; ++u) {
-    const int key = u * kKeys + group;
-    k_from[u] = d < a.dim ? (uint32_t)(key * (int)k_pos + d * size) : 0x80000000u;
-    v_from[u] = d < a.dim ? (uint32_t)(key * (int)v_pos + d * size) : 0x80000000u;
-  }
+  for (int u = 0; u < kDeep; ++u)
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int key = u * kKeys + group, e = element(i);
+      k_from[u][i] = e < a.dim ? (uint32_t)(key * (int)k_pos + e * size) : 0x80000000u;
+      v_from[u][i] = e < a.dim ? (uint32_t)(key * (int)v_pos + e * size) : 0x80000000u;
+    }
   struct Loaded {
     uint4v k[kDeep][kLoads], v[kDeep][kLoads];
   };
@@ -88,11 +92,11 @@ __global__ __launch_bounds__(kThreads, 2) void attention_token_kernel(const Atte
 #pragma unroll
     for (int u = 0; u < kDeep; ++u)
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i) to.k[u][i] = __builtin_amdgcn_raw_buffer_load_b128(k_buffer, (int)(k_from[u] + 16 * i), 0, 0);
+      for (int i = 0; i < kLoads; ++i) to.k[u][i] = __builtin_amdgcn_raw_buffer_load_b128(k_buffer, (int)k_from[u][i], 0, kPolicy);
 #pragma unroll
     for (int u = 0; u < kDeep; ++u)
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i) to.v[u][i] = __builtin_amdgcn_raw_buffer_load_b128(v_buffer, (int)(v_from[u] + 16 * i), 0, 0);
+      for (int i = 0; i < kLoads; ++i) to.v[u][i] = __builtin_amdgcn_raw_buffer_load_b128(v_buffer, (int)v_from[u][i], 0, kPolicy);
   };
   Loaded next;
   int step = first + wave;
@@ -102,14 +106,17 @@ __global__ __launch_bounds__(kThreads, 2) void attention_token_kernel(const Atte
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     const RowAt at = row_at(a, kv_head, r < a.rows ? r : 0);
-    const Frag<false> f =
-        load_frag<false>(a.q.at, batch * a.q.batch + at.head * a.q.head + at.query * a.q.pos + d, r < a.rows && d < a.dim);
+    const int64_t q_at = batch * a.q.batch + at.head * a.q.head + at.query * a.q.pos;
     m[r] = -infinity();
     l[r] = 0.0f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      q[r][j] = f.v[j];
-      out[r][j] = 0.0f;
+    for (int i = 0; i < kLoads; ++i) {
+      const uint4v f = r < a.rows && element(i) < a.dim ? Elements<false>::load(a.q.at, q_at + element(i)) : uint4v{0, 0, 0, 0};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        q[r][4 * i + j] = __uint_as_float(f[j]);
+        out[r][4 * i + j] = 0.0f;
+      }
     }
   }
   for (; step < last; step += kWaves) {
@@ -184,7 +191,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_token_kernel(const Atte
       stats[r][slot][1] = l[r];
     }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) sums[r][slot][d + j] = out[r][j];
+    for (int j = 0; j < 8; ++j) sums[r][slot][element(j / 4) + j % 4] = out[r][j];
   }
   __syncthreads();
   // a thread an element of a row
@@ -217,17 +224,25 @@ __global__ __launch_bounds__(kThreads, 2) void attention_token_kernel(const Atte
   }
 }
 
+template <int G, int R>
+void launch_rows(const AttentionArgs& a, hipStream_t s) {
+  const dim3 grid((unsigned)(a.kv_heads * a.batch * (a.parts ? a.parts : 1)));
+  if (past_caches(a))
+    attention_token_kernel<G, R, true><<<grid, dim3(kThreads), 0, s>>>(a);
+  else
+    attention_token_kernel<G, R, false><<<grid, dim3(kThreads), 0, s>>>(a);
+}
+
 template <int G>
 void launch_group(const AttentionArgs& a, hipStream_t s) {
-  const dim3 grid((unsigned)(a.kv_heads * a.batch * (a.parts ? a.parts : 1)));
   if (a.rows <= 1)
-    attention_token_kernel<G, 1><<<grid, dim3(kThreads), 0, s>>>(a);
+    launch_rows<G, 1>(a, s);
   else if (a.rows <= 2)
-    attention_token_kernel<G, 2><<<grid, dim3(kThreads), 0, s>>>(a);
+    launch_rows<G, 2>(a, s);
   else if (a.rows <= 4)
-    attention_token_kernel<G, 4><<<grid, dim3(kThreads), 0, s>>>(a);
+    launch_rows<G, 4>(a, s);
   else
-    attention_token_kernel<G, 8><<<grid, dim3(kThreads), 0, s>>>(a);
+    launch_rows<G, 8>(a, s);
 }
 
 }  // namespace

@@ -100,6 +100,20 @@ def test_uneven_lengths(shape, types):
             check((out,), want[:1], tolerance[:1], TYPES[types])
 
 
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("shape", [(1, 1, 132000, 8, 4, 128), (2, 2, 132000, 4, 4, 64), (3, 3, 180000, 2, 1, 128)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_beyond_the_caches(shape, types):
+    """Keys and values that are read past them, and one call's fewer."""
+    print(f"[attention] beyond the caches {shape} {types}", flush=True)
+    given = inputs(*shape, TYPES[types], seed=sum(shape))
+    for lengths in (None, some_lengths(shape[0], shape[2])):
+        out = attention(*given[:3], causal=True, key_lengths=lengths)
+        n = None if lengths is None else lengths.clamp(0, shape[2])
+        want, tolerance = reference(*given, True, n, shape[5] ** -0.5, TYPES[types])
+        check((out,), want[:1], tolerance[:1], TYPES[types])
+
+
 def test_large_scores():
     """Scores of thousands, alike and apart: no overflow, no NaN."""
     print("[attention] large scores", flush=True)
