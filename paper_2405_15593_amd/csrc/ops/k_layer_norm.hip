@@ -114,8 +114,14 @@ struct GroupSum {
   }
 };
 
-// A row's pieces in the registers: G threads to a row, P pieces each.
-template <bool BF16, int P, int G>
+// A row's pieces in the registers: G threads to a row, P pieces each.  SETTLED: a
+// row's last piece, where it is not whole, is loaded with what lies before it, so
+// that no load waits for another, and settled when it is used.  (Forward and
+// backward, bfloat16, with a load per element there: 16384 x 4004 148 instead of
+// 203 us, 100000 x 100 73 instead of 108.  binary32's pieces are four elements:
+// forward up to 3% more.  Backward with two pieces a thread it spills: 132 instead
+// of 111.)
+template <bool BF16, int P, int G, bool SETTLED>
 struct Row {
   typedef Elements<BF16> E;
   uint4v q[P];
@@ -123,8 +129,29 @@ struct Row {
   __device__ void load(const void* p, int64_t from, int t, int cols) {
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-      const int at = (i * G + t) * E::kPer;
-      q[i] = load_piece<BF16, PAST>(p, from + at, cols - at);
+      const int at = (i * G + t) * E::kPer, last = cols - E::kPer;
+      if constexpr (!SETTLED) {
+        q[i] = load_piece<BF16, PAST>(p, from + at, cols - at);
+      } else {
+        q[i] = uint4v{0, 0, 0, 0};
+        if (last < 0)
+          q[i] = load_some<BF16>(p, from + at, cols - at);
+        else if (at < cols)
+          q[i] = PAST ? E::load_past(p, from + (at < last ? at : last)) : E::load(p, from + (at < last ? at : last));
+      }
+    }
+  }
+  __device__ void settle(int t, int cols) {
+    if (!SETTLED || cols < E::kPer) return;
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const int left = cols - (i * G + t) * E::kPer;
+      if (left <= 0 || left >= E::kPer) continue;
+      const int off = (E::kPer - left) * E::kSize;  // bytes of the elements before
+      if (off & 8) q[i] = uint4v{q[i][2], q[i][3], 0, 0};
+      if (off & 4) q[i] = uint4v{q[i][1], q[i][2], q[i][3], 0};
+      if (BF16 && (off & 2))
+        q[i] = uint4v{q[i][0] >> 16 | q[i][1] << 16, q[i][1] >> 16 | q[i][2] << 16, q[i][2] >> 16 | q[i][3] << 16, q[i][3] >> 16};
     }
   }
   __device__ float get(int i, int j) const { return E::get(q[i], j); }
@@ -149,7 +176,7 @@ __global__ __launch_bounds__(G* R) void layer_norm_kernel(const LayerNormArgs a)
   constexpr bool kAhead = G == 256 || G == 1024;  // the next row's pieces are loaded while a row is summed
   const int64_t step = (int64_t)gridDim.x * R;
   int64_t row = (int64_t)blockIdx.x * R + threadIdx.x / G;
-  Row<BF16, P, G> next;
+  Row<BF16, P, G, BF16> next;
   auto load = [&](int64_t r) { next.template load<PAST>(a.x, r < a.rows ? r * a.x_ld : 0, t, r < a.rows ? cols : 0); };
   if (kAhead) load(row);
   float w[P][per], b[P][per];
@@ -161,9 +188,10 @@ __global__ __launch_bounds__(G* R) void layer_norm_kernel(const LayerNormArgs a)
   }
   for (int64_t first = (int64_t)blockIdx.x * R; first < a.rows; first += step, row += step) {
     if (!kAhead) load(row);
-    const Row<BF16, P, G> x = next;
+    Row<BF16, P, G, BF16> x = next;
     const bool live = row < a.rows;
     if (kAhead && first + step < a.rows) load(row + step);
+    x.settle(t, cols);
     float sum = 0.0f;
 #pragma unroll
     for (int i = 0; i < P; ++i)
@@ -217,7 +245,7 @@ __global__ __launch_bounds__(G* R) void layer_norm_grad_kernel(const LayerNormAr
   constexpr bool kAhead = P == 1;  // (two pieces': 129 instead of 89 us)
   const int64_t step = (int64_t)gridDim.x * R;
   int64_t row = (int64_t)blockIdx.x * R + which;
-  Row<BF16, P, G> next_x, next_dy;
+  Row<BF16, P, G, BF16 && kAhead> next_x, next_dy;
   float next_mean = 0.0f, next_rstd = 0.0f;
   auto load = [&](int64_t r) {
     const bool there = r < a.rows;
@@ -239,9 +267,11 @@ __global__ __launch_bounds__(G* R) void layer_norm_grad_kernel(const LayerNormAr
   for (int64_t first = (int64_t)blockIdx.x * R; first < a.rows; first += step, row += step) {
     const bool live = row < a.rows;
     if (!kAhead) load(row);
-    const Row<BF16, P, G> x = next_x, dy = next_dy;
+    Row<BF16, P, G, BF16 && kAhead> x = next_x, dy = next_dy;
     const float mean = next_mean, rstd = next_rstd;
     if (kAhead && first + step < a.rows) load(row + step);
+    x.settle(t, cols);
+    dy.settle(t, cols);
     float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
     for (int i = 0; i < P; ++i)
