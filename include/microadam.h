@@ -619,7 +619,7 @@ typedef struct microadam_attention {
 
 /*
  * Bytes of workspace for the forward call (grad = 0) and for the gradients
- * (grad = 1), by the sizes and dtype alone.  It is 256-byte aligned, of any
+ * (grad = 1), by the sizes, dtype and causal alone.  It is 256-byte aligned, of any
  * content, belongs to the caller and is in use until the queued work is done;
  * where the bytes are 0 it may be NULL.
  */
@@ -639,8 +639,8 @@ int microadam_attention_forward(const microadam_attention* attention, const micr
 
 /*
  * dq, dk and dv for dout, from the operands of the forward call and the out and
- * `saved` that it wrote.  The gradients of shared heads are summed in
- * registers, in binary32, in one order: the same call gives the same bits.
+ * `saved` that it wrote.  The gradients of shared heads are summed in binary32,
+ * in an order that goes by the sizes: the same call gives the same bits.
  */
 int microadam_attention_grad(const microadam_attention* attention, const microadam_heads* out,
                              const void* saved, uint64_t saved_bytes, const microadam_heads* dout,

@@ -60,6 +60,7 @@ int check(const microadam_attention* t, AttentionArgs& a) {
   a.c = c;
   a.lengths = t->key_lengths;
   a.parts = attention_parts(a);
+  a.grad_parts = attention_grad_parts(a);
   return MICROADAM_OK;
 }
 
@@ -136,7 +137,9 @@ void set_saved(AttentionArgs& a, const void* saved) {
 uint64_t part_rows(const AttentionArgs& a) { return (uint64_t)a.batch * a.kv_heads * a.parts * a.rows; }
 
 uint64_t workspace_of(const AttentionArgs& a, bool grad) {
-  if (grad) return up(stats_bytes(a));
+  if (grad)
+    return up(stats_bytes(a)) +
+           up((uint64_t)a.grad_parts * 2 * a.batch * a.kv_heads * a.keys * a.dim * sizeof(float));
   return a.parts ? up(part_rows(a) * 2 * sizeof(float)) + up(part_rows(a) * a.dim * sizeof(float)) : 0;
 }
 
@@ -238,10 +241,11 @@ int microadam_attention_grad(const microadam_attention* attention, const microad
   if ((rc = check_saved(a, saved, saved_size))) return rc;
   if ((rc = check_workspace(a, true, workspace, workspace_bytes))) return rc;
   read[6] = run(saved, (int64_t)saved_bytes(a));
-  written[3] = run(stats_bytes(a) ? workspace : nullptr, (int64_t)workspace_of(a, true));
+  written[3] = run(workspace_of(a, true) ? workspace : nullptr, (int64_t)workspace_of(a, true));
   if ((rc = check_apart(written, 4, read, 7))) return rc;
   set_saved(a, saved);
   a.delta = (float*)workspace;
+  a.grad_part = (float*)((uint8_t*)workspace + up(stats_bytes(a)));
   if (a.batch > 0) {
     const hipError_t e = launch_attention_grad(a, (hipStream_t)stream);
     if (e != hipSuccess) return report_hip(e, "launching attention's backward pass");

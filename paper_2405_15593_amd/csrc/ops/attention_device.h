@@ -30,6 +30,10 @@ struct AttentionArgs {
   float* part_out;    // [batch][kv_heads][parts][rows][dim]
   float* part_stats;  // [batch][kv_heads][parts][rows][2]
   int32_t parts;      // 0: not split
+  // backward, with the rows that see a key split over workgroups: dk and dv of each
+  // part, without dk's scale
+  float* grad_part;    // [grad_parts][2][batch][kv_heads][keys][dim]
+  int32_t grad_parts;  // 0: not split
 };
 
 constexpr int kMostParts = 256;
@@ -68,6 +72,9 @@ void launch_attention_token(const AttentionArgs& a, hipStream_t s);
 
 // How many parts a forward call's keys are split into; 0: not at all.
 int32_t attention_parts(const AttentionArgs& a);
+
+// How many parts the backward call's rows are split into for dk and dv; 0: not at all.
+int32_t attention_grad_parts(const AttentionArgs& a);
 
 hipError_t launch_attention(const AttentionArgs& a, hipStream_t s);
 hipError_t launch_attention_grad(const AttentionArgs& a, hipStream_t s);

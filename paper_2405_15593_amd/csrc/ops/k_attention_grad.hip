@@ -8,7 +8,8 @@
 // order that changes: dq by rows, as forward, in z^T = k q^T, dp^T = v dout^T and
 // dq^T += k^T ds^T; then dk and dv by keys, in z = q k^T, dp = dout v^T, dv^T +=
 // dout^T p and dk^T += q^T ds, over all rows of the query heads that share the
-// keys.  Seven products where one kernel with shared sums would take five.
+// keys (split into parts that a third kernel joins where the keys' workgroups are
+// few).  Seven products where one kernel with shared sums would take five.
 //
 // p and ds are rounded to bfloat16 before their products with bfloat16 operands
 // (half a step, 2^-8 of each); their sums are binary32.
@@ -17,6 +18,8 @@
 // 32 heads of 128, causal, bfloat16 take 423 to 472 and 542 to 619 us (890 to 1010
 // TFLOP/s of the products that are computed; a large library product 1390), the
 // matrix cores 49 and 50% busy at 2.0 GHz, no bank conflicts.
+#include <algorithm>
+
 #include "attention_tile.h"
 
 namespace microadam {
@@ -227,8 +230,10 @@ __global__ __launch_bounds__(kThreads, (BF16 && !SPLIT) || D <= 64 ? 2 : 1) void
                             : lds + kTiles + (place * 2 * kTile + n) * 4);
   };
   const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), h = lane >> 5;
-  const Work work = work_of(blockIdx.x, a.kv_heads * a.batch);
-  const int tile = work.order, head_of = work.head;  // (the first keys are seen by the most rows)
+  const int parts = !SPLIT && a.grad_parts ? a.grad_parts : 1;
+  const Work work = work_of(blockIdx.x, a.kv_heads * a.batch * parts);
+  const int tile = work.order, head_of = work.head / parts;  // (the first keys are seen by the most rows)
+  const int part = work.head - head_of * parts;
   const typename T::Lane places(lane);
   const int kv_head = head_of % a.kv_heads, batch = head_of / a.kv_heads;
   const int length = keys_of(a, batch);
@@ -261,7 +266,8 @@ __global__ __launch_bounds__(kThreads, (BF16 && !SPLIT) || D <= 64 ? 2 : 1) void
     from = (from < 0 ? 0 : from) / kTile;
   }
   const int of_head = (a.queries + kTile - 1) / kTile - from;
-  const int turns = key0 < length && of_head > 0 ? of_head * a.group : 0;
+  const int all = key0 < length && of_head > 0 ? of_head * a.group : 0;
+  const int start = (int)((int64_t)part * all / parts), turns = (int)((int64_t)(part + 1) * all / parts);
 
   Staged<BF16, D, kTile, SPLIT ? 64 : kThreads> next_q, next_do;
   float next_lse = 0.0f, next_delta = 0.0f;
@@ -379,13 +385,13 @@ __global__ __launch_bounds__(kThreads, (BF16 && !SPLIT) || D <= 64 ? 2 : 1) void
     join_waves(dv, (float*)lds, wave, lane);
     if (wave > 0) return;
   } else {
-    if (turns > 0) {
-      load(0);
-      store(0);
+    if (turns > start) {
+      load(start);
+      store(start & 1);
     }
     wait_all();
     __syncthreads();
-    for (int turn = 0; turn < turns; ++turn) {
+    for (int turn = start; turn < turns; ++turn) {
       add(turn, turn & 1, [&]() {
         if (turn + 1 < turns) load(turn + 1);
       });
@@ -395,6 +401,16 @@ __global__ __launch_bounds__(kThreads, (BF16 && !SPLIT) || D <= 64 ? 2 : 1) void
   }
   if (key >= a.keys) return;
   // (a key behind the length has scores of its zeros: no gradient)
+  if (parts > 1) {
+    const int64_t rows = (int64_t)a.batch * a.kv_heads * a.keys, at = (int64_t)head_of * a.keys + key;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) {
+      store_column<false>(a.grad_part, (2 * part * rows + at) * a.dim + 32 * i, a.dim - 32 * i, live ? dk[i] : zeros(), 1.0f, lane);
+      store_column<false>(a.grad_part, ((2 * part + 1) * rows + at) * a.dim + 32 * i, a.dim - 32 * i, live ? dv[i] : zeros(), 1.0f,
+                          lane);
+    }
+    return;
+  }
   const float one = live ? 1.0f : 0.0f;
   const int64_t dk_at = batch * a.dk.batch + kv_head * a.dk.head + key * a.dk.pos;
   const int64_t dv_at = batch * a.dv.batch + kv_head * a.dv.head + key * a.dv.pos;
@@ -403,6 +419,27 @@ __global__ __launch_bounds__(kThreads, (BF16 && !SPLIT) || D <= 64 ? 2 : 1) void
     store_column<BF16>(a.dk.at, dk_at + 32 * i, a.dim - 32 * i, live ? dk[i] : zeros(), a.scale, lane);
     store_column<BF16>(a.dv.at, dv_at + 32 * i, a.dim - 32 * i, live ? dv[i] : zeros(), one, lane);
   }
+}
+
+// The parts of dk (blockIdx.y 0) and dv (1) joined, four elements a thread.
+template <bool BF16>
+__global__ __launch_bounds__(kThreads) void attention_dkv_join_kernel(const AttentionArgs a) {
+  const int quads = a.dim / 4;
+  const int64_t rows = (int64_t)a.batch * a.kv_heads * a.keys, n = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  const int64_t row = n / quads;
+  if (row >= rows) return;
+  const int d = (int)(n - row * quads) * 4, which = blockIdx.y;
+  const float* from = a.grad_part + (which * rows + row) * a.dim + d;
+  float4v sum = *(const float4v*)from;
+  for (int p = 1; p < a.grad_parts; ++p) sum += *(const float4v*)(from + 2 * p * rows * a.dim);
+  if (which == 0) sum *= a.scale;
+  const int64_t head_of = row / a.keys, key = row - head_of * a.keys;
+  const HeadTensor& to = which ? a.dv : a.dk;
+  const int64_t at = head_of / a.kv_heads * to.batch + head_of % a.kv_heads * to.head + key * to.pos + d;
+  if (BF16)
+    ((Four2*)((uint16_t*)to.at + at))->q = uint2v{pack_bf16(sum[0], sum[1]), pack_bf16(sum[2], sum[3])};
+  else
+    ((Four4*)((float*)to.at + at))->q = sum;
 }
 
 template <bool BF16, int D>
@@ -416,7 +453,11 @@ void launch_both(const AttentionArgs& a, hipStream_t s) {
       attention_dq_kernel<BF16, D, false><<<dim3(groups(a.rows, kRows)), dim3(kThreads), 0, s>>>(a);
   }
   if (a.keys) {
-    if (few_groups(a, a.keys))
+    if (a.grad_parts) {
+      attention_dkv_kernel<BF16, D, false><<<dim3(groups(a.keys, kRows) * a.grad_parts), dim3(kThreads), 0, s>>>(a);
+      const int64_t quads = (int64_t)heads * a.keys * (a.dim / 4);
+      attention_dkv_join_kernel<BF16><<<dim3((unsigned)((quads + kThreads - 1) / kThreads), 2), dim3(kThreads), 0, s>>>(a);
+    } else if (few_groups(a, a.keys))
       attention_dkv_kernel<BF16, D, true><<<dim3(groups(a.keys, 32)), dim3(kThreads), 0, s>>>(a);
     else
       attention_dkv_kernel<BF16, D, false><<<dim3(groups(a.keys, kRows)), dim3(kThreads), 0, s>>>(a);
@@ -436,6 +477,27 @@ void launch_dim(const AttentionArgs& a, hipStream_t s) {
 }
 
 }  // namespace
+
+// Where the query heads that share a key head are many, its workgroups are few and
+// long, causal ones of all lengths: the rows are then split into parts of 64 tiles
+// and more, up to four (causal; else two) workgroups of them to a CU.  Where there
+// are not even workgroups of 128 keys for the CUs, into parts of 16 tiles and more,
+// instead of the shared ones, if there are eight.  dq, dk and dv, not split / split, us:
+//   bfloat16  32 heads of 128 on 8   2 x 2048 causal 508 / 330   full 592 / 505
+//                                    1 x 4096        973 / 572       1119 / 925
+//             32 of 128 on 1         1 x 4096       1818 / 619
+//             4 of 64 on 1           1 x 4096        151 / 82         166 / 106
+//             (parts of 32 tiles: 32 on 32, 1 x 2048  191 / 200       247 / 289)
+//   binary32  16 of 128 on 2         1 x 2048       1484 / 698       1692 / 1065
+int32_t attention_grad_parts(const AttentionArgs& a) {
+  const int64_t groups = (int64_t)((a.keys + kRows - 1) / kRows) * a.kv_heads * a.batch;
+  if (groups < 1 || a.rows < 1) return 0;
+  const int64_t turns = (int64_t)((a.queries + kTile - 1) / kTile) * a.group;  // of a workgroup, at most
+  const bool few = few_groups(a, a.keys);
+  const int64_t want = few || a.causal ? 1024 : 512;
+  const int64_t parts = std::min((want + groups - 1) / groups, turns / (few ? 16 : 64));
+  return parts >= (few ? 8 : 2) ? (int32_t)parts : 0;
+}
 
 hipError_t launch_attention_grad(const AttentionArgs& a, hipStream_t s) {
   if (a.bf16)

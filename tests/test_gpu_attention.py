@@ -73,6 +73,28 @@ def test_shapes(shape, causal, types):
 
 
 @pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("causal", [False, True], ids=["full", "causal"])
+@pytest.mark.parametrize("shape", [(1, 1030, 1050, 8, 1, 64), (2, 260, 100, 32, 1, 40), (1, 530, 270, 16, 1, 128), (1, 300, 290, 48, 2, 96),
+                                   (512, 33, 20, 64, 1, 16)], ids=lambda s: "x".join(map(str, s)))
+def test_many_rows_for_few_keys(shape, causal, types):
+    """dk and dv in parts of the rows, of key heads that many query heads share."""
+    print(f"[attention] many rows {shape} causal {causal} {types}", flush=True)
+    given = inputs(*shape, TYPES[types], seed=sum(shape))
+    first = check_all(*given, causal=causal)
+    again = run(*given, causal=causal)
+    assert all(torch.equal(a, b) for a, b in zip(first, again))
+    if 1 < shape[0] < 100:
+        check_all(*given, causal=causal, lengths=some_lengths(shape[0], shape[2]))
+    # gradients at strides
+    q, k, v, dout = given
+    if shape[2] > 1:
+        k1 = torch.cat((k, k), 1)[:, ::2]
+        got = run(q, k1, v, dout, causal=causal)
+        want = run(q, k1.contiguous(), v, dout, causal=causal)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("types", TYPES)
 @pytest.mark.parametrize("scale", [1e-3, 0.3, 4.0])
 def test_scales(scale, types):
     """From even probabilities to ones of a single key."""
