@@ -8,7 +8,9 @@ again.  Query heads may share key heads.  A batch of single queries over long
 keys (generation) and prompts go through the same call.
 
 Tensors are float32 or bfloat16 on a ROCm device, the dim a multiple of 8 up to
-128.  Work is queued on torch's current stream.
+128.  Work is queued on torch's current stream.  A backward pass can be captured
+into a graph together with its forward pass; as with torch's own operators no
+eager graph of the same leaves may be alive then.
 """
 from __future__ import annotations
 

@@ -5,7 +5,9 @@
 input is float32 or bfloat16 on a ROCm device, weight and bias are of one of
 these dtypes too, the input's or the other (float32 weights of bfloat16
 activations).  Rows at one stride are read where they lie; any other layout is
-copied first.  Work is queued on torch's current stream.
+copied first.  Work is queued on torch's current stream.  A backward pass can be
+captured into a graph together with its forward pass; as with torch's own
+operators no eager graph of the same leaves may be alive then.
 """
 from __future__ import annotations
 
