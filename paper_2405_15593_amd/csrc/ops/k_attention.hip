@@ -161,7 +161,7 @@ __global__ __launch_bounds__(kThreads, BF16 || D <= 64 ? 2 : 1) void attention_k
   __shared__ __align__(16) uint8_t lds[2][2][T::kBytes];  // [turn][keys, values]
   const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
   const int tiles = (a.rows + kRows - 1) / kRows;
-  const Work work = work_of(blockIdx.x, a.kv_heads * a.batch);
+  const Work work = work_of(blockIdx.x, gridDim.x, a.kv_heads * a.batch);
   const int tile = tiles - 1 - work.order, head_of = work.head;  // (the last rows see the most keys)
   const typename T::Lane places(lane);
   const int kv_head = head_of % a.kv_heads, batch = head_of / a.kv_heads;
@@ -244,7 +244,7 @@ __global__ __launch_bounds__(kThreads, BF16 || D <= 64 ? 2 : 1) void attention_f
     block /= a.parts;
   }
   const int tiles = (a.rows + kFewRows - 1) / kFewRows;
-  const Work work = work_of(block, a.kv_heads * a.batch);
+  const Work work = work_of(block, gridDim.x / (a.parts ? a.parts : 1), a.kv_heads * a.batch);
   const int tile = tiles - 1 - work.order, head_of = work.head;  // (the last rows see the most keys)
   const int kv_head = head_of % a.kv_heads, batch = head_of / a.kv_heads;
   const int length = keys_of(a, batch);

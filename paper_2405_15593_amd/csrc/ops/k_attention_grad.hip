@@ -64,7 +64,7 @@ __global__ __launch_bounds__(kThreads, (BF16 && !SPLIT) || D <= 64 ? 2 : 1) void
   const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
   const int stager = SPLIT ? lane : (int)threadIdx.x;
   const int tiles = (a.rows + own_rows - 1) / own_rows;
-  const Work work = work_of(blockIdx.x, a.kv_heads * a.batch);
+  const Work work = work_of(blockIdx.x, gridDim.x, a.kv_heads * a.batch);
   const int tile = tiles - 1 - work.order, head_of = work.head;  // (the last rows see the most keys)
   const typename T::Lane places(lane);
   const int kv_head = head_of % a.kv_heads, batch = head_of / a.kv_heads;
@@ -231,7 +231,7 @@ __global__ __launch_bounds__(kThreads, (BF16 && !SPLIT) || D <= 64 ? 2 : 1) void
   };
   const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), h = lane >> 5;
   const int parts = !SPLIT && a.grad_parts ? a.grad_parts : 1;
-  const Work work = work_of(blockIdx.x, a.kv_heads * a.batch * parts);
+  const Work work = work_of(blockIdx.x, gridDim.x, a.kv_heads * a.batch * parts);
   const int tile = work.order, head_of = work.head / parts;  // (the first keys are seen by the most rows)
   const int part = work.head - head_of * parts;
   const typename T::Lane places(lane);
