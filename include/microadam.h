@@ -507,8 +507,8 @@ int microadam_token_logprobs_grad(const microadam_logits* logits, const float* g
  * Nothing is allocated on the device: the workspace (8-byte aligned, of any
  * content; microadam_clip_workspace says how many bytes) belongs to the caller
  * and is in use until the queued work is done.  The three arrays are read
- * before the call returns.  A list takes 2 launches, and one (clipping: two)
- * more for every further 160 gradients.
+ * before the call returns.  A list takes 2 launches (clipping more than 256 MiB:
+ * 3), and one (clipping: two) more for every further 160 gradients.
  */
 int microadam_clip_workspace(uint64_t* bytes);
 

@@ -18,7 +18,7 @@ using namespace microadam;
 
 namespace {
 
-constexpr uint64_t kWorkspace = (uint64_t)kClipSlots * sizeof(double);
+constexpr uint64_t kWorkspace = (uint64_t)(kClipSlots + 1) * sizeof(double);
 // The last-level cache's 256 MiB: beyond it reads past the caches take 549 instead
 // of 652 us for 3.8 GB, and the scaling 1440 instead of 1510; a list of 53 MB is
 // scaled in 21 instead of 18 us.
@@ -121,10 +121,10 @@ int queue(const void* const* grads, const int64_t* numels, const int32_t* dtypes
     if ((e = launch_square_sums(a, s)) != hipSuccess) return report_hip(e, "launching the sums of squares");
     a.add = 1;
   } while (i < n);
-  if (!scale) {
+  if (!scale || a.past) {
     a.norm = norm;
     if ((e = launch_grad_norm(a, s)) != hipSuccess) return report_hip(e, "launching the norm");
-    return MICROADAM_OK;
+    if (!scale) return MICROADAM_OK;
   }
   // the last launch's tensors first, as they were read last
   for (size_t k = starts.size(); k-- > 0;) {

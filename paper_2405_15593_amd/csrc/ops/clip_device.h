@@ -7,9 +7,9 @@
 namespace microadam {
 
 constexpr int kClipTensors = 160;             // of a launch, whose table is a kernel argument
-constexpr int kClipSlots = 2048;              // partial sums: workgroups of a launch, at most
+constexpr int kClipSlots = 1024;              // partial sums: workgroups of a launch, at most
 constexpr int64_t kClipChunk = 32768;         // bytes that a workgroup takes at a time
-constexpr int64_t kClipMost = (int64_t)1 << 30;  // chunks of a launch
+constexpr int64_t kClipMost = (int64_t)1 << 29;  // chunks of a launch
 
 struct ClipArgs {
   // A tensor's address, with bit 0 set for bfloat16 (an address is even), its
@@ -19,7 +19,7 @@ struct ClipArgs {
   uint64_t end[kClipTensors];
   int32_t first[kClipTensors + 1];
   int32_t n;
-  double* partial;  // kClipSlots
+  double* partial;  // kClipSlots, then the norm where `past`
   int32_t slots;    // in use
   int32_t past;     // the whole list is more than the caches hold
   int32_t add;      // to what an earlier launch of the call left there

@@ -7,12 +7,13 @@
 // keeps its sum of squares in binary64, which neither tiny nor huge gradients
 // leave, and writes one partial sum.  Every workgroup of the scaling pass adds
 // the partial sums itself, in one fixed order, so that no launch stands between
-// and the same list gives the same bits.  The scaling takes the chunks from the
+// and the same list gives the same bits; of a list past the caches, whose
+// workgroups are many, a kernel before it does.  The scaling takes the chunks from the
 // last to the first: what the norm read last is still in the cache.  Where the
 // factor is 1 nothing is written.
 //
-// The bound is memory.  1.9e9 bfloat16 gradients (3.8 GB): the sum 545 us (6.9
-// TB/s), the scaling 1412 (5.3 TB/s, read and written).  A list of 53 MB, which the
+// The bound is memory.  1.9e9 bfloat16 gradients (3.8 GB): the sum 540 us (6.9
+// TB/s), the scaling 1325 (5.7 TB/s, read and written).  A list of 53 MB, which the
 // last-level cache holds: 13 and 20 us; one of 15 MB: 6 us and 2 for the norm.
 #include "clip_device.h"
 #include "elements.h"
@@ -21,7 +22,14 @@ namespace microadam {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kScaleGroups = 4096;  // workgroups of the scaling pass, at most
+// Workgroups of the scaling pass, at most, and the parts of a chunk that they take
+// one each, of a list past the caches: 3.8 GB clipped / below the limit 1870 / 565 us.
+// (More would cost what is not clipped: one workgroup a part 1813 / 599, 4096 that
+// take chunk after chunk 1960 / 561.  Within the caches halves cost 105 MB 33
+// instead of 31 us.)
+constexpr int kScaleGroups = 1 << 16;
+template <bool PAST>
+constexpr int kScaleParts = PAST ? 2 : 1;
 constexpr int kPieces = (int)(kClipChunk / 16 / kThreads);  // a thread's, of a chunk
 
 __device__ inline double wave_sum(double x) {
@@ -140,7 +148,9 @@ __device__ inline double norm_of(const ClipArgs& a) {
 
 __global__ __launch_bounds__(kThreads) void grad_norm_kernel(const ClipArgs a) {
   const double norm = norm_of(a);
-  if (threadIdx.x == 0) *a.norm = (float)norm;
+  if (threadIdx.x) return;
+  *a.norm = (float)norm;
+  a.partial[kClipSlots] = norm;
 }
 
 // (the product in binary64: a factor below binary32's normal range, of
@@ -157,19 +167,20 @@ __device__ inline uint4v scale_piece(const uint4v& q, double c) {
 }
 
 template <bool BF16, bool PAST>
-__device__ inline void scale_chunk(uint64_t from, uint64_t at, uint64_t end, double c) {
+__device__ inline void scale_part(uint64_t from, uint64_t at, uint64_t end, double c) {
   typedef Elements<BF16> E;
-  if (from >= at && from + kClipChunk <= end) {
+  constexpr int kBytes = (int)kClipChunk / kScaleParts<PAST>, kOwn = kBytes / 16 / kThreads;
+  if (from >= at && from + kBytes <= end) {
     uint4v* p = (uint4v*)from;
-    uint4v q[kPieces];
+    uint4v q[kOwn];
 #pragma unroll
-    for (int i = 0; i < kPieces; ++i) q[i] = load_piece<PAST>(p + i * kThreads + threadIdx.x);
+    for (int i = 0; i < kOwn; ++i) q[i] = load_piece<PAST>(p + i * kThreads + threadIdx.x);
 #pragma unroll
-    for (int i = 0; i < kPieces; ++i)
+    for (int i = 0; i < kOwn; ++i)
       store_piece<PAST>(p + i * kThreads + threadIdx.x, scale_piece<BF16>(q[i], c));
     return;
   }
-  for (int i = threadIdx.x; i < (int)(kClipChunk / 16); i += kThreads) {
+  for (int i = threadIdx.x; i < kBytes / 16; i += kThreads) {
     const uint64_t p = from + (uint64_t)i * 16;
     if (p >= end) break;
     if (p >= at && p + 16 <= end)
@@ -181,19 +192,20 @@ __device__ inline void scale_chunk(uint64_t from, uint64_t at, uint64_t end, dou
 
 template <bool PAST>
 __global__ __launch_bounds__(kThreads) void scale_grads_kernel(const ClipArgs a) {
-  const double norm = norm_of(a);
-  if (a.norm && blockIdx.x == 0 && threadIdx.x == 0) *a.norm = (float)norm;
+  const double norm = PAST ? a.partial[kClipSlots] : norm_of(a);
+  if (!PAST && a.norm && blockIdx.x == 0 && threadIdx.x == 0) *a.norm = (float)norm;
   if (norm + a.eps <= a.max_norm) return;
   const double c = a.max_norm / (norm + a.eps);  // NaN of a NaN norm
-  for (int k = a.first[a.n] - 1 - (int)blockIdx.x; k >= 0; k -= (int)gridDim.x) {
-    const int t = tensor_of(a, k);
+  constexpr int parts = kScaleParts<PAST>;
+  for (int k = a.first[a.n] * parts - 1 - (int)blockIdx.x; k >= 0; k -= (int)gridDim.x) {
+    const int t = tensor_of(a, k / parts);
     const bool bf16 = a.at[t] & 1;
     const uint64_t at = a.at[t] & ~(uint64_t)1, end = a.end[t];
-    const uint64_t from = (at & ~(uint64_t)15) + (uint64_t)(k - a.first[t]) * kClipChunk;
+    const uint64_t from = (at & ~(uint64_t)15) + (uint64_t)(k - a.first[t] * parts) * (kClipChunk / parts);
     if (bf16)
-      scale_chunk<true, PAST>(from, at, end, c);
+      scale_part<true, PAST>(from, at, end, c);
     else
-      scale_chunk<false, PAST>(from, at, end, c);
+      scale_part<false, PAST>(from, at, end, c);
   }
 }
 
@@ -212,12 +224,18 @@ hipError_t launch_grad_norm(const ClipArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
+template <bool PAST>
+static void scale_grads(const ClipArgs& a, hipStream_t s) {
+  const int64_t parts = (int64_t)a.first[a.n] * kScaleParts<PAST>;
+  const int grid = parts < 1 ? 1 : parts < kScaleGroups ? (int)parts : kScaleGroups;
+  scale_grads_kernel<PAST><<<dim3(grid), dim3(kThreads), 0, s>>>(a);
+}
+
 hipError_t launch_scale_grads(const ClipArgs& a, hipStream_t s) {
-  const int chunks = a.first[a.n], grid = chunks < 1 ? 1 : chunks < kScaleGroups ? chunks : kScaleGroups;
   if (a.past)
-    scale_grads_kernel<true><<<dim3(grid), dim3(kThreads), 0, s>>>(a);
+    scale_grads<true>(a, s);
   else
-    scale_grads_kernel<false><<<dim3(grid), dim3(kThreads), 0, s>>>(a);
+    scale_grads<false>(a, s);
   return hipGetLastError();
 }
 

@@ -78,6 +78,34 @@ def test_lists(name, start, dtype):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+def test_beyond_the_caches(dtype):
+    """More than 256 MiB, tensors of all ends among them; above the limit and below."""
+    print(f"[clip] beyond the caches {dtype}", flush=True)
+    wide = 9001 if dtype == torch.float32 else 18001
+    flat, grads = bucket([(3,), (8009, wide), (8193,), (1,), (16385,), (40000, 7)], dtype, start=1)
+    before, whole = [g.clone() for g in grads], flat.clone()
+    want = math.sqrt(sum(float(g.double().square().sum()) for g in grads))
+    check_norm(grad_norm(grads), want)
+    check_norm(clip_grads(grads, 2.0 * want), want)
+    assert torch.equal(flat, whole)
+    check_norm(clip_grads(grads, 0.37 * want), want)
+    factor = 0.37 * want / (want + 1e-6)
+    for a, b in zip(grads, before):
+        for x, y in zip(a.reshape(-1).split(1 << 24), b.reshape(-1).split(1 << 24)):
+            exact = y.double() * factor
+            floor = {torch.float32: 2.0 ** -150, torch.bfloat16: 2.0 ** -134}[dtype]
+            assert bool(((x.double() - exact).abs() <= exact.abs() * HALF[dtype] * SLACK + floor).all())
+    assert torch.equal(flat[:1], whole[:1]) and torch.equal(flat[-5:], whole[-5:])
+    again = whole.clone()
+    views, at = [], 1
+    for g in before:
+        views.append(again[at:at + g.numel()].view(g.shape))
+        at += g.numel()
+    clip_grads(views, 0.37 * want)
+    assert torch.equal(again, flat)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
 def test_more_than_the_caches_hold(dtype):
     """A list of 300 MB, in binary64 on the device."""
     print(f"[clip] 300 MB {dtype}", flush=True)
