@@ -41,13 +41,20 @@ constexpr int kMostParts = 256;
 // Whether 128 rows (or keys) to a workgroup are too few workgroups for 256 CUs, so
 // that its four waves had better share 32 of them and take every fourth tile of
 // the others.  One workgroup to a CU, two for binary32, whose matrix instructions
-// leave no time over.  Forward / backward in us, shared or not:
+// leave no time over, and some more for causal ones of short rows and many keys, of
+// which the longest would be waited for.  Forward / backward in us, shared or not:
 //   bfloat16  1 x 2048 x 8 heads of 128, causal  128 workgroups  26 / 81   47 / 159
 //             2 x  512 x 32           "          256             23 / 94   20 / 56
 //   binary32  4 x 1024 x 8 heads of 64, causal   256             54 / 193  86 / 267
 //             32 x 512 x 4            "          512             64 / 257  60 / 196
+//   bfloat16  1 x 2048 x 16 heads of 64, causal  256             26 / 64   33 / 102
+//             1 x 4096 x 10           "          320             52 / 128  62 / 159
+//             3 x 1024 x 16           "          384             23 / 65   22 / 62
+//             4 x  512 x 16           "          256             16 / 36   13 / 36
 inline bool few_groups(const AttentionArgs& a, int positions) {
-  return (int64_t)((positions + 127) / 128) * a.kv_heads * a.batch < (a.bf16 ? 256 : 512);
+  const bool uneven = a.causal && a.dim <= 64 && a.keys >= 1024 && a.queries >= a.keys / 2;
+  const int enough = !a.bf16 ? 512 : uneven ? 321 : 256;
+  return (int64_t)((positions + 127) / 128) * a.kv_heads * a.batch < enough;
 }
 
 // Whether the rows go to the kernel without matrix products.

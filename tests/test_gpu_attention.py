@@ -94,6 +94,14 @@ def test_many_rows_for_few_keys(shape, causal, types):
         assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
+@pytest.mark.parametrize("dim", [24, 64])
+def test_causal_of_many_lengths(dim):
+    """Workgroups of causal rows that are shared, or go from short to long."""
+    print(f"[attention] causal of many lengths {dim}", flush=True)
+    check_all(*inputs(1, 1030, 1030, 30, 30, dim, torch.bfloat16), causal=True)
+    check_all(*inputs(3, 520, 500, 32, 32, dim, torch.bfloat16), causal=True)
+
+
 @pytest.mark.parametrize("types", TYPES)
 @pytest.mark.parametrize("scale", [1e-3, 0.3, 4.0])
 def test_scales(scale, types):
