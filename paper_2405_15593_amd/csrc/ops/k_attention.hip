@@ -410,7 +410,15 @@ __global__ __launch_bounds__(WAVES == 1 ? kThreads : 64 * WAVES) void attention_
   if (a.lse && lane == 0) a.lse[stat] = sum == 0.0f ? infinity() : top + __builtin_amdgcn_logf(sum);
 }
 
-bool few_rows(const AttentionArgs& a) { return a.rows <= kFewRows || few_groups(a, a.rows); }
+// Whether the rows go to attention_few_kernel: besides few_groups' rule causal ones
+// of many keys whatever the head's size (bfloat16, shared or not, us: 16 heads of 96,
+// 2048 keys, 256 workgroups 32 / 44; 4 of 128, 8192 keys, 256 119 / 161; 10 of 128,
+// 4096 keys, 320 82 / 88; 12 of 128, 4096 keys, 384 93 / 89).
+bool few_rows(const AttentionArgs& a) {
+  const int64_t groups = (int64_t)((a.rows + kRows - 1) / kRows) * a.kv_heads * a.batch;
+  const bool uneven = a.bf16 && a.causal && a.keys >= 2048 && a.queries >= a.keys / 2;
+  return a.rows <= kFewRows || few_groups(a, a.rows) || (uneven && groups <= 320);
+}
 
 template <bool BF16, int D>
 void launch_rows(const AttentionArgs& a, hipStream_t s) {

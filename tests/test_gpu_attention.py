@@ -102,6 +102,18 @@ def test_causal_of_many_lengths(dim):
     check_all(*inputs(3, 520, 500, 32, 32, dim, torch.bfloat16), causal=True)
 
 
+def test_long_causal_prompts():
+    """Some of the heads: the others' binary64 scores would take gibibytes."""
+    print("[attention] long causal prompts", flush=True)
+    q, k, v, dout = inputs(1, 2100, 2150, 16, 16, 128, torch.bfloat16)
+    got = run(q, k, v, dout, causal=True)
+    plain = attention(q, k, v, causal=True)
+    some = [0, 7, 15]
+    want = reference(*(t[:, :, some] for t in (q, k, v, dout)), True, None, 128 ** -0.5, torch.bfloat16)
+    check([t[:, :, some] for t in got], *want, torch.bfloat16)
+    assert torch.equal(plain, got[0])
+
+
 @pytest.mark.parametrize("types", TYPES)
 @pytest.mark.parametrize("scale", [1e-3, 0.3, 4.0])
 def test_scales(scale, types):
