@@ -10,7 +10,9 @@ keys (generation) and prompts go through the same call.
 Tensors are float32 or bfloat16 on a ROCm device, the dim a multiple of 8 up to
 128.  Work is queued on torch's current stream.  A backward pass can be captured
 into a graph together with its forward pass; as with torch's own operators no
-eager graph of the same leaves may be alive then.
+eager graph of the same leaves may be alive then.  Tracers that record torch's own
+operators (torch.jit.trace, make_fx) are refused; torch.compile calls it between
+its graphs.
 """
 from __future__ import annotations
 

@@ -7,7 +7,8 @@ themselves.  The norm stays on the device: nothing waits for it.
 
 Gradients are float32 or bfloat16 on one ROCm device, mixed as they come, of
 any shape, without gaps or overlaps in memory.  Work is queued on torch's
-current stream.
+current stream.  Tracers that record torch's own operators (torch.jit.trace,
+make_fx) are refused.
 """
 from __future__ import annotations
 

@@ -8,8 +8,11 @@
 // 3.7, forward and backward 100 / 64 (of which torch.autograd.grad around an empty
 // function is some 45), attention likewise 105 / 63, the norm of a small model's
 // gradients 23 / 10.
+#include <c10/core/impl/LocalDispatchKeySet.h>
+#include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/custom_function.h>
+#include <torch/csrc/jit/frontend/tracer.h>
 #include <torch/csrc/utils/pybind.h>
 
 #include <algorithm>
@@ -63,6 +66,24 @@ void refuse_tangent(const Tensor& t, const char* what) {
   if (t.defined() && t._fw_grad(0).defined()) not_implemented(std::string(what) + ": no derivatives in forward mode");
 }
 
+// Whether a graph of torch's operators is being recorded (torch.jit.trace, make_fx
+// and torch.export).  It would hold the allocations made here and none of the
+// launches: a function that returns memory that nothing wrote.  Other dispatch modes
+// only watch.
+bool is_traced() {
+  return torch::jit::tracer::isTracing() || c10::impl::tls_is_dispatch_key_included(c10::DispatchKey::PreDispatch) ||
+         c10::impl::TorchDispatchModeTLS::get_mode(c10::impl::TorchDispatchModeKey::PROXY).has_value();
+}
+
+void refuse_trace(const char* what) {
+  if (is_traced()) not_implemented(std::string(what) + ": not recorded by torch's tracers");
+}
+
+// ... of a backward pass, whose forward pass was not recorded.
+void refuse_trace_here(const char* what) {
+  TORCH_CHECK_NOT_IMPLEMENTED(!is_traced(), what, ": the backward pass is not recorded by torch's tracers");
+}
+
 typedef std::optional<Tensor> Perhaps;  // (autograd's functions take a tensor that is not there as none at all)
 Perhaps perhaps(const Tensor& t) { return t.defined() ? Perhaps(t) : Perhaps(); }
 Tensor given(const Perhaps& t) { return t.value_or(Tensor()); }
@@ -114,6 +135,7 @@ bool is_dense(const Tensor& t) {
 
 Tensor clip(const char* what, const std::vector<Tensor>& grads, bool scale, double max_norm, double eps,
             const Perhaps& workspace) {
+  refuse_trace(what);
   if (grads.empty()) throw py::value_error("grads: at least one tensor");
   const Tensor& first = grads[0];
   const bool grad_mode = c10::GradMode::is_enabled();
@@ -230,6 +252,7 @@ class LayerNorm : public torch::autograd::Function<LayerNorm> {
   }
 
   static variable_list backward(AutogradContext* ctx, const variable_list& grads) {
+    refuse_trace_here("layer_norm");
     variable_list result(4);
     {
       const c10::AutoGradMode off(false);
@@ -261,6 +284,7 @@ class LayerNorm : public torch::autograd::Function<LayerNorm> {
 
 Tensor layer_norm(const Tensor& x, const Perhaps& given_weight, const Perhaps& given_bias, double eps) {
   const Tensor weight = given(given_weight), bias = given(given_bias);
+  refuse_trace("layer_norm");
   for (const Tensor* t : {&x, &weight, &bias}) refuse_tangent(*t, "layer_norm");
   check_dtype(x, "x");
   if (!x.is_cuda()) throw py::value_error("x: a tensor on a ROCm device");
@@ -325,6 +349,7 @@ class Attention : public torch::autograd::Function<Attention> {
   }
 
   static variable_list backward(AutogradContext* ctx, const variable_list& grads) {
+    refuse_trace_here("attention");
     variable_list result(6);
     {
       const c10::AutoGradMode off(false);
@@ -349,6 +374,7 @@ class Attention : public torch::autograd::Function<Attention> {
 
 Tensor attention(const Tensor& q, const Tensor& k, const Tensor& v, bool causal, double scale,
                  const Perhaps& key_lengths) {
+  refuse_trace("attention");
   for (const Tensor* t : {&q, &k, &v}) refuse_tangent(*t, "attention");
   for (const auto& [t, what] : {std::pair<const Tensor&, const char*>{q, "q"}, {k, "k"}, {v, "v"}}) {
     check_dtype(t, what);

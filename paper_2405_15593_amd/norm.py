@@ -7,7 +7,9 @@ these dtypes too, the input's or the other (float32 weights of bfloat16
 activations).  Rows at one stride are read where they lie; any other layout is
 copied first.  Work is queued on torch's current stream.  A backward pass can be
 captured into a graph together with its forward pass; as with torch's own
-operators no eager graph of the same leaves may be alive then.
+operators no eager graph of the same leaves may be alive then.  Tracers that record
+torch's own operators (torch.jit.trace, make_fx) are refused; torch.compile calls it
+between its graphs.
 """
 from __future__ import annotations
 
