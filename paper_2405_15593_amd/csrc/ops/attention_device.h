@@ -43,14 +43,16 @@ constexpr int kMostParts = 256;
 // the others.  One workgroup to a CU, two for binary32, whose matrix instructions
 // leave no time over, and some more for causal ones of short rows and many keys, of
 // which the longest would be waited for.  Forward / backward in us, shared or not:
-//   bfloat16  1 x 2048 x 8 heads of 128, causal  128 workgroups  26 / 81   47 / 159
-//             2 x  512 x 32           "          256             23 / 94   20 / 56
+//   bfloat16  1 x 2048 x 8 heads of 128, causal  128 workgroups  29 / 117  48 / 163
+//             2 x  512 x 32           "          256             26 / 104  20 / 60
 //   binary32  4 x 1024 x 8 heads of 64, causal   256             54 / 193  86 / 267
 //             32 x 512 x 4            "          512             64 / 257  60 / 196
-//   bfloat16  1 x 2048 x 16 heads of 64, causal  256             26 / 64   33 / 102
-//             1 x 4096 x 10           "          320             52 / 128  62 / 159
-//             3 x 1024 x 16           "          384             23 / 65   22 / 62
-//             4 x  512 x 16           "          256             16 / 36   13 / 36
+//   bfloat16  1 x 2048 x 16 heads of 64, causal  256             30 / 77   35 / 103
+//             1 x 4096 x 10           "          320             59 / 160  63 / 162
+//             3 x 1024 x 16           "          384             25 / 72   22 / 64
+//             4 x  512 x 16           "          256             16 / 38   13 / 36
+// (Shared ones of bfloat16 multiply what the rounding of p and ds leaves over too, a
+// tenth of their time.)
 inline bool few_groups(const AttentionArgs& a, int positions) {
   const bool uneven = a.causal && a.dim <= 64 && a.keys >= 1024 && a.queries >= a.keys / 2;
   const int enough = !a.bf16 ? 512 : uneven ? 321 : 256;

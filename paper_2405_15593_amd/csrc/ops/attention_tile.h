@@ -101,6 +101,20 @@ __device__ inline Frag<BF16> as_frag(const float16v& d) {
   return f;
 }
 
+// What bfloat16's rounding of the same results left over, 2^-8 of each rounded in
+// turn: the two fragments together are 16 bits of a result.
+template <int HALF>
+__device__ inline Frag<true> rest_of(const float16v& d, const Frag<true>& rounded) {
+  const uint4v r = __builtin_bit_cast(uint4v, rounded.v);
+  uint4v q;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    q[i] = pack_bf16(d[8 * HALF + 2 * i] - __uint_as_float(r[i] << 16), d[8 * HALF + 2 * i + 1] - __uint_as_float(r[i] & 0xffff0000u));
+  Frag<true> f;
+  f.v = __builtin_bit_cast(bf16x8, q);
+  return f;
+}
+
 // Eight elements of memory, zeros where there are none.
 template <bool BF16>
 __device__ inline Frag<BF16> load_frag(const void* p, int64_t at, bool there) {

@@ -63,9 +63,19 @@ __device__ inline void mask(float16v (&s)[N], int first, int limit, int lane, fl
 // tiles pass without a factor for sum and output.  Each row decides for itself
 // (its factor is 1 where another row's is not), so that no row's bits go by its
 // neighbours.
+//
+// The matrix instruction takes p in bfloat16 where v is that.  WHOLE: what p's
+// rounding leaves over is multiplied too, so that p has 16 bits and out's own
+// rounding is the error that is left, 1.6e-3 of the result's norm instead of 2.1e-3
+// to 2.4e-3.  It is taken where a workgroup's waves share rows: one token's time
+// goes by memory (8 x 4096 keys 28.2 -> 28.7 us, 64 x 2048 83 -> 84), some hundred
+// rows' by the way of a tile (3 x 515 rows, 1031 keys of 80, 17.7 -> 20.3).  Full
+// workgroups of 128 rows, which the matrix cores bound, would take 360 -> 450 us for
+// 2 x 4096 tokens, 32 heads of 128, causal: there p is rounded, half a step, 2^-8 of
+// each, with random signs.
 constexpr float kAhead = 8.0f;
 
-template <bool BF16, int D, int KEYS>
+template <bool BF16, int D, int KEYS, bool WHOLE>
 __device__ inline void add_tile(float16v (&s)[KEYS / 32], const uint8_t* values,
                                 const typename Tile<BF16, D, KEYS>::Lane& at, float c, float& m, float& l,
                                 float16v (&out)[D / 32]) {
@@ -110,6 +120,14 @@ __device__ inline void add_tile(float16v (&s)[KEYS / 32], const uint8_t* values,
     for (int part = 0; part < parts; ++part) {
       multiply(out[part], v[2 * part], p0);
       multiply(out[part], v[2 * part + 1], p1);
+    }
+    if constexpr (BF16 && WHOLE) {
+      const Frag<true> r0 = rest_of<0>(s[i], p0), r1 = rest_of<1>(s[i], p1);
+#pragma unroll
+      for (int part = 0; part < parts; ++part) {
+        multiply(out[part], v[2 * part], r0);
+        multiply(out[part], v[2 * part + 1], r1);
+      }
     }
     if (i + 1 < n) {
       read(i + 1);
@@ -215,7 +233,7 @@ __global__ __launch_bounds__(kThreads, BF16 || D <= 64 ? 2 : 1) void attention_k
       float16v s[keys / 32];
       scores<BF16, D, keys>(s, lds[turn & 1][0], places, q);
       if (first + keys > least) mask(s, first, limit, lane, -infinity());
-      add_tile<BF16, D, keys>(s, lds[turn & 1][1], places, a.c, m, l, out);
+      add_tile<BF16, D, keys, false>(s, lds[turn & 1][1], places, a.c, m, l, out);
     }
     if (turn + 1 < turns) store(turn + 1);
     __syncthreads();
@@ -292,7 +310,7 @@ __global__ __launch_bounds__(kThreads, BF16 || D <= 64 ? 2 : 1) void attention_f
     float16v s[1];
     scores<BF16, D, kFewKeys>(s, keys, places, q);
     if (first + kFewKeys > least) mask(s, first, limit, lane, -infinity());
-    add_tile<BF16, D, kFewKeys>(s, values, places, a.c, m, l, out);
+    add_tile<BF16, D, kFewKeys, true>(s, values, places, a.c, m, l, out);
     wave_order();
   }
   l = add_halves(l);
@@ -412,12 +430,12 @@ __global__ __launch_bounds__(WAVES == 1 ? kThreads : 64 * WAVES) void attention_
 
 // Whether the rows go to attention_few_kernel: besides few_groups' rule causal ones
 // of many keys whatever the head's size (bfloat16, shared or not, us: 16 heads of 96,
-// 2048 keys, 256 workgroups 32 / 44; 4 of 128, 8192 keys, 256 119 / 161; 10 of 128,
-// 4096 keys, 320 82 / 88; 12 of 128, 4096 keys, 384 93 / 89).
+// 2048 keys, 256 workgroups 38 / 45; 4 of 128, 8192 keys, 256 148 / 164; 10 of 128,
+// 4096 keys, 320 98 / 90; 12 of 128, 4096 keys, 384 110 / 91).
 bool few_rows(const AttentionArgs& a) {
   const int64_t groups = (int64_t)((a.rows + kRows - 1) / kRows) * a.kv_heads * a.batch;
   const bool uneven = a.bf16 && a.causal && a.keys >= 2048 && a.queries >= a.keys / 2;
-  return a.rows <= kFewRows || few_groups(a, a.rows) || (uneven && groups <= 320);
+  return a.rows <= kFewRows || few_groups(a, a.rows) || (uneven && groups <= 256);
 }
 
 template <bool BF16, int D>

@@ -11,8 +11,14 @@
 // keys (split into parts that a third kernel joins where the keys' workgroups are
 // few).  Seven products where one kernel with shared sums would take five.
 //
-// p and ds are rounded to bfloat16 before their products with bfloat16 operands
-// (half a step, 2^-8 of each); their sums are binary32.
+// The matrix instruction takes p and ds in bfloat16 where the operands are that;
+// their sums are binary32.  Where a workgroup's waves share rows or keys (SPLIT),
+// what the rounding leaves over is multiplied too: p and ds have 16 bits, and the
+// results' own rounding is the error that is left, 1.65e-3 of their norm instead of
+// 2.35e-3 (both kernels, 3 x 515 rows, 1031 keys of 80: 56 -> 62 us).  Full workgroups,
+// which the matrix cores bound, would take 1010 -> 1590 us for 2 x 4096 tokens, 32
+// heads of 128, causal (dk and dv of 128 elements spill 120 bytes a lane): there p and
+// ds are rounded, half a step, 2^-8 of each, with random signs.
 //
 // The bound is the matrix cores beside the vector work: 2 sequences of 4096 tokens,
 // 32 heads of 128, causal, bfloat16 take 423 to 472 and 542 to 619 us (890 to 1010
@@ -167,6 +173,14 @@ __global__ __launch_bounds__(kThreads, (BF16 && !SPLIT) || D <= 64 ? 2 : 1) void
       for (int part = 0; part < D / 32; ++part) {
         multiply(dq[part], across[2 * part], d0);
         multiply(dq[part], across[2 * part + 1], d1);
+      }
+      if constexpr (BF16 && SPLIT) {
+        const Frag<true> r0 = rest_of<0>(s, d0), r1 = rest_of<1>(s, d1);
+#pragma unroll
+        for (int part = 0; part < D / 32; ++part) {
+          multiply(dq[part], across[2 * part], r0);
+          multiply(dq[part], across[2 * part + 1], r1);
+        }
       }
     } else if (kLate) {
       more();
@@ -352,7 +366,25 @@ __global__ __launch_bounds__(kThreads, (BF16 && !SPLIT) || D <= 64 ? 2 : 1) void
     }
     const Frag<BF16> p0 = as_frag<BF16, 0>(s), p1 = as_frag<BF16, 1>(s);
     const Frag<BF16> d0 = as_frag<BF16, 0>(dp), d1 = as_frag<BF16, 1>(dp);
-    if (BF16) {
+    if constexpr (BF16 && SPLIT) {
+      schedule_here();
+#pragma unroll
+      for (int i = kAhead; i < D / 16; ++i) across[i] = T::across(douts, places, 16 * (i % 2), i / 2);
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) multiply(dv[i / 2], across[i], i % 2 ? p1 : p0);
+      schedule_here();
+      const Frag<BF16> pr0 = rest_of<0>(s, p0), pr1 = rest_of<1>(s, p1);
+      const Frag<BF16> dr0 = rest_of<0>(dp, d0), dr1 = rest_of<1>(dp, d1);
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) multiply(dv[i / 2], across[i], i % 2 ? pr1 : pr0);
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) across[i] = T::across(queries, places, 16 * (i % 2), i / 2);
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) multiply(dk[i / 2], across[i], i % 2 ? d1 : d0);
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) multiply(dk[i / 2], across[i], i % 2 ? dr1 : dr0);
+      schedule_here();
+    } else if (BF16) {
       schedule_here();
 #pragma unroll
       for (int i = kAhead; i < D / 16; ++i) across[i] = T::across(douts, places, 16 * (i % 2), i / 2);
