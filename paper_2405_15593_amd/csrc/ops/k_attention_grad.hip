@@ -272,14 +272,17 @@ __global__ __launch_bounds__(kThreads, (BF16 && !SPLIT) || D <= 64 ? 2 : 1) void
     all.store(values, threadIdx.x);
   }
 
-  // The query heads one after the other, each from the first tile of queries
-  // that see one of the workgroup's keys.
-  int from = 0;
+  // The query heads one after the other, each from the first tile of queries that
+  // see one of the workgroup's keys on.  The first tile of all begins with the first
+  // query that sees a key: the others are not read, whose p of zero would not take
+  // away a NaN.
+  int from = 0, origin = 0;
   if (a.causal) {
-    from = key0 - (a.keys - a.queries);
+    origin = a.queries > a.keys ? (a.queries - a.keys) % kTile : 0;
+    from = key0 - (a.keys - a.queries) - origin;
     from = (from < 0 ? 0 : from) / kTile;
   }
-  const int of_head = (a.queries + kTile - 1) / kTile - from;
+  const int of_head = (a.queries - origin + kTile - 1) / kTile - from;
   const int all = key0 < length && of_head > 0 ? of_head * a.group : 0;
   const int start = (int)((int64_t)part * all / parts), turns = (int)((int64_t)(part + 1) * all / parts);
 
@@ -291,7 +294,7 @@ __global__ __launch_bounds__(kThreads, (BF16 && !SPLIT) || D <= 64 ? 2 : 1) void
   next_do.start(a.dim, (int)do_pos, stager);
   auto load = [&](int turn) {
     const int of = uniform(turn / of_head), head = kv_head * a.group + of;
-    const int first = (from + turn - of * of_head) * kTile;
+    const int first = (from + turn - of * of_head) * kTile + origin;
     next_q.load((const uint8_t*)a.q.at + (batch * a.q.batch + head * a.q.head) * size, q_pos, a.dim, first, a.queries);
     next_do.load((const uint8_t*)a.dout.at + (batch * a.dout.batch + head * a.dout.head) * size, do_pos, a.dim, first,
                  a.queries);
@@ -345,8 +348,8 @@ __global__ __launch_bounds__(kThreads, (BF16 && !SPLIT) || D <= 64 ? 2 : 1) void
       for (int i = 0; i < 4; ++i) s[4 * g + i] = exp2_fast(__builtin_fmaf(s[4 * g + i], a.c, -lse[i]));
     }
     // the tile's first query does not see the wave's last key
-    const int in_head = from + turn - uniform(turn / of_head) * of_head;
-    const int hidden = wave_key + 31 - (in_head * kTile + a.keys - a.queries);
+    const int first = (from + turn - uniform(turn / of_head) * of_head) * kTile + origin;
+    const int hidden = wave_key + 31 - (first + a.keys - a.queries);
     if (a.causal && hidden > 0) {
       const int at = (lane & 31) - 31 + hidden - 4 * h;  // rows below it do not see the lane's key
 #pragma unroll
@@ -359,7 +362,7 @@ __global__ __launch_bounds__(kThreads, (BF16 && !SPLIT) || D <= 64 ? 2 : 1) void
       for (int i = 0; i < 4; ++i) dp[4 * g + i] = s[4 * g + i] * (dp[4 * g + i] - delta[i]);
     }
     // queries that see one key (as in dq): with one in all, or the first that sees any
-    const int alone = a.queries - a.keys - in_head * kTile;
+    const int alone = a.queries - a.keys - first;
     if (length == 1 || (a.causal && wave_key == 0 && alone >= 0 && alone < kTile)) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) dp[r] = length == 1 || 8 * (r / 4) + 4 * h + r % 4 == alone ? 0.0f : dp[r];
