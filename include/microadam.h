@@ -539,6 +539,8 @@ int microadam_clip_grads(void* const* grads, const int64_t* numels, const int32_
  * in binary32 or more, y rounded once to x's dtype.  cols is at most 2^24, rows
  * at most 2^31, rows times ld at most 2^60; addresses are aligned to their
  * element type, and rows may start anywhere.  A row with NaN or an infinity gives NaN in its own y.
+ * The sums of x and of (x - m)^2 over a row stay in binary32's range (a result whose
+ * variance overflows is b, as with r = 0).
  */
 typedef struct microadam_rows {
   const void* x;
@@ -563,7 +565,9 @@ int microadam_layer_norm(const microadam_rows* rows, void* y, int64_t y_ld, floa
  * row), with g = dy w:
  *     dx = r (g - mean g - h mean(g h)),  dweight = sum dy h,  dbias = sum dy
  * (sums over the rows; zeros without rows), from the x, weight and eps of the
- * forward call and the mean and rstd that it wrote.  Each of dx, dweight and
+ * forward call and the mean and rstd that it wrote.  h is then taken with the mean
+ * as it was written, rounded to binary32: off by up to 2^-24 |m| r besides, where y
+ * keeps all bits.  Each of dx, dweight and
  * dbias may be NULL.  Sums are held in binary32, partly first per workgroup,
  * and joined in an order that goes by the sizes: the same call gives the same
  * bits.  The workspace (16-byte aligned, of any content;

@@ -7,11 +7,15 @@
 // A row stays in the registers of a group of threads (a wave, up to a whole
 // workgroup), so that x is read once forward, and x and dy once backward.  The
 // variance is summed from differences to the mean, and corrected by what they
-// sum to: a mean far from zero costs no bits.  Backward a group keeps its
-// columns' sums of dw and db in registers over all its rows; the groups of a
-// workgroup are joined in LDS, the workgroups' sums by a second kernel, each in
-// a fixed order.  Rows too long for registers are read once more per pass, and
-// their dw and db summed by columns.
+// sum to: forward a mean far from zero costs no bits.  Backward the mean comes
+// from memory, rounded to binary32, which moves a row's h by up to 2^-24 |m| r, less
+// than its other roundings while |m| r is below 64.  (Summing the differences again
+// and taking their mean from h: 3 to 8% of the backward pass, and rows above 8192
+// elements spill, 82 -> 264 us for 4096 x 16384.)  Backward a group keeps its columns'
+// sums of dw and db in registers over all its rows; the groups of a workgroup are
+// joined in LDS, the workgroups' sums by a second kernel, each in a fixed order.
+// Rows too long for registers are read once more per pass, and their dw and db
+// summed by columns.
 //
 // The bound is memory.  16384 x 4096 bfloat16, forward and backward in turn: 125 us
 // (5.4 TB/s), 49 of them forward, 4 to 5 the join.  Small matrices take a row's own

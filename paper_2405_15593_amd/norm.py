@@ -24,6 +24,8 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opt
                eps: float = 1e-5) -> torch.Tensor:
     """Rows (the last dimension) of ``x`` with their mean taken off, divided by
     the root of their variance plus ``eps``, times ``weight``, plus ``bias``; of
-    x's shape and dtype.  There is no derivative of the backward pass, nor one
-    in forward mode."""
+    x's shape and dtype.  The backward pass takes the mean as it was saved, rounded
+    to float32: of rows whose mean lies more than some 64 standard deviations from
+    zero gradients have fewer bits than the result.  There is no derivative of the
+    backward pass, nor one in forward mode."""
     return operators().layer_norm(x, weight, bias, eps)
