@@ -104,13 +104,13 @@ int queue(const void* const* grads, const int64_t* numels, const int32_t* dtypes
   a.max_norm = max_norm;
   a.eps = eps;
   // one number of slots for all launches of the call
-  int64_t most = 1, chunks = 0;
+  int64_t most = 1, bytes = 0;  // (bytes: a small gradient's chunk is nearly empty)
   for (int32_t i = 0; i < n;) {
     i = fill(a, grads, numels, dtypes, n, i);
-    chunks += a.first[a.n];
+    for (int32_t k = 0; k < a.n; ++k) bytes += (int64_t)(a.end[k] - (a.at[k] & ~(uint64_t)1));
     most = std::max(most, (int64_t)a.first[a.n]);
   }
-  a.past = chunks > kCached / kClipChunk ? 1 : 0;
+  a.past = bytes > kCached ? 1 : 0;
   a.slots = (int32_t)std::min<int64_t>(kClipSlots, most);
   hipError_t e;
   std::vector<int32_t> starts;
