@@ -599,10 +599,10 @@ int microadam_layer_norm_grad(const microadam_rows* rows, const float* mean, con
  * operands are multiplied in binary32.  With bfloat16 operands p and the scores'
  * gradients are multiplied as the sum of two bfloat16 (16 bits, off by 2^-16 of
  * each) in calls too small to fill the chip: where batch times kv_heads times the
- * tiles of 128 rows (of dk and dv: keys) are below 256, up to 320 of causal heads of
- * at most 64 elements; out also where at most 32 rows share a key head, generation's
- * form.  Larger calls round them to bfloat16 (half a step, 2^-8 of each), as do dk
- * and dv of many rows for few keys.
+ * tiles of 128 rows (of dk and dv: keys) are below 256, with causal = 1 and many keys
+ * up to 320; out also where at most 32 rows share a key head, generation's form.
+ * Larger calls round them to bfloat16 (half a step, 2^-8 of each), as do dk and dv of
+ * many rows for few keys.
  *
  * batch times kv_heads times the tiles of 128 rows (or keys) stay below 2^24.
  *

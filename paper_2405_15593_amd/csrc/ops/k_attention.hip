@@ -16,7 +16,7 @@
 // (alone they run at 1.6), vector instructions 42% of the time, no bank conflicts.
 // Two waves a SIMD interleave them; eight waves in two groups that take turns at
 // the two kinds of work gave 1%.  The bound of few rows is memory: one query of 32
-// heads on 8 over 8 x 4096 keys 24 us and 4 for the join (134 MB, 5.5 TB/s).
+// heads on 8 over 8 x 4096 keys 25 us and 4 for the join (134 MB, 5.4 TB/s).
 #include <algorithm>
 
 #include "attention_tile.h"
